@@ -115,7 +115,8 @@ typedef enum {
     ATTNW_ERR_UNSUPPORTED = -4, /* d not a multiple of 16 (bf16) / 4 (fp32) or above 256; a dimension beyond the 32-bit grid limits */
     ATTNW_ERR_ALIGN = -5,       /* a base pointer is not 16-byte aligned */
     ATTNW_ERR_ALIAS = -6,       /* output overlaps an input */
-    ATTNW_ERR_LAUNCH = -7       /* the HIP runtime refused the launch */
+    ATTNW_ERR_LAUNCH = -7,      /* the HIP runtime refused the launch */
+    ATTNW_ERR_WORKSPACE = -8    /* a workspace smaller than the call needs */
 } attnw_status;
 
 /*
@@ -224,6 +225,149 @@ int attnw_scale(const void *X, void *Y, int64_t count, float scale,
 int attnw_attention(const void *Q, const void *K, const void *V, void *O,
                     int64_t B, int64_t H, int64_t N, int64_t d,
                     float scale, int dtype, void *stream);
+
+/*
+ * Serving with a paged cache: rotary positions, appending new tokens to the cache,
+ * attention of new tokens over it, the weight that its slots collect, and eviction by
+ * it.  Unlike the calls above these take a description of the cache (and a rule of the
+ * scores) by address; it is read during the call and not kept.
+ *
+ * The cache.  Keys and values lie in pages of page_size slots, K and V being
+ * [pages][kv_heads][page_size][d].  Slot j of sequence b is row j % page_size of page
+ * table[b][j / page_size]; lengths[b] of a sequence's slots are in use.  Sequences may
+ * share pages that are only read.  A ragged batch of new tokens is a dense array of rows,
+ * sequence b owning rows starts[b] .. starts[b + 1] - 1 (starts: batch + 1 numbers, in
+ * order, the last one at most `tokens`); its n new tokens are its LAST n slots, token i
+ * at slot lengths[b] - n + i: lengths count them already.
+ *
+ * table, lengths, starts, positions and prefix are read by the kernels, in stream order, so that
+ * calls can be recorded and replayed while they change.  What they hold cannot be refused by
+ * the host; it is brought into range instead, so that nothing outside the arrays is read or written: a page
+ * id outside 0 .. pages - 1 is written to by nobody and reads as the nearest page, a
+ * length above max_pages * page_size counts as that, tokens before a sequence's first slot are not
+ * cached, see nothing but the prefix, and count as empty rows where that is empty.
+ *
+ * Types: as above (ATTNW_F32, ATTNW_BF16; fp32 products and sums on the fp32
+ * instruction, bf16 weights rounded to bf16 before they multiply V).  d up to 256, a multiple of 16 (bf16) or 4
+ * (fp32); page_size any; up to 2^30 slots a sequence; heads a multiple of kv_heads, query
+ * head h using kv head h / (heads / kv_heads).  Data pointers 16-byte aligned, the
+ * others as their type.  Strides are in elements, from one token's row to the next.
+ */
+typedef struct attnw_cache {
+    void *K, *V;                /* [pages][kv_heads][page_size][d] */
+    const int32_t *table;       /* [batch][max_pages] */
+    int32_t *lengths;           /* [batch] */
+    int64_t batch, pages, max_pages, page_size, kv_heads, d;
+    int32_t dtype;              /* attnw_dtype of K, V and of what meets them */
+} attnw_cache;
+
+/*
+ * What a new token at slot i makes of slot j:
+ *   x = scale * q . k;   x = cap * tanh(x / cap) where cap > 0;   x = x - slopes[h] * |i - j| where slopes are given,
+ * for the slots it sees: j <= i, of those the last `window` (itself among them) where
+ * window > 0; and every slot below prefix[b] in any case.  Other slots have no part in
+ * the result, whatever K and V hold there (NaN included).  Distances are counted in slots.
+ */
+typedef struct attnw_rule {
+    float scale, cap;
+    const float *slopes;        /* [heads] or NULL */
+    const int32_t *prefix;      /* [batch] or NULL */
+    int64_t window;             /* 0: none */
+} attnw_rule;
+
+/* Columns that turn together: (j, j + rot / 2), or (2 j, 2 j + 1). */
+typedef enum {
+    ATTNW_HALVES = 0,
+    ATTNW_PAIRS = 1
+} attnw_layout;
+
+/*
+ * The table of a rotation of `rot` columns (even, up to 256), row p: gain * cos(p f_j) at
+ * column j, gain * sin(p f_j) at rot / 2 + j, j < rot / 2, p < positions, rounded once from 64 bits.
+ *   f_j = base^(-2 j / rot) * (k_j + (1 - k_j) / factor),  k_j = 0, 1 or in between as
+ * the turns that column j makes in `original` tokens are at most `low`, at least `high` or in
+ * between: factor 1 leaves the frequencies alone, low = high = infinity slows all of them (positions
+ * interpolated), finite ones only the slow columns.
+ */
+int attnw_rotary_table(float *table, int64_t positions, int64_t rot, double base,
+                       double factor, double low, double high, double original,
+                       double gain, void *stream);
+
+/*
+ * Rotary positions:  the first rot columns of every head turn by the angles of row
+ * positions[t] of the table ([rows][rot]), the others are copied.  inverse != 0: the transposed
+ * map, which is the gradient of the other (and the other way back where gain is 1).
+ *
+ * X, Y : tokens rows of `heads` heads of d elements, x_stride and y_stride apart.  Y == X with
+ * equal strides (in place: heads of a wider row, queries and keys of a projection) is allowed,
+ * any other overlap is ATTNW_ERR_ALIAS.  d up to 256, any; rot even, up to d.
+ * A token whose position the table does not have comes out as NaN in its turned columns.
+ */
+int attnw_rotary(const void *X, void *Y, const float *table, const int32_t *positions,
+                 int64_t tokens, int64_t heads, int64_t d, int64_t rot, int64_t rows,
+                 int64_t x_stride, int64_t y_stride, int layout, int inverse, int dtype,
+                 void *stream);
+
+/*
+ * New tokens into the cache, one launch:  R = Q turned ([tokens][heads][d], dense), keys
+ * turned and values as they are into the tokens' slots.  rot = 0: nothing turns (table may be NULL);
+ * heads = 0: no queries (Q and R may be NULL).  positions NULL: a token's slot is its position.
+ * Q == R with q_stride == heads * d (in place) is allowed.  The pages of new
+ * tokens must not be shared between sequences.
+ */
+int attnw_cache_append(const attnw_cache *cache, const void *Q, const void *K,
+                       const void *V, void *R, const float *table,
+                       const int32_t *positions, const int32_t *starts, int64_t tokens,
+                       int64_t heads, int64_t rot, int64_t rows, int64_t q_stride,
+                       int64_t kv_stride, int layout, void *stream);
+
+/* Bytes of workspace that attnw_paged_attention needs at most for calls of these sizes on this
+ * cache (0: none), or a negative attnw_status.  Lengths and tables play no part. */
+int64_t attnw_paged_workspace(const attnw_cache *cache, int64_t tokens, int64_t heads);
+
+/*
+ * Attention of the new tokens over the cache, their own slots among them (append first):
+ *   O[t][h] = sum_j w_j V_j,  w = softmax of x over the slots that token t sees,
+ *   lse[t][h] = log sum_j exp(x_j)   (lse may be NULL).
+ * A row that sees nothing gives 0 and -infinity.  Rows of tokens that no sequence owns are
+ * not written.
+ *
+ * Q : rows of heads * d, q_stride apart (a multiple of 16 bytes).   O : [tokens][heads][d], dense.
+ * workspace: at least attnw_paged_workspace bytes, 16-byte aligned, of any content; calls that
+ * may run at the same time need one each.  Two launches at most.
+ */
+int attnw_paged_attention(const attnw_cache *cache, const attnw_rule *rule, const void *Q,
+                          void *O, float *lse, const int32_t *starts, int64_t tokens,
+                          int64_t heads, int64_t q_stride, void *workspace,
+                          int64_t workspace_bytes, void *stream);
+
+/*
+ * The weight that slots collect from the new tokens:
+ *   sums[b][g][j] = before[b][g][j] + sum over the new tokens i and heads h of kv head g of exp(x_ij - lse_ih),
+ * j < lengths[b]; [batch][kv_heads][max_pages * page_size] each, the new tokens' own slots
+ * starting from 0, before NULL: all of them.  Q, lse, starts as attnw_paged_attention had
+ * them; sums == before (in place) is allowed.  Rows whose lse is -infinity add nothing.  V is not looked at.
+ */
+int attnw_paged_sums(const attnw_cache *cache, const attnw_rule *rule, const void *Q,
+                     const float *lse, const float *before, float *sums,
+                     const int32_t *starts, int64_t tokens, int64_t heads,
+                     int64_t q_stride, void *stream);
+
+/*
+ * Eviction:  of every sequence longer than `keep` slots each kv head keeps the last `recent` ones and, of the
+ * others, the keep - recent of the largest sums (equal ones: the lower slot; NaN less than
+ * anything), in their order; shorter sequences keep all.  Rows of K and V and sums are copied to the slots
+ * 0 .. of the cache `into`, into->lengths[b] = min(lengths[b], keep), and
+ * kept[b][g][i] ([batch][kv_heads][keep]) is the slot that slot i was, -1 behind the last.
+ *
+ * `into`: same batch, kv_heads, d and dtype, room for keep >= 1 slots.  Its K and V may be the
+ * arrays of `cache` (one pool), its lengths too; its pages must then be others than those that
+ * any sequence still reads.  (Nothing is moved in place: pages shared with other sequences stay as they are.)
+ * sums and into_sums: [batch][kv_heads][max_pages * page_size] of their caches.
+ */
+int attnw_cache_evict(const attnw_cache *cache, const attnw_cache *into,
+                      const float *sums, float *into_sums, int32_t *kept, int64_t keep,
+                      int64_t recent, void *stream);
 
 /* Human-readable name of a status code; never NULL. */
 const char *attnw_status_string(int status);

@@ -8,10 +8,21 @@ raises if the library has not been built - there is no CPU fallback.
 from .binding import (  # noqa: F401
     ATTNW_BF16,
     ATTNW_F32,
+    ATTNW_HALVES,
+    ATTNW_PAIRS,
+    AttnwCache,
     AttnwError,
+    AttnwRule,
     attnw_attention,
+    attnw_cache_append,
+    attnw_cache_evict,
     attnw_fused,
     attnw_gemm_scores,
+    attnw_paged_attention,
+    attnw_paged_sums,
+    attnw_paged_workspace,
+    attnw_rotary,
+    attnw_rotary_table,
     attnw_scale,
     attnw_softmax,
     attnw_softmax_cast,

@@ -26,6 +26,8 @@ from typing import Optional
 
 ATTNW_F32 = 0
 ATTNW_BF16 = 1
+ATTNW_HALVES = 0
+ATTNW_PAIRS = 1
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
@@ -34,7 +36,8 @@ _LIB = os.path.join(_PKG, "libattnw.so")
 _ENTRY = os.path.join(_PKG, "_entry.so")
 
 EXPORTS = ("attnw_fused", "attnw_softmax", "attnw_softmax_cast", "attnw_gemm_scores", "attnw_scale", "attnw_attention",
-           "attnw_status_string", "attnw_version")
+           "attnw_rotary_table", "attnw_rotary", "attnw_cache_append", "attnw_paged_workspace", "attnw_paged_attention",
+           "attnw_paged_sums", "attnw_cache_evict", "attnw_status_string", "attnw_version")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -47,6 +50,8 @@ _entry = None
 _entries = {}               # the public functions by name
 _points = []                # (function that one stands for, kinds of its arguments, what it looks `direct` up in)
 _direct = {}                # the callables of _entry.so among what they call
+_word_points = []           # the same for entry points of addresses and whole numbers in any order
+_word_direct = {}
 
 
 class AttnwError(RuntimeError):
@@ -92,7 +97,7 @@ def build(verbose: bool = False) -> str:
         run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *[o for _, o in jobs], "-o", _LIB])
     global _lib
     _lib = None
-    for entry in _direct.values():                # (their C functions are the old library's)
+    for entry in [*_direct.values(), *_word_direct.values()]:     # (their C functions are the old library's)
         entry.bind(0)
     _attach()
     return _LIB
@@ -119,12 +124,23 @@ def load_library():
         lib.attnw_softmax_cast.restype = ci
         lib.attnw_scale.argtypes = [vp, vp, i64, ctypes.c_float, ci, vp]
         lib.attnw_scale.restype = ci
+        cd = ctypes.c_double
+        lib.attnw_rotary_table.argtypes = [vp, i64, i64, cd, cd, cd, cd, cd, cd, vp]
+        lib.attnw_rotary.argtypes = [vp] * 4 + [i64] * 7 + [ci] * 3 + [vp]
+        lib.attnw_cache_append.argtypes = [vp] * 8 + [i64] * 6 + [ci, vp]
+        lib.attnw_paged_workspace.argtypes = [vp, i64, i64]
+        lib.attnw_paged_attention.argtypes = [vp] * 6 + [i64] * 3 + [vp, i64, vp]
+        lib.attnw_paged_sums.argtypes = [vp] * 7 + [i64] * 3 + [vp]
+        lib.attnw_cache_evict.argtypes = [vp] * 5 + [i64] * 2 + [vp]
+        for name in ("rotary_table", "rotary", "cache_append", "paged_attention", "paged_sums", "cache_evict"):
+            getattr(lib, f"attnw_{name}").restype = ci
+        lib.attnw_paged_workspace.restype = i64
         lib.attnw_status_string.argtypes = [ci]
         lib.attnw_status_string.restype = ctypes.c_char_p
         lib.attnw_version.argtypes = []
         lib.attnw_version.restype = ci
         _lib = lib
-        for name, entry in _direct.items():
+        for name, entry in [*_direct.items(), *_word_direct.items()]:
             entry.bind(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value)
     return _lib
 
@@ -135,6 +151,14 @@ def _ptr(x) -> Optional[int]:
     if hasattr(x, "data_ptr"):
         return int(x.data_ptr())
     return int(x)
+
+
+def _struct(x, kind) -> Optional[int]:
+    if x is None:
+        return None
+    if not isinstance(x, kind):                   # (the host reads it: an address of anything else would crash the process)
+        raise TypeError(f"{kind.__name__} expected, not {type(x).__name__}")
+    return x._address
 
 
 def _stream(stream) -> Optional[int]:
@@ -158,18 +182,26 @@ def attnw_version() -> int:
     return int(load_library().attnw_version())
 
 
+def _in_front(function, points, kinds):
+    """A function of the same signature that calls what its scope has as `direct`: `function`, until _attach puts a callable of ``_entry.so`` there."""
+    name, arguments = function.__name__, ", ".join(inspect.signature(function).parameters)
+    scope = {"direct": function}
+    exec(f"def {name}({arguments}):\n    return direct({arguments})", scope)
+    points.append((function, kinds, scope))
+    _entries[name] = functools.update_wrapper(scope[name], function)
+    _entries[name].__defaults__ = function.__defaults__
+    return _entries[name]
+
+
 def _entry_point(pointers: int, sizes: int, scales: int, dtypes: int):
     """The function by way of a callable of ``_entry.so``, for arguments: pointers, sizes, a scale, element types, a stream.  What
     is returned is a function still, of the same signature (copied, pickled, referred to weakly, inspected, bound like one)."""
-    def wrap(function):
-        name, arguments = function.__name__, ", ".join(inspect.signature(function).parameters)
-        scope = {"direct": function}
-        exec(f"def {name}({arguments}):\n    return direct({arguments})", scope)
-        _points.append((function, (pointers, sizes, scales, dtypes), scope))
-        _entries[name] = functools.update_wrapper(scope[name], function)
-        _entries[name].__defaults__ = function.__defaults__
-        return _entries[name]
-    return wrap
+    return lambda function: _in_front(function, _points, (pointers, sizes, scales, dtypes))
+
+
+def _word_entry_point(kinds: str):
+    """The same for arguments of the given kinds (s: a structure, p: an address, i: a whole number, n: one of 32 bits) and a stream."""
+    return lambda function: _in_front(function, _word_points, (kinds,))
 
 
 def _attach() -> None:
@@ -185,6 +217,12 @@ def _attach() -> None:
         return
     for function, kinds, scope in _points:
         scope["direct"] = _direct[function.__name__] = _entry.Entry(function, _check, *kinds)
+    try:
+        entries = [_entry.Words(function, _check, *kinds) for function, kinds, _ in _word_points]
+    except (AttributeError, ValueError):          # (built from sources older than this file: ctypes alone for these until the next build)
+        return
+    for (function, _, scope), entry in zip(_word_points, entries):
+        scope["direct"] = _word_direct[function.__name__] = entry
 
 
 @_entry_point(3, 4, 1, 1)
@@ -225,6 +263,87 @@ def attnw_attention(Q, K, V, O, B: int, H: int, N: int, d: int, scale: float, dt
     """O = softmax(scale * Q K^T) V, weights kept on chip; see ``attnw_attention`` in include/attnw.h."""
     _check(load_library().attnw_attention(_ptr(Q), _ptr(K), _ptr(V), _ptr(O), B, H, N, d, float(scale), int(dtype),
                                           _stream(stream)))
+
+
+class AttnwCache(ctypes.Structure):
+    """A paged cache; see ``attnw_cache`` in include/attnw.h.  K, V, table and lengths: addresses or tensors, which it keeps alive."""
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("batch", ctypes.c_int64), ("pages", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("page_size", ctypes.c_int64),
+                ("kv_heads", ctypes.c_int64), ("d", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+    def __init__(self, K, V, table, lengths, batch: int, pages: int, max_pages: int, page_size: int, kv_heads: int, d: int, dtype: int):
+        super().__init__(_ptr(K), _ptr(V), _ptr(table), _ptr(lengths), batch, pages, max_pages, page_size, kv_heads, d, dtype)
+        self._kept = (K, V, table, lengths)
+        self._address = ctypes.addressof(self)
+
+
+class AttnwRule(ctypes.Structure):
+    """What scores are made of beside the products, and what a token sees; see ``attnw_rule`` in include/attnw.h."""
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("prefix", ctypes.c_void_p),
+                ("window", ctypes.c_int64)]
+
+    def __init__(self, scale: float, cap: float = 0.0, slopes=None, prefix=None, window: int = 0):
+        super().__init__(scale, cap, _ptr(slopes), _ptr(prefix), window)
+        self._kept = (slopes, prefix)
+        self._address = ctypes.addressof(self)
+
+
+def _cache(x) -> Optional[int]:
+    return _struct(x, AttnwCache)
+
+
+def _rule(x) -> Optional[int]:
+    return _struct(x, AttnwRule)
+
+
+def attnw_rotary_table(table, positions: int, rot: int, base: float = 10000.0, factor: float = 1.0, low: float = 0.0,
+                       high: float = 0.0, original: float = 0.0, gain: float = 1.0, stream=None) -> None:
+    """Cosines and sines of rotary positions; see ``attnw_rotary_table`` in include/attnw.h."""
+    _check(load_library().attnw_rotary_table(_ptr(table), positions, rot, base, factor, low, high, original, gain, _stream(stream)))
+
+
+@_word_entry_point("ppppiiiiiiinnn")
+def attnw_rotary(X, Y, table, positions, tokens: int, heads: int, d: int, rot: int, rows: int, x_stride: int, y_stride: int, layout: int,
+                 inverse: int, dtype: int, stream=None) -> None:
+    """Y = X with rotary positions, or the gradient of that; see ``attnw_rotary`` in include/attnw.h."""
+    _check(load_library().attnw_rotary(_ptr(X), _ptr(Y), _ptr(table), _ptr(positions), tokens, heads, d, rot, rows, x_stride, y_stride,
+                                       int(layout), int(inverse), int(dtype), _stream(stream)))
+
+
+@_word_entry_point("spppppppiiiiiin")
+def attnw_cache_append(cache, Q, K, V, R, table, positions, starts, tokens: int, heads: int, rot: int, rows: int, q_stride: int,
+                       kv_stride: int, layout: int, stream=None) -> None:
+    """Queries turned, keys turned and values into the cache; see ``attnw_cache_append`` in include/attnw.h."""
+    _check(load_library().attnw_cache_append(_cache(cache), _ptr(Q), _ptr(K), _ptr(V), _ptr(R), _ptr(table), _ptr(positions), _ptr(starts),
+                                             tokens, heads, rot, rows, q_stride, kv_stride, int(layout), _stream(stream)))
+
+
+def attnw_paged_workspace(cache, tokens: int, heads: int) -> int:
+    """Bytes of workspace that ``attnw_paged_attention`` needs; see include/attnw.h."""
+    size = int(load_library().attnw_paged_workspace(_cache(cache), tokens, heads))
+    _check(min(size, 0))
+    return size
+
+
+@_word_entry_point("ssppppiiipi")
+def attnw_paged_attention(cache, rule, Q, O, lse, starts, tokens: int, heads: int, q_stride: int, workspace, workspace_bytes: int,
+                          stream=None) -> None:
+    """Attention of new tokens over a paged cache; see ``attnw_paged_attention`` in include/attnw.h."""
+    _check(load_library().attnw_paged_attention(_cache(cache), _rule(rule), _ptr(Q), _ptr(O), _ptr(lse), _ptr(starts), tokens, heads, q_stride,
+                                                _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+@_word_entry_point("sspppppiii")
+def attnw_paged_sums(cache, rule, Q, lse, before, sums, starts, tokens: int, heads: int, q_stride: int, stream=None) -> None:
+    """The weight that slots collect from new tokens; see ``attnw_paged_sums`` in include/attnw.h."""
+    _check(load_library().attnw_paged_sums(_cache(cache), _rule(rule), _ptr(Q), _ptr(lse), _ptr(before), _ptr(sums), _ptr(starts), tokens, heads,
+                                           q_stride, _stream(stream)))
+
+
+@_word_entry_point("sspppii")
+def attnw_cache_evict(cache, into, sums, into_sums, kept, keep: int, recent: int, stream=None) -> None:
+    """The slots that collected the most weight into other pages; see ``attnw_cache_evict`` in include/attnw.h."""
+    _check(load_library().attnw_cache_evict(_cache(cache), _cache(into), _ptr(sums), _ptr(into_sums), _ptr(kept), keep, recent, _stream(stream)))
 
 
 _attach()

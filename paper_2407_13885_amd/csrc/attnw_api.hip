@@ -11,7 +11,7 @@
 
 namespace {
 
-constexpr int kVersion = 104;   // 0.1.4: major * 10000 + minor * 100 + patch; a patch step per entry point added since 0.1.0
+constexpr int kVersion = 111;   // 0.1.11: major * 10000 + minor * 100 + patch; a patch step per entry point added since 0.1.0
 
 bool mul_overflows(int64_t a, int64_t b, int64_t* out)
 {
@@ -174,6 +174,7 @@ const char* attnw_status_string(int status)
     case ATTNW_ERR_ALIGN: return "pointer not 16-byte aligned";
     case ATTNW_ERR_ALIAS: return "output overlaps an input";
     case ATTNW_ERR_LAUNCH: return "kernel launch failed";
+    case ATTNW_ERR_WORKSPACE: return "workspace smaller than the call needs";
     default: return "unknown status";
     }
 }

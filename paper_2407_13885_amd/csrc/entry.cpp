@@ -11,6 +11,8 @@
 #include <climits>
 #include <cstddef>
 #include <cstdint>
+#include <cstring>
+#include <utility>
 
 namespace {
 
@@ -25,7 +27,7 @@ struct Entry {
     int pointers, sizes, has_scale, dtypes;
 };
 
-PyObject *s_data_ptr, *s_cuda_stream;
+PyObject *s_data_ptr, *s_cuda_stream, *s_address;
 
 // 1: converted, 0: not of the expected kind, -1: an exception is set
 int address(PyObject* x, PyObject* attribute, bool method, void** out)
@@ -165,6 +167,128 @@ PyMethodDef entry_methods[] = {{"bind", entry_bind, METH_O, "bind(address): the 
                                {nullptr, nullptr, 0, nullptr}};
 
 PyTypeObject entry_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
+// The same for entry points that take addresses and whole numbers only (in any order, the stream last): a whole number is passed in the place of
+// an address alike, and a C function that takes an int reads the low half of it.
+constexpr int kMostWords = 18;
+struct Words {
+    PyObject_HEAD
+    vectorcallfunc call;
+    PyObject *any, *check;
+    void* fn;
+    int count;
+    char kinds[kMostWords];                       // 's' a structure of the binding, 'p' an address, 'i' a whole number of 64 bits, 'n' one of 32; the stream is not among them
+};
+
+template <int... I> int words_invoke(void* fn, const i64* w, std::integer_sequence<int, I...>)
+{
+    return reinterpret_cast<int (*)(decltype(static_cast<void>(I), i64())...)>(fn)(w[I]...);
+}
+
+// `words` arguments, of which there are at most kMostWords
+template <int N = 1> int words_invoke(void* fn, const i64* w, int words)
+{
+    if constexpr (N > kMostWords) return 0;
+    else return words == N ? words_invoke(fn, w, std::make_integer_sequence<int, N>()) : words_invoke<N + 1>(fn, w, words);
+}
+
+PyObject* words_call(PyObject* self, PyObject* const* args, size_t nargsf, PyObject* names)
+{
+    Words* const e = reinterpret_cast<Words*>(self);
+    const Py_ssize_t given = PyVectorcall_NARGS(nargsf);
+    if (e->fn && (!names || PyTuple_GET_SIZE(names) == 0) && (given == e->count || given == e->count + 1)) {
+        i64 w[kMostWords];
+        int ok = 1;
+        for (int i = 0; ok > 0 && i < e->count; ++i) {
+            if (e->kinds[i] == 's') {             // (an address of anything else would be read as one: the Python function refuses it)
+                void* p = nullptr;
+                ok = PyLong_CheckExact(args[i]) ? 0 : address(args[i], s_address, false, &p);
+                w[i] = static_cast<i64>(reinterpret_cast<uintptr_t>(p));
+            } else if (e->kinds[i] == 'p') {
+                void* p = nullptr;
+                ok = address(args[i], s_data_ptr, true, &p);
+                w[i] = static_cast<i64>(reinterpret_cast<uintptr_t>(p));
+            } else {
+                ok = whole(args[i], &w[i]);
+                if (ok > 0 && e->kinds[i] == 'n' && (w[i] < INT_MIN || w[i] > INT_MAX)) ok = 0;
+            }
+        }
+        void* stream = nullptr;
+        if (ok > 0 && given > e->count) ok = address(args[e->count], s_cuda_stream, false, &stream);
+        if (ok < 0) return nullptr;
+        if (ok > 0) {
+            int status;
+            w[e->count] = static_cast<i64>(reinterpret_cast<uintptr_t>(stream));
+            Py_BEGIN_ALLOW_THREADS
+            status = words_invoke(e->fn, w, e->count + 1);
+            Py_END_ALLOW_THREADS
+            if (status == 0) Py_RETURN_NONE;
+            PyObject* const code = PyLong_FromLong(status);
+            if (!code) return nullptr;
+            PyObject* const r = PyObject_CallOneArg(e->check, code);
+            Py_DECREF(code);
+            return r;
+        }
+    }
+    return PyObject_Vectorcall(e->any, args, nargsf, names);
+}
+
+// Words(function, check, kinds)
+int words_init(PyObject* self, PyObject* args, PyObject*)
+{
+    Words* const e = reinterpret_cast<Words*>(self);
+    PyObject *any, *check;
+    const char* kinds;
+    if (!PyArg_ParseTuple(args, "OOs", &any, &check, &kinds)) return -1;
+    const size_t count = strlen(kinds);
+    if (count < 1 || count >= kMostWords || strspn(kinds, "spin") != count) {
+        PyErr_SetString(PyExc_ValueError, "no such entry point");
+        return -1;
+    }
+    Py_XSETREF(e->any, Py_NewRef(any));
+    Py_XSETREF(e->check, Py_NewRef(check));
+    e->fn = nullptr;
+    e->count = static_cast<int>(count);
+    memcpy(e->kinds, kinds, count);
+    e->call = words_call;
+    return 0;
+}
+
+PyObject* words_bind(PyObject* self, PyObject* arg)
+{
+    void* const fn = PyLong_AsVoidPtr(arg);
+    if (PyErr_Occurred()) return nullptr;
+    reinterpret_cast<Words*>(self)->fn = fn;
+    Py_RETURN_NONE;
+}
+
+int words_traverse(PyObject* self, visitproc visit, void* arg)
+{
+    Words* const e = reinterpret_cast<Words*>(self);
+    Py_VISIT(e->any);
+    Py_VISIT(e->check);
+    return 0;
+}
+
+int words_clear(PyObject* self)
+{
+    Words* const e = reinterpret_cast<Words*>(self);
+    Py_CLEAR(e->any);
+    Py_CLEAR(e->check);
+    return 0;
+}
+
+void words_dealloc(PyObject* self)
+{
+    PyObject_GC_UnTrack(self);
+    words_clear(self);
+    Py_TYPE(self)->tp_free(self);
+}
+
+PyMethodDef words_methods[] = {{"bind", words_bind, METH_O, "bind(address): the C function, from now on called directly"},
+                               {nullptr, nullptr, 0, nullptr}};
+
+PyTypeObject words_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_entry", "Entry points of libattnw.so as Python callables.", -1, nullptr};
 
 }  // namespace
@@ -173,7 +297,8 @@ PyMODINIT_FUNC PyInit__entry(void)
 {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!s_data_ptr || !s_cuda_stream) return nullptr;
+    s_address = PyUnicode_InternFromString("_address");
+    if (!s_data_ptr || !s_cuda_stream || !s_address) return nullptr;
     entry_type.tp_name = "paper_2407_13885_amd._entry.Entry";
     entry_type.tp_basicsize = sizeof(Entry);
     entry_type.tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_HAVE_VECTORCALL | Py_TPFLAGS_HAVE_GC;
@@ -186,8 +311,21 @@ PyMODINIT_FUNC PyInit__entry(void)
     entry_type.tp_clear = entry_clear;
     entry_type.tp_methods = entry_methods;
     if (PyType_Ready(&entry_type) < 0) return nullptr;
+    words_type.tp_name = "paper_2407_13885_amd._entry.Words";
+    words_type.tp_basicsize = sizeof(Words);
+    words_type.tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_HAVE_VECTORCALL | Py_TPFLAGS_HAVE_GC;
+    words_type.tp_vectorcall_offset = offsetof(Words, call);
+    words_type.tp_call = PyVectorcall_Call;
+    words_type.tp_new = PyType_GenericNew;
+    words_type.tp_init = words_init;
+    words_type.tp_dealloc = words_dealloc;
+    words_type.tp_traverse = words_traverse;
+    words_type.tp_clear = words_clear;
+    words_type.tp_methods = words_methods;
+    if (PyType_Ready(&words_type) < 0) return nullptr;
     PyObject* const m = PyModule_Create(&module_def);
     if (!m) return nullptr;
     if (PyModule_AddObject(m, "Entry", Py_NewRef(reinterpret_cast<PyObject*>(&entry_type))) < 0) return nullptr;
+    if (PyModule_AddObject(m, "Words", Py_NewRef(reinterpret_cast<PyObject*>(&words_type))) < 0) return nullptr;
     return m;
 }

@@ -1,0 +1,225 @@
+// Shared by the kernels of the paged cache: how a slot is found, what a row of queries sees, how the work of a ragged batch is dealt out.
+//
+// What comes from device memory (lengths, starts, page ids) cannot be checked before the launch; the kernels bring it into range where they
+// read it, so that nothing outside the caller's arrays is touched whatever it holds.
+#pragma once
+
+#include "device_utils.h"
+#include "launchers.h"
+
+namespace attnw {
+
+// n / d for 0 <= n < 2^31 (d >= 1): with 2^l >= d, m = ceil(2^(31 + l) / d) is at most 2^32 - 1 and m d - 2^(31 + l) < d <= 2^l, so that
+// floor(n m / 2^(31 + l)) is exact.
+struct FastDiv {
+    uint32_t d, m, shift;
+};
+inline FastDiv fast_div(uint32_t d)
+{
+    uint32_t l = 0;
+    while (((uint64_t)1 << l) < d) ++l;
+    const uint64_t one = (uint64_t)1 << (31 + l);
+    return {d, (uint32_t)((one + d - 1) / d), 31 + l};
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const FastDiv& f) { return (uint32_t)(((uint64_t)n * f.m) >> f.shift); }
+
+// The cache as kernels take it.
+struct CacheView {
+    const char *K, *V;
+    const int32_t *table, *lengths;
+    int64_t page_bytes, head_bytes;               // of a page, of one head's rows in it
+    int32_t batch, pages, max_pages, kv_heads, slots, row_bytes;   // slots: a sequence can have
+    FastDiv page;
+};
+
+// Slots of sequence b in use, new tokens of it and its first row of the call.
+struct Sequence {
+    int32_t length, tokens, first;
+};
+__device__ __forceinline__ Sequence sequence_at(const CacheView& c, const int32_t* starts, int32_t all, int b)
+{
+    Sequence s;
+    s.length = max(0, min(c.lengths[b], c.slots));
+    s.first = max(0, min(starts[b], all));
+    s.tokens = max(0, min(starts[b + 1], all) - s.first);
+    return s;
+}
+
+// Bytes from the start of K or V to slot j (in range) of a sequence's head.
+__device__ __forceinline__ int64_t slot_offset(const CacheView& c, const int32_t* pages_of, int kv_head, int j)
+{
+    const uint32_t p = quotient((uint32_t)j, c.page);
+    const int32_t id = max(0, min(pages_of[p], c.pages - 1));
+    return id * c.page_bytes + kv_head * c.head_bytes + (int64_t)(j - (int)(p * c.page.d)) * c.row_bytes;
+}
+
+// What the scores are made of beside the products.
+struct RuleView {
+    float scale, cap;
+    const float* slopes;
+    const int32_t* prefix;
+    int32_t window;                               // at most 2^30 (no window: 2^30, more than any sequence has)
+};
+
+// A score as exponent of 2: scale (or cap) and log2(e) in it.  EXACT: tanh to fp32's last bits instead of by way of 2^x (off by 2^-23).
+template <bool CAPPED, bool EXACT> struct ScoreMap {
+    float c, inner;                               // dot -> c dot, or c tanh(inner dot)
+    __device__ __forceinline__ explicit ScoreMap(const RuleView& r)
+    {
+        c = (CAPPED ? r.cap : r.scale) * kLog2e;
+        inner = !CAPPED ? 0.0f : EXACT ? r.scale / r.cap : r.scale / r.cap * (2.0f * kLog2e);
+    }
+    __device__ __forceinline__ float operator()(float dot) const
+    {
+        if constexpr (!CAPPED) return dot * c;
+        else if constexpr (EXACT) return c * tanhf(dot * inner);
+        else return c * (1.0f - 2.0f * __builtin_amdgcn_rcpf(fast_exp2(dot * inner) + 1.0f));
+    }
+};
+
+// Of 16 bytes of elements T: whether one is infinite or NaN; those as 1 and the others as 0; those as 0.
+template <typename T> __device__ __forceinline__ uint32_t lost_bits(uint32_t w)
+{
+    if constexpr (sizeof(T) == 4) return (w & 0x7f800000u) == 0x7f800000u ? 0xffffffffu : 0u;
+    else return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+template <typename T> __device__ __forceinline__ bool any_lost(const u32x4& v)
+{
+    return (lost_bits<T>(v[0]) | lost_bits<T>(v[1]) | lost_bits<T>(v[2]) | lost_bits<T>(v[3])) != 0;
+}
+template <typename T> __device__ __forceinline__ u32x4 lost_as_one(const u32x4& v)
+{
+    const uint32_t one = sizeof(T) == 4 ? 0x3f800000u : 0x3f803f80u;
+    return u32x4{lost_bits<T>(v[0]) & one, lost_bits<T>(v[1]) & one, lost_bits<T>(v[2]) & one, lost_bits<T>(v[3]) & one};
+}
+template <typename T> __device__ __forceinline__ u32x4 without_lost(const u32x4& v)
+{
+    return u32x4{v[0] & ~lost_bits<T>(v[0]), v[1] & ~lost_bits<T>(v[1]), v[2] & ~lost_bits<T>(v[2]), v[3] & ~lost_bits<T>(v[3])};
+}
+
+__device__ __forceinline__ int64_t wave_inclusive_sum(int64_t v, int lane)
+{
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int64_t o = __shfl_up(v, off, 64);
+        if (lane >= off) v += o;
+    }
+    return v;
+}
+
+// The work of a ragged batch as one list: a query block (rows of one kv head of one sequence) is `units` places of it, one for each `unit` keys
+// that its last rows see.  A workgroup takes `per` consecutive places, so that long and short sequences load all of them alike; a block whose
+// places fall to several of them leaves partial results, which a second launch joins.  Every block of a sequence has the same
+// number of places: a block whose rows see fewer keys has them spread over its places.
+struct PlanShape {
+    int32_t rows, unit, group;                    // rows of a block, keys of a place, query heads of a kv head
+    int32_t workgroups, least;                    // to deal to; places worth a workgroup of its own
+};
+struct SequencePlan {
+    int32_t blocks;                               // of one kv head
+    int32_t units;                                // places of a block
+};
+__device__ __forceinline__ SequencePlan sequence_plan(const PlanShape& p, const Sequence& s, int32_t prefix, int32_t window)
+{
+    SequencePlan r;
+    r.blocks = (int32_t)(((int64_t)s.tokens * p.group + p.rows - 1) / p.rows);
+    const int32_t all = (s.length + p.unit - 1) / p.unit;
+    // a block's rows belong to at most this many tokens, which together see a window and so many keys more
+    const int32_t span = min((p.rows + p.group - 2) / p.group + 1, s.tokens);
+    const int32_t near = (int32_t)(((int64_t)window + span + p.unit - 2) / p.unit) + 2;
+    const int32_t first = (max(0, min(prefix, s.length)) + p.unit - 1) / p.unit;
+    r.units = max(1, min(all, first + near));
+    return r;
+}
+
+// All places of a batch (a wave's lanes count the sequences), `count(b)` being those of sequence b.
+template <typename Count>
+__device__ __forceinline__ int64_t plan_total(int batch, int lane, Count&& count)
+{
+    int64_t sum = 0;
+    for (int b = lane; b < batch; b += 64) sum += count(b);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    return sum;
+}
+// (the sequence that holds place `at` of the total, and the places before it)
+template <typename Count>
+__device__ __forceinline__ void plan_find(int batch, int lane, int64_t at, Count&& count, int32_t& found, int64_t& before)
+{
+    int64_t base = 0;
+    for (int b0 = 0; b0 < batch; b0 += 64) {
+        const int64_t mine = b0 + lane < batch ? count(b0 + lane) : 0;
+        const int64_t end = base + wave_inclusive_sum(mine, lane);
+        const uint64_t past = __builtin_amdgcn_ballot_w64(end > at);
+        if (past) {
+            const int first = __builtin_ctzll(past);
+            found = b0 + first;
+            before = __shfl(end - mine, first, 64);
+            return;
+        }
+        base = __shfl(end, 63, 64);
+    }
+    found = -1;
+    before = base;
+}
+
+// Keys that the rows at positions first .. last of a sequence see, as places of `unit` keys: [0, head) and [tail, end).
+struct Span {
+    int32_t head, tail, end;
+    __device__ __forceinline__ int32_t count() const { return head + end - tail; }
+    __device__ __forceinline__ int32_t unit(int32_t i) const { return i < head ? i : tail + (i - head); }
+};
+__device__ __forceinline__ Span visible_span(int32_t unit, int32_t first, int32_t last, int32_t length, int32_t prefix, int32_t window)
+{
+    Span s;
+    s.head = (min(prefix, length) + unit - 1) / unit;
+    const int32_t low = max(0, first - window + 1);
+    s.tail = max(s.head, low / unit);
+    s.end = max(s.tail, (last + unit) / unit);    // (last + 1 + unit - 1) / unit; last >= -1 rounded towards zero gives 0 there
+    return s;
+}
+
+// Launchers (arguments validated).
+hipError_t launch_rotary_table(float* table, int64_t positions, int64_t rot, double base, double factor, double low, double high, double original,
+                               double gain, hipStream_t stream);
+struct RotaryArgs {
+    DType dt;
+    const void *Q, *K, *V;                        // K, V: null where only Q is turned
+    void *R, *Kc, *Vc;
+    const float* angles;
+    const int32_t *positions, *starts;
+    int64_t tokens, heads, d, rot, rows, q_stride, kv_stride, r_stride;
+    bool interleaved, inverse;
+    CacheView cache;                              // (where K, V are given)
+};
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+
+struct PagedArgs {
+    DType dt;
+    CacheView cache;
+    RuleView rule;
+    const void* Q;
+    void* O;
+    float *lse, *workspace;
+    const int32_t* starts;
+    int64_t tokens, heads, d, q_stride;
+};
+int64_t paged_workspace(DType dt, const CacheView& cache, int64_t tokens, int64_t heads, int64_t d);
+hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t stream);
+
+struct SumsArgs {
+    DType dt;
+    CacheView cache;
+    RuleView rule;
+    const void* Q;
+    const float *lse, *before;
+    float* sums;
+    const int32_t* starts;
+    int64_t tokens, heads, d, q_stride;
+};
+hipError_t launch_paged_sums(const SumsArgs& a, hipStream_t stream);
+
+hipError_t launch_evict(const CacheView& from, const CacheView& into, int32_t* into_lengths, const float* sums, float* into_sums, int32_t* kept,
+                        int64_t keep, int64_t recent, hipStream_t stream);
+
+}  // namespace attnw
