@@ -249,7 +249,7 @@ int attnw_attention(const void *Q, const void *K, const void *V, void *O,
  *
  * Types: as above (ATTNW_F32, ATTNW_BF16; fp32 products and sums on the fp32
  * instruction, bf16 weights rounded to bf16 before they multiply V).  d up to 256, a multiple of 16 (bf16) or 4
- * (fp32); page_size any; up to 2^30 slots a sequence; heads a multiple of kv_heads, query
+ * (fp32); page_size any (a page under 4 GiB); up to 2^30 slots a sequence; heads a multiple of kv_heads, query
  * head h using kv head h / (heads / kv_heads).  Data pointers 16-byte aligned, the
  * others as their type.  Strides are in elements, from one token's row to the next.
  */
@@ -335,6 +335,8 @@ int64_t attnw_paged_workspace(const attnw_cache *cache, int64_t tokens, int64_t 
  * Q : rows of heads * d, q_stride apart (a multiple of 16 bytes).   O : [tokens][heads][d], dense.
  * workspace: at least attnw_paged_workspace bytes, 16-byte aligned, of any content; calls that
  * may run at the same time need one each.  Two launches at most.
+ * (ATTNW_PAGED_KERNEL=rows / =tiles in the environment, read at every call of this function and of the one
+ * before it, puts all bf16 calls on the kernel for few / for many rows; unset, the sizes decide.)
  */
 int attnw_paged_attention(const attnw_cache *cache, const attnw_rule *rule, const void *Q,
                           void *O, float *lse, const int32_t *starts, int64_t tokens,

@@ -125,7 +125,7 @@ void evict_move_kernel(CacheView from, CacheView into, int32_t* into_lengths, co
         const uint32_t p = quotient(row, into.page);
         const int32_t id = into.table[(int64_t)b * into.max_pages + p];
         if ((uint32_t)id >= (uint32_t)into.pages) continue;    // no such page: nothing is moved
-        const int64_t to = id * into.page_bytes + h * into.head_bytes + (int64_t)(row - p * into.page.d) * into.row_bytes + c * 16;
+        const int64_t to = (int64_t)((uint64_t)(uint32_t)id * into.page_bytes) + (uint32_t)h * into.head_bytes + (row - p * into.page.d) * (uint32_t)into.row_bytes + c * 16;
         const int64_t at = slot_offset(from, from.table + (int64_t)b * from.max_pages, h, slot) + c * 16;
         const uint4 k = *reinterpret_cast<const uint4*>(from.K + at), v = *reinterpret_cast<const uint4*>(from.V + at);
         *reinterpret_cast<uint4*>(const_cast<char*>(into.K) + to) = k;

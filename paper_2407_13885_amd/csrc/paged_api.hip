@@ -47,7 +47,8 @@ int check_support(const attnw_cache* c)
     const int64_t most = (int64_t)1 << 30;
     int64_t heads;
     if (c->pages > most || c->batch > most || c->kv_heads > (1 << 16) || c->max_pages * c->page_size > kMostSlots ||
-        mul_overflows(c->batch, c->kv_heads, &heads) || heads > (1 << 23))
+        mul_overflows(c->batch, c->kv_heads, &heads) || heads > (1 << 23) ||
+        c->kv_heads * c->page_size * c->d * size_of(c->dtype) >= (int64_t)1 << 32)   // (a page: offsets in it have 32 bits)
         return ATTNW_ERR_UNSUPPORTED;
     return ATTNW_OK;
 }
@@ -72,8 +73,8 @@ CacheView view(const attnw_cache* c)
     v.table = c->table;
     v.lengths = c->lengths;
     v.row_bytes = (int32_t)(c->d * size_of(c->dtype));
-    v.head_bytes = c->page_size * v.row_bytes;
-    v.page_bytes = c->kv_heads * v.head_bytes;
+    v.head_bytes = (uint32_t)(c->page_size * v.row_bytes);
+    v.page_bytes = (uint32_t)(c->kv_heads * v.head_bytes);
     v.batch = (int32_t)c->batch;
     v.pages = (int32_t)c->pages;
     v.max_pages = (int32_t)c->max_pages;
@@ -245,7 +246,12 @@ int64_t attnw_paged_workspace(const attnw_cache* cache, int64_t tokens, int64_t 
     if ((e = check_call(cache, &rule, tokens, heads, wide)) != ATTNW_OK) return e;
     if (cache->batch == 0 || tokens == 0 || heads == 0) return 0;
     if ((e = check_call_support(cache, &rule, tokens, heads, wide)) != ATTNW_OK) return e;
-    return attnw::paged_workspace(static_cast<DType>(cache->dtype), view(cache), tokens, heads, cache->d);
+    attnw::PagedArgs a{};
+    a.dt = static_cast<DType>(cache->dtype);
+    a.cache = view(cache);
+    a.tokens = tokens;
+    a.heads = heads;
+    return attnw::paged_workspace(a);
 }
 
 int attnw_paged_attention(const attnw_cache* cache, const attnw_rule* rule, const void* Q, void* O, float* lse, const int32_t* starts, int64_t tokens,
@@ -260,7 +266,19 @@ int attnw_paged_attention(const attnw_cache* cache, const attnw_rule* rule, cons
     if ((e = check_pointers(cache)) != ATTNW_OK) return e;
     if (!Q || !O || !starts) return ATTNW_ERR_NULL;
     if ((e = check_call_support(cache, rule, tokens, heads, q_stride)) != ATTNW_OK) return e;
-    const int64_t need = attnw::paged_workspace(static_cast<DType>(cache->dtype), view(cache), tokens, heads, cache->d);
+    attnw::PagedArgs a{};
+    a.dt = static_cast<DType>(cache->dtype);
+    a.cache = view(cache);
+    a.rule = view(rule);
+    a.Q = Q;
+    a.O = O;
+    a.lse = lse;
+    a.workspace = static_cast<float*>(workspace);
+    a.starts = starts;
+    a.tokens = tokens;
+    a.heads = heads;
+    a.q_stride = q_stride;
+    const int64_t need = attnw::paged_workspace(a);
     if (need > 0 && !workspace) return ATTNW_ERR_NULL;
     if (workspace_bytes < need) return ATTNW_ERR_WORKSPACE;
     if (!cache_aligned(cache) || !aligned(Q, 16) || !aligned(O, 16) || !aligned(lse, 4) || !aligned(starts, 4) || !aligned(workspace, 16) ||
@@ -278,19 +296,6 @@ int attnw_paged_attention(const attnw_cache* cache, const attnw_rule* rule, cons
         for (const Range& o : written)
             if (&o != &w && o.at && o.bytes && overlaps(w.at, w.bytes, o.at, o.bytes)) return ATTNW_ERR_ALIAS;
     }
-    attnw::PagedArgs a{};
-    a.dt = static_cast<DType>(cache->dtype);
-    a.cache = view(cache);
-    a.rule = view(rule);
-    a.Q = Q;
-    a.O = O;
-    a.lse = lse;
-    a.workspace = static_cast<float*>(workspace);
-    a.starts = starts;
-    a.tokens = tokens;
-    a.heads = heads;
-    a.d = cache->d;
-    a.q_stride = q_stride;
     return status(attnw::launch_paged_attention(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -332,7 +337,6 @@ int attnw_paged_sums(const attnw_cache* cache, const attnw_rule* rule, const voi
     a.starts = starts;
     a.tokens = tokens;
     a.heads = heads;
-    a.d = cache->d;
     a.q_stride = q_stride;
     return status(attnw::launch_paged_sums(a, static_cast<hipStream_t>(stream)));
 }

@@ -9,25 +9,29 @@
 
 namespace attnw {
 
-// n / d for 0 <= n < 2^31 (d >= 1): with 2^l >= d, m = ceil(2^(31 + l) / d) is at most 2^32 - 1 and m d - 2^(31 + l) < d <= 2^l, so that
-// floor(n m / 2^(31 + l)) is exact.
+// n / d for 0 <= n < 2^31, d >= 1.  With 2^l >= d > 2^(l - 1), m = ceil(2^(31 + l) / d) is at most 2^32 - 1 for d > 1 and m d - 2^(31 + l) < d <= 2^l, so
+// that floor(n m / 2^(31 + l)) is exact; d = 1 has m = 0 and n itself added.
 struct FastDiv {
-    uint32_t d, m, shift;
+    uint32_t d, m, shift, self;
 };
 inline FastDiv fast_div(uint32_t d)
 {
-    uint32_t l = 0;
+    if (d == 1) return {1, 0, 0, ~0u};
+    uint32_t l = 1;
     while (((uint64_t)1 << l) < d) ++l;
     const uint64_t one = (uint64_t)1 << (31 + l);
-    return {d, (uint32_t)((one + d - 1) / d), 31 + l};
+    return {d, (uint32_t)((one + d - 1) / d), l - 1, 0};
 }
-__device__ __forceinline__ uint32_t quotient(uint32_t n, const FastDiv& f) { return (uint32_t)(((uint64_t)n * f.m) >> f.shift); }
+__host__ __device__ __forceinline__ uint32_t quotient(uint32_t n, const FastDiv& f)
+{
+    return ((uint32_t)(((uint64_t)n * f.m) >> 32) >> f.shift) + (n & f.self);
+}
 
 // The cache as kernels take it.
 struct CacheView {
     const char *K, *V;
     const int32_t *table, *lengths;
-    int64_t page_bytes, head_bytes;               // of a page, of one head's rows in it
+    uint32_t page_bytes, head_bytes;              // of a page, of one head's rows in it
     int32_t batch, pages, max_pages, kv_heads, slots, row_bytes;   // slots: a sequence can have
     FastDiv page;
 };
@@ -50,7 +54,7 @@ __device__ __forceinline__ int64_t slot_offset(const CacheView& c, const int32_t
 {
     const uint32_t p = quotient((uint32_t)j, c.page);
     const int32_t id = max(0, min(pages_of[p], c.pages - 1));
-    return id * c.page_bytes + kv_head * c.head_bytes + (int64_t)(j - (int)(p * c.page.d)) * c.row_bytes;
+    return (int64_t)((uint64_t)(uint32_t)id * c.page_bytes) + (uint32_t)kv_head * c.head_bytes + (uint32_t)(j - (int)(p * c.page.d)) * (uint32_t)c.row_bytes;
 }
 
 // What the scores are made of beside the products.
@@ -77,24 +81,40 @@ template <bool CAPPED, bool EXACT> struct ScoreMap {
     }
 };
 
-// Of 16 bytes of elements T: whether one is infinite or NaN; those as 1 and the others as 0; those as 0.
-template <typename T> __device__ __forceinline__ uint32_t lost_bits(uint32_t w)
+// Of 16 bytes of elements T: whether one is infinite or NaN; those as 1 and the others as 0; those as 0.  (An exponent of ones carries into the sign's
+// place when one is added at its end.)
+template <typename T> __device__ __forceinline__ uint32_t lost_signs(uint32_t w)
 {
-    if constexpr (sizeof(T) == 4) return (w & 0x7f800000u) == 0x7f800000u ? 0xffffffffu : 0u;
-    else return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+    if constexpr (sizeof(T) == 4) return ((w & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+    else return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
 }
-template <typename T> __device__ __forceinline__ bool any_lost(const u32x4& v)
+template <typename T> __device__ __forceinline__ uint32_t any_lost(const u32x4& v)
 {
-    return (lost_bits<T>(v[0]) | lost_bits<T>(v[1]) | lost_bits<T>(v[2]) | lost_bits<T>(v[3])) != 0;
+    return lost_signs<T>(v[0]) | lost_signs<T>(v[1]) | lost_signs<T>(v[2]) | lost_signs<T>(v[3]);
 }
 template <typename T> __device__ __forceinline__ u32x4 lost_as_one(const u32x4& v)
 {
-    const uint32_t one = sizeof(T) == 4 ? 0x3f800000u : 0x3f803f80u;
-    return u32x4{lost_bits<T>(v[0]) & one, lost_bits<T>(v[1]) & one, lost_bits<T>(v[2]) & one, lost_bits<T>(v[3]) & one};
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (lost_signs<T>(v[i]) >> 1) - (lost_signs<T>(v[i]) >> 8);   // 0x40.. - 0x00800..
+    return r;
 }
 template <typename T> __device__ __forceinline__ u32x4 without_lost(const u32x4& v)
 {
-    return u32x4{v[0] & ~lost_bits<T>(v[0]), v[1] & ~lost_bits<T>(v[1]), v[2] & ~lost_bits<T>(v[2]), v[3] & ~lost_bits<T>(v[3])};
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t t = lost_signs<T>(v[i]);
+        r[i] = v[i] & ~(sizeof(T) == 4 ? (uint32_t)((int32_t)t >> 31) : (t << 1) - (t >> 15));
+    }
+    return r;
+}
+
+// A value that all lanes of a wave have, as one that the compiler knows they have.
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)x) | (int64_t)__builtin_amdgcn_readfirstlane((int32_t)(x >> 32)) << 32;
 }
 
 __device__ __forceinline__ int64_t wave_inclusive_sum(int64_t v, int lane)
@@ -140,7 +160,7 @@ __device__ __forceinline__ int64_t plan_total(int batch, int lane, Count&& count
     for (int b = lane; b < batch; b += 64) sum += count(b);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    return sum;
+    return uniform(sum);
 }
 // (the sequence that holds place `at` of the total, and the places before it)
 template <typename Count>
@@ -154,10 +174,10 @@ __device__ __forceinline__ void plan_find(int batch, int lane, int64_t at, Count
         if (past) {
             const int first = __builtin_ctzll(past);
             found = b0 + first;
-            before = __shfl(end - mine, first, 64);
+            before = uniform(__shfl(end - mine, first, 64));
             return;
         }
-        base = __shfl(end, 63, 64);
+        base = uniform(__shfl(end, 63, 64));
     }
     found = -1;
     before = base;
@@ -202,10 +222,17 @@ struct PagedArgs {
     void* O;
     float *lse, *workspace;
     const int32_t* starts;
-    int64_t tokens, heads, d, q_stride;
+    int64_t tokens, heads, q_stride;
 };
-int64_t paged_workspace(DType dt, const CacheView& cache, int64_t tokens, int64_t heads, int64_t d);
+int64_t paged_workspace(const PagedArgs& a);       // (of a, sizes alone)
 hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t stream);
+// Blocks of 16 rows, each wave with keys of its own: any call.
+int64_t paged_rows_workspace(const PagedArgs& a);
+hipError_t launch_paged_rows(const PagedArgs& a, hipStream_t stream);
+// bf16, blocks of 128 or 256 rows, which share the keys: any call, for chunks.
+bool prefers_paged_tiles(const PagedArgs& a);
+int64_t paged_tiles_workspace(const PagedArgs& a);
+hipError_t launch_paged_tiles(const PagedArgs& a, hipStream_t stream);
 
 struct SumsArgs {
     DType dt;
@@ -215,7 +242,7 @@ struct SumsArgs {
     const float *lse, *before;
     float* sums;
     const int32_t* starts;
-    int64_t tokens, heads, d, q_stride;
+    int64_t tokens, heads, q_stride;
 };
 hipError_t launch_paged_sums(const SumsArgs& a, hipStream_t stream);
 

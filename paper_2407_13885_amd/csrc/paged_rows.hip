@@ -9,9 +9,7 @@
 // from memory, one tile under way while it computes another, and no barrier ties the waves together; they meet once a segment, when their
 // partial results are joined.  The places of a ragged batch are dealt out evenly (PlanShape): a sequence of 16384 slots beside 63 short ones is
 // shared by as many workgroups as its length is worth.
-#include "qk_common.h"
-#include "attention_common.h"
-#include "paged_common.h"
+#include "paged_attention.h"
 
 namespace attnw {
 namespace {
@@ -36,46 +34,9 @@ template <typename T, int UB> struct RowsCfg {
     static_assert(STAGES <= kDirectLds && FIT >= 2);
 };
 
-// At most N transfers under way, and no read from LDS before that.
-template <int N> __device__ __forceinline__ void arrived()
-{
-    wait_vmem_le<N>();
-#if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("" ::: "memory");
-#endif
-}
-
-struct RowsArgs {
-    const char* Q;
-    char* O;
-    float *lse, *partial;
-    const int32_t* starts;
-    int64_t q_stride;                             // bytes of a token's row of Q
-    int32_t tokens, heads, group;
-    CacheView cache;
-    RuleView rule;
-    PlanShape plan;
-};
-
-struct Counted {
-    const RowsArgs& a;
-    __device__ __forceinline__ int64_t operator()(int b) const
-    {
-        const Sequence s = sequence_at(a.cache, a.starts, a.tokens, b);
-        const SequencePlan p = sequence_plan(a.plan, s, a.rule.prefix ? a.rule.prefix[b] : 0, a.rule.window);
-        return (int64_t)p.blocks * p.units * a.cache.kv_heads;
-    }
-};
-
-__device__ __forceinline__ int64_t places_each(const PlanShape& p, int64_t total)
-{
-    const int64_t even = (total + p.workgroups - 1) / p.workgroups;
-    return even > p.least ? even : p.least;
-}
-
 template <typename T, int UB, bool GENERAL, int THREADS = 64 * RowsCfg<T, UB>::NW>
 __global__ __launch_bounds__(THREADS)
-void paged_rows_kernel(RowsArgs a)
+void paged_rows_kernel(AttendArgs a)
 {
     using C = RowsCfg<T, UB>;
     using L = RowLayout<UB>;
@@ -101,7 +62,6 @@ void paged_rows_kernel(RowsArgs a)
     int32_t b;
     int64_t before;
     plan_find(a.cache.batch, lane, at, count, b, before);
-    b = __builtin_amdgcn_readfirstlane(b);
 
     const ScoreMap<false, F32> plain(a.rule);
     bool first_segment = true;
@@ -130,7 +90,7 @@ void paged_rows_kernel(RowsArgs a)
         const int first = base + (int)(row0 / a.group), last = base + (int)((row0 + rows - 1) / a.group);
         const int64_t row = row0 + min(l16, rows - 1);
         const int token = (int)(row / a.group), head = kv_head * a.group + (int)(row - (int64_t)token * a.group);
-        const int query = base + token, low = query - a.rule.window;   // sees low < j <= query
+        const int query = base + token;   // sees the slots query - window + 1 .. query
         const float slope = GENERAL && a.rule.slopes ? a.rule.slopes[head] * kLog2e : 0.0f;
 
         u32x4 qf[UB];
@@ -171,7 +131,8 @@ void paged_rows_kernel(RowsArgs a)
                     // a lane's key of the tile (lanes KT .. again the same ones), past the end the last
                     const int slot = min(key0 + (lane & (KT - 1)), k1 - 1);
                     const uint32_t p = quotient(slot, a.cache.page);
-                    const int64_t off = ids[p - p0] * a.cache.page_bytes + (int64_t)(slot - (int)(p * a.cache.page.d)) * rb + kv_head * a.cache.head_bytes;
+                    const int64_t off = (int64_t)((uint64_t)(uint32_t)ids[p - p0] * a.cache.page_bytes) + (uint32_t)(slot - (int)(p * a.cache.page.d)) * (uint32_t)rb +
+                                        (uint32_t)kv_head * a.cache.head_bytes;
                     const int lo = (int)(uint32_t)off, hi = (int)(off >> 32);
 #pragma unroll
                     for (int v = 0; v < 2; ++v)
@@ -226,7 +187,7 @@ void paged_rows_kernel(RowsArgs a)
 #pragma unroll
                         for (int i = 0; i < NK * 4; ++i) {
                             const int j = key + 16 * (i / 4) + i % 4;
-                            if (!(j < k1 && ((j <= query && j > low) || j < prefix))) x[i] = -__builtin_inff();
+                            if (j >= k1 || ((uint32_t)(query - j) >= (uint32_t)a.rule.window && j >= prefix)) x[i] = -__builtin_inff();
                         }
                     }
                     float top = x[0];
@@ -280,10 +241,10 @@ void paged_rows_kernel(RowsArgs a)
                     if (!whole) {
                         // A value that is no number must not reach the rows that do not see it, by way of a weight of 0: such values
                         // count as 0, and make the columns of the rows that do see them NaN.
-                        bool bad = false;
+                        uint32_t bad = 0;
 #pragma unroll
                         for (int c = 0; c < CB; ++c) bad |= any_lost<T>(v_frag(c));
-                        if (__builtin_amdgcn_ballot_w64(bad) != 0) {
+                        if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
                             float saw[NK * 4];
 #pragma unroll
                             for (int i = 0; i < NK * 4; ++i) saw[i] = x[i] == -__builtin_inff() ? 0.0f : 1.0f;
@@ -353,12 +314,8 @@ void paged_rows_kernel(RowsArgs a)
                 const int64_t rr = row0 + r;
                 const int tk = (int)(rr / a.group), h = kv_head * a.group + (int)(rr - (int64_t)tk * a.group);
                 const int64_t o = (int64_t)(seq.first + tk) * a.heads + h;
-                const f32x4 y = sum * (l == 0.0f ? 0.0f : 1.0f / l);
-                if (c * (int)sizeof(T) < rb) {
-                    if constexpr (F32) *reinterpret_cast<f32x4*>(a.O + o * rb + c * 4) = y;
-                    else *reinterpret_cast<u32x2*>(a.O + o * rb + c * 2) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-                }
-                if (c == 0 && a.lse) a.lse[o] = l == 0.0f ? -__builtin_inff() : (top + fast_log2(l)) * (1.0f / kLog2e);
+                store_output<T>(a.O, o, rb, c, sum, l);
+                if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
             } else {
                 *reinterpret_cast<f32x4*>(out + r * C::COLS + c) = sum;
                 if (c == 0) {
@@ -370,108 +327,25 @@ void paged_rows_kernel(RowsArgs a)
     }
 }
 
-// The partial results of blocks that several workgroups worked on.  A workgroup per (block, kv head).
-template <typename T>
-__global__ __launch_bounds__(256)
-void paged_join_kernel(RowsArgs a, int32_t cols)
-{
-    const int lane = threadIdx.x & 63;
-    const Counted count{a};
-    const int64_t total = plan_total(a.cache.batch, lane, count);
-    const int64_t per = places_each(a.plan, total);
-    const auto blocks = [&](int i) __attribute__((always_inline)) {
-        const Sequence s = sequence_at(a.cache, a.starts, a.tokens, i);
-        return (((int64_t)s.tokens * a.group + a.plan.rows - 1) / a.plan.rows) * a.cache.kv_heads;
-    };
-    for (int64_t x = blockIdx.x;; x += gridDim.x) {
-        int32_t b;
-        int64_t before;
-        plan_find(a.cache.batch, lane, x, blocks, b, before);
-        b = __builtin_amdgcn_readfirstlane(b);
-        if (b < 0) return;
-        const Sequence seq = sequence_at(a.cache, a.starts, a.tokens, b);
-        const SequencePlan plan = sequence_plan(a.plan, seq, a.rule.prefix ? a.rule.prefix[b] : 0, a.rule.window);
-        const int64_t mine = x - before;
-        const int kv_head = (int)(mine / plan.blocks), block = (int)(mine - (int64_t)kv_head * plan.blocks);
-        int64_t x0 = 0;
-        for (int i = lane; i < b; i += 64) x0 += count(i);
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) x0 += __shfl_xor(x0, off, 64);
-        x0 += mine * plan.units;
-        const int64_t w0 = x0 / per, w1 = (x0 + plan.units - 1) / per;
-        if (w0 == w1) continue;
-        const int64_t row0 = (int64_t)block * a.plan.rows;
-        const int rows = (int)min((int64_t)a.plan.rows, (int64_t)seq.tokens * a.group - row0);
-        const int64_t slot = (int64_t)a.plan.rows * (cols + 2);
-        const auto part = [&](int64_t w) __attribute__((always_inline)) { return a.partial + (2 * w + (w == w0 && w0 * per != x0 ? 1 : 0)) * slot; };
-        const int quads = cols / 4, rb = a.cache.row_bytes;
-        for (int i = threadIdx.x; i < rows * quads; i += 256) {
-            const int r = i / quads, c = (i - r * quads) * 4;
-            float top = -__builtin_inff();
-            for (int64_t w = w0; w <= w1; ++w) top = fmaxf(top, part(w)[a.plan.rows * cols + 2 * r]);
-            const float ref = top == -__builtin_inff() ? 0.0f : top;
-            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-            float l = 0.0f;
-#pragma unroll 4
-            for (int64_t w = w0; w <= w1; ++w) {
-                const float* p = part(w);
-                const float f = fast_exp2(p[a.plan.rows * cols + 2 * r] - ref);
-                l += f * p[a.plan.rows * cols + 2 * r + 1];
-                sum += *reinterpret_cast<const f32x4*>(p + r * cols + c) * f;
-            }
-            const int64_t rr = row0 + r;
-            const int tk = (int)(rr / a.group), h = kv_head * a.group + (int)(rr - (int64_t)tk * a.group);
-            const int64_t o = (int64_t)(seq.first + tk) * a.heads + h;
-            const f32x4 y = sum * (l == 0.0f ? 0.0f : 1.0f / l);
-            if (c * (int)sizeof(T) < rb) {
-                if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(a.O + o * rb + c * 4) = y;
-                else *reinterpret_cast<u32x2*>(a.O + o * rb + c * 2) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-            }
-            if (c == 0 && a.lse) a.lse[o] = l == 0.0f ? -__builtin_inff() : (top + fast_log2(l)) * (1.0f / kLog2e);
-        }
-    }
-}
-
-template <typename T, int UB> RowsArgs rows_args(const PagedArgs& p)
+template <typename T, int UB> PlanShape plan_of(const PagedArgs& p)
 {
     using C = RowsCfg<T, UB>;
-    RowsArgs a;
-    a.Q = static_cast<const char*>(p.Q);
-    a.O = static_cast<char*>(p.O);
-    a.lse = p.lse;
-    a.partial = p.workspace;
-    a.starts = p.starts;
-    a.q_stride = p.q_stride * (int64_t)sizeof(T);
-    a.tokens = (int32_t)p.tokens;
-    a.heads = (int32_t)p.heads;
-    a.group = (int32_t)(p.heads / p.cache.kv_heads);
-    a.cache = p.cache;
-    a.rule = p.rule;
-    a.plan = {kRows, C::UNIT, a.group, (compute_units() * C::PER_CU + 7) & ~7, 1};
-    return a;
+    return {kRows, C::UNIT, (int32_t)(p.heads / p.cache.kv_heads), (compute_units() * C::PER_CU + 7) & ~7, 1};
 }
 
 template <typename T, int UB> hipError_t launch(const PagedArgs& p, hipStream_t stream)
 {
     using C = RowsCfg<T, UB>;
-    const RowsArgs a = rows_args<T, UB>(p);
+    const AttendArgs a = attend_args(p, plan_of<T, UB>(p), sizeof(T));
     if (p.rule.cap > 0.0f || p.rule.slopes)
         paged_rows_kernel<T, UB, true><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a);
     else
         paged_rows_kernel<T, UB, false><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    // (every sequence may have one block that is not full)
-    const int64_t blocks = (p.tokens * a.group / kRows + p.cache.batch) * p.cache.kv_heads;
-    paged_join_kernel<T><<<(uint32_t)(blocks < 1 << 20 ? blocks : 1 << 20), 256, 0, stream>>>(a, C::COLS);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : launch_join<T>(a, C::COLS, stream);
 }
 
-template <typename T, int UB> int64_t workspace()
-{
-    using C = RowsCfg<T, UB>;
-    return (int64_t)((compute_units() * C::PER_CU + 7) & ~7) * 2 * kRows * (C::COLS + 2) * 4;
-}
+template <typename T, int UB> int64_t workspace(const PagedArgs& p) { return partial_bytes(plan_of<T, UB>(p), RowsCfg<T, UB>::COLS); }
 
 template <typename T, typename F> auto by_row(int row_bytes, F&& f)
 {
@@ -494,16 +368,23 @@ template <typename T, typename F> auto by_row(int row_bytes, F&& f)
 
 }  // namespace
 
-int64_t paged_workspace(DType dt, const CacheView& cache, int64_t, int64_t, int64_t)
+int64_t paged_rows_workspace(const PagedArgs& p)
 {
-    if (dt == DType::F32) return by_row<float>(cache.row_bytes, [&](auto ub) { return workspace<float, decltype(ub)::value>(); });
-    return by_row<uint16_t>(cache.row_bytes, [&](auto ub) { return workspace<uint16_t, decltype(ub)::value>(); });
+    if (p.dt == DType::F32) return by_row<float>(p.cache.row_bytes, [&](auto ub) { return workspace<float, decltype(ub)::value>(p); });
+    return by_row<uint16_t>(p.cache.row_bytes, [&](auto ub) { return workspace<uint16_t, decltype(ub)::value>(p); });
 }
 
-hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t stream)
+hipError_t launch_paged_rows(const PagedArgs& p, hipStream_t stream)
 {
-    if (a.dt == DType::F32) return by_row<float>(a.cache.row_bytes, [&](auto ub) { return launch<float, decltype(ub)::value>(a, stream); });
-    return by_row<uint16_t>(a.cache.row_bytes, [&](auto ub) { return launch<uint16_t, decltype(ub)::value>(a, stream); });
+    if (p.dt == DType::F32) return by_row<float>(p.cache.row_bytes, [&](auto ub) { return launch<float, decltype(ub)::value>(p, stream); });
+    return by_row<uint16_t>(p.cache.row_bytes, [&](auto ub) { return launch<uint16_t, decltype(ub)::value>(p, stream); });
+}
+
+int64_t paged_workspace(const PagedArgs& p) { return prefers_paged_tiles(p) ? paged_tiles_workspace(p) : paged_rows_workspace(p); }
+
+hipError_t launch_paged_attention(const PagedArgs& p, hipStream_t stream)
+{
+    return prefers_paged_tiles(p) ? launch_paged_tiles(p, stream) : launch_paged_rows(p, stream);
 }
 
 }  // namespace attnw

@@ -53,7 +53,6 @@ void paged_sums_kernel(SumsKernelArgs a)
     int32_t b;
     int64_t before;
     plan_find(a.cache.batch, lane, at, count, b, before);
-    b = __builtin_amdgcn_readfirstlane(b);
     const ScoreMap<false, F32> plain(a.rule);
 
     while (at < end && b < a.cache.batch) {

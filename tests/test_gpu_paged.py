@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2407_13885_amd as attnw
-from gpu_util import DT, TORCH_DT, require_gpu
+from gpu_util import DT, TORCH_DT, kernels, require_gpu
 from paged_util import Problem, evicted, within
 
 pytestmark = pytest.mark.gpu
@@ -53,6 +53,30 @@ def test_head_sizes(dtype, d):
     check_attention(Problem(dtype, [(1, 190), (18, 75)], 4, 2, d, 16, seed=d))
 
 
+@pytest.fixture(params=["rows", "tiles"])
+def kernel(request, monkeypatch):
+    monkeypatch.setenv("ATTNW_PAGED_KERNEL", request.param)
+    return request.param
+
+
+def test_either_kernel_of_a_shape(kernel):
+    p = Problem("bf16", [(1, 300), (9, 9)], 4, 2, 64, 16).on_gpu()
+    work = torch.empty(attnw.attnw_paged_workspace(p.cache, p.T, 4), dtype=torch.uint8, device="cuda")
+    O, d = torch.empty((p.T, 4, 64), dtype=torch.bfloat16, device="cuda"), p.dev
+    ran = kernels(lambda s: attnw.attnw_paged_attention(p.cache, p.rule, d["Q"], O, None, d["starts"], p.T, 4, p.q_stride, work, work.numel(), s))
+    assert f"paged_{kernel}_kernel" in ran[0]
+
+
+@pytest.mark.parametrize("name,sequences,heads,kv_heads,d,page", SHAPES, ids=[s[0] for s in SHAPES])
+def test_shapes_of_either_kernel(kernel, name, sequences, heads, kv_heads, d, page):
+    check_attention(Problem("bf16", sequences, heads, kv_heads, d, page, seed=len(name)))
+
+
+@pytest.mark.parametrize("d", [16, 32, 48, 64, 80, 96, 112, 128, 144, 160, 176, 192, 208, 256])
+def test_head_sizes_of_either_kernel(kernel, d):
+    check_attention(Problem("bf16", [(1, 190), (50, 775)], 4, 2, d, 16 if d % 64 else 24, seed=d))
+
+
 RULES = [
     ("cap", dict(cap=5.0, sharp=3.0)),
     ("bias by distance", dict(slopes=True)),
@@ -90,9 +114,10 @@ def test_rows_that_see_nothing(dtype):
     assert bool((O == 0).all()) and bool(torch.isneginf(lse).all())
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_what_is_hidden_has_no_part(dtype):
+@pytest.mark.parametrize("dtype,kernel_of", [("bf16", "rows"), ("bf16", "tiles"), ("f32", "")])
+def test_what_is_hidden_has_no_part(dtype, kernel_of, monkeypatch):
     """Keys and values of tokens that a row does not see may hold NaN and infinity: later ones of its chunk, ones in front of its window."""
+    monkeypatch.setenv("ATTNW_PAGED_KERNEL", kernel_of)
     for window, prefix in ((0, None), (30, None), (12, [5])):
         p = Problem(dtype, [(40, 100)], 4, 2, 64, 16, window=window, prefix=prefix)
         for slot, kind in ((99, math.nan), (80, math.inf), (62, -math.inf)):
@@ -197,6 +222,11 @@ def test_recorded_and_replayed():
         within(lse, want_lse, lse_off, "lse")
         want, bound = p.collected(lse.cpu(), None)
         within(sums, want, bound, "sums")
+
+
+@pytest.mark.parametrize("name,more", RULES, ids=[r[0] for r in RULES])
+def test_rules_of_either_kernel(kernel, name, more):
+    check_attention(Problem("bf16", [(1, 410), (40, 333), (150, 1020)], 8, 4, 64, 32, seed=3, **more))
 
 
 # ---- the weight that slots collect --------------------------------------------------------------------------------------------------------
