@@ -99,7 +99,7 @@ int check_call_support(const attnw_cache* c, const attnw_rule* r, int64_t tokens
 {
     const int e = check_support(c);
     if (e != ATTNW_OK) return e;
-    if (heads % c->kv_heads != 0 || heads > (1 << 16) || tokens > ((int64_t)1 << 30) || tokens * heads > ((int64_t)1 << 34)) return ATTNW_ERR_UNSUPPORTED;
+    if (heads % c->kv_heads != 0 || heads > (1 << 16) || tokens > ((int64_t)1 << 30) || tokens * heads > ((int64_t)1 << 30)) return ATTNW_ERR_UNSUPPORTED;
     if (q_stride < heads * c->d || q_stride * size_of(c->dtype) % 16 != 0) return ATTNW_ERR_UNSUPPORTED;
     if (!std::isfinite(r->scale) || !std::isfinite(r->cap)) return ATTNW_ERR_UNSUPPORTED;
     return ATTNW_OK;

@@ -39,12 +39,6 @@ struct Counted {
     }
 };
 
-__device__ __forceinline__ int64_t places_each(const PlanShape& p, int64_t total)
-{
-    const int64_t even = (total + p.workgroups - 1) / p.workgroups;
-    return even > p.least ? even : p.least;
-}
-
 // A row of partial results, or a whole one: 4 columns of the output of token, head (numbered o), l the sum of its weights.
 template <typename T> __device__ __forceinline__ void store_output(char* O, int64_t o, int rb, int c, f32x4 y, float l)
 {
@@ -64,7 +58,7 @@ void paged_join_kernel(AttendArgs a, int32_t cols)
     const int lane = threadIdx.x & 63;
     const Counted count{a};
     const int64_t total = plan_total(a.cache.batch, lane, count);
-    const int64_t per = places_each(a.plan, total);
+    const Deal deal = deal_out(total, a.plan.workgroups, a.plan.least);
     const auto blocks = [&](int i) __attribute__((always_inline)) {
         const Sequence s = sequence_at(a.cache, a.starts, a.tokens, i);
         return (((int64_t)s.tokens * a.group + a.plan.rows - 1) / a.plan.rows) * a.cache.kv_heads;
@@ -83,12 +77,13 @@ void paged_join_kernel(AttendArgs a, int32_t cols)
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) x0 += __shfl_xor(x0, off, 64);
         x0 = uniform(x0) + mine * plan.units;
-        const int64_t w0 = x0 / per, w1 = (x0 + plan.units - 1) / per;
+        const int64_t w0 = deal.owner(x0), w1 = deal.owner(x0 + plan.units - 1);
         if (w0 == w1) continue;
         const int64_t row0 = (int64_t)block * a.plan.rows;
         const int rows = (int)min((int64_t)a.plan.rows, (int64_t)seq.tokens * a.group - row0);
         const int64_t slot = (int64_t)a.plan.rows * (cols + 2);
-        const auto part = [&](int64_t w) __attribute__((always_inline)) { return a.partial + (2 * w + (w == w0 && w0 * per != x0 ? 1 : 0)) * slot; };
+        const bool later = deal.first(w0) != x0;   // (the first of them began with another block)
+        const auto part = [&](int64_t w) __attribute__((always_inline)) { return a.partial + (2 * w + (w == w0 && later ? 1 : 0)) * slot; };
         const int quads = cols / 4, rb = a.cache.row_bytes;
         for (int i = threadIdx.x; i < rows * quads; i += 256) {
             const int r = i / quads, c = (i - r * quads) * 4;

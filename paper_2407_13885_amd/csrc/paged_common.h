@@ -65,6 +65,10 @@ struct RuleView {
     int32_t window;                               // at most 2^30 (no window: 2^30, more than any sequence has)
 };
 
+// What a rule has beside the scale: kernels are built for each.
+enum : int { kPlain = 0, kCap = 1, kBias = 2 };
+inline int rule_mode(const RuleView& r) { return (r.cap > 0.0f ? kCap : kPlain) | (r.slopes ? kBias : kPlain); }
+
 // A score as exponent of 2: scale (or cap) and log2(e) in it.  EXACT: tanh to fp32's last bits instead of by way of 2^x (off by 2^-23).
 template <bool CAPPED, bool EXACT> struct ScoreMap {
     float c, inner;                               // dot -> c dot, or c tanh(inner dot)
@@ -77,7 +81,7 @@ template <bool CAPPED, bool EXACT> struct ScoreMap {
     {
         if constexpr (!CAPPED) return dot * c;
         else if constexpr (EXACT) return c * tanhf(dot * inner);
-        else return c * (1.0f - 2.0f * __builtin_amdgcn_rcpf(fast_exp2(dot * inner) + 1.0f));
+        else return __builtin_fmaf(-2.0f * c, __builtin_amdgcn_rcpf(fast_exp2(dot * inner) + 1.0f), c);
     }
 };
 
@@ -128,7 +132,7 @@ __device__ __forceinline__ int64_t wave_inclusive_sum(int64_t v, int lane)
 }
 
 // The work of a ragged batch as one list: a query block (rows of one kv head of one sequence) is `units` places of it, one for each `unit` keys
-// that its last rows see.  A workgroup takes `per` consecutive places, so that long and short sequences load all of them alike; a block whose
+// that its last rows see.  A workgroup takes as many consecutive places as any other (Deal), so that long and short sequences load all of them alike; a block whose
 // places fall to several of them leaves partial results, which a second launch joins.  Every block of a sequence has the same
 // number of places: a block whose rows see fewer keys has them spread over its places.
 struct PlanShape {
@@ -183,6 +187,31 @@ __device__ __forceinline__ void plan_find(int batch, int lane, int64_t at, Count
     before = base;
 }
 
+// The list dealt out: workgroup w has the places first(w) .. first(w + 1) - 1, numbers of `least` but at the end; all of them have some.
+struct Deal {
+    int64_t total;
+    int32_t workgroups, least;
+    __device__ __forceinline__ int64_t first(int64_t w) const { return w >= workgroups ? total : w * total / ((int64_t)workgroups * least) * least; }
+    __device__ __forceinline__ int64_t owner(int64_t x) const   // whose place x is
+    {
+        const int64_t w = ((x / least + 1) * workgroups * least - 1) / total;
+        return w < workgroups ? w : workgroups - 1;
+    }
+};
+__device__ __forceinline__ Deal deal_out(int64_t total, int32_t workgroups, int32_t least)
+{
+    const int64_t most = total / least;
+    return {total, most < 1 ? 1 : most < workgroups ? (int32_t)most : workgroups, least};
+}
+// Which workgroup a block of the launch is (-1: none): neighbours on one XCD, also where there are fewer than were launched.
+__device__ __forceinline__ int32_t dealt_workgroup(const Deal& d)
+{
+    const uint32_t padded = (d.workgroups + 7) & ~7u;
+    if (blockIdx.x >= padded) return -1;
+    const int32_t w = (int32_t)xcd_contiguous_block_id(blockIdx.x, padded);
+    return w < d.workgroups ? w : -1;
+}
+
 // Keys that the rows at positions first .. last of a sequence see, as places of `unit` keys: [0, head) and [tail, end).
 struct Span {
     int32_t head, tail, end;
@@ -227,12 +256,15 @@ struct PagedArgs {
 int64_t paged_workspace(const PagedArgs& a);       // (of a, sizes alone)
 hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t stream);
 // Blocks of 16 rows, each wave with keys of its own: any call.
-int64_t paged_rows_workspace(const PagedArgs& a);
-hipError_t launch_paged_rows(const PagedArgs& a, hipStream_t stream);
+int64_t paged_rows_workspace_f32(const PagedArgs& a);
+hipError_t launch_paged_rows_f32(const PagedArgs& a, hipStream_t stream);
 // bf16, blocks of 128 or 256 rows, which share the keys: any call, for chunks.
 bool prefers_paged_tiles(const PagedArgs& a);
 int64_t paged_tiles_workspace(const PagedArgs& a);
 hipError_t launch_paged_tiles(const PagedArgs& a, hipStream_t stream);
+hipError_t launch_paged_tiles_cap(const PagedArgs& a, hipStream_t stream);
+hipError_t launch_paged_tiles_bias(const PagedArgs& a, hipStream_t stream);
+hipError_t launch_paged_tiles_both(const PagedArgs& a, hipStream_t stream);
 
 struct SumsArgs {
     DType dt;

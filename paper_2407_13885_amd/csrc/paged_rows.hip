@@ -1,390 +1,16 @@
-// Attention of new tokens over a paged cache, blocks of 16 rows: single tokens and short chunks (any chunk in fp32).
-//
-//     O = softmax(s) V,  s = scale q . k  -> cap tanh(s / cap) -> s - slope |i - j|,  over the slots j that the token at slot i sees
-//
-// A row is one query head of one token; the heads of a kv head and their tokens share a block, so that K and V are read once for all of them.
-// The running maximum and sum of the softmax make one sweep over the keys enough.
-//
-// What bounds it: the read of K and V.  Nothing is used by two waves, so each wave brings its own tiles into LDS, 16 bytes a lane straight
-// from memory, one tile under way while it computes another, and no barrier ties the waves together; they meet once a segment, when their
-// partial results are joined.  The places of a ragged batch are dealt out evenly (PlanShape): a sequence of 16384 slots beside 63 short ones is
-// shared by as many workgroups as its length is worth.
-#include "paged_attention.h"
+// Attention over a paged cache by blocks of 16 rows (paged_rows.h), bf16; and which kernel a call goes to.
+#include "paged_rows.h"
 
 namespace attnw {
-namespace {
 
-constexpr int kRows = 16;                         // of a block
-constexpr int kIds = 1024;                        // page ids kept on chip at a time
-
-// UB: 64-byte groups of a row on chip.
-template <typename T, int UB> struct RowsCfg {
-    static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int KT = F32 ? 16 : 32;      // keys of a tile
-    static constexpr int DB = UB * 64, CPR = UB * 4, TILE = KT * DB, XFERS = TILE / 1024;
-    static constexpr int COLS = DB / (int)sizeof(T), CB = COLS / 16;
-    static constexpr int FIT = 128 * 1024 / (4 * TILE);
-    static constexpr int NW = FIT >= 8 ? 8 : FIT >= 4 ? 4 : 2;
-    static constexpr int UNIT = KT * NW;          // keys of a place
-    static constexpr int PITCH = COLS + 4;        // floats of a row of partial results
-    static constexpr int STAGES = NW * 4 * TILE;
-    static constexpr int LDS = STAGES + kIds * 4 + NW * kRows * 8;
-    static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;
-    static_assert(4 * TILE >= kRows * PITCH * 4, "partial results of a wave in its stages");
-    static_assert(STAGES <= kDirectLds && FIT >= 2);
-};
-
-template <typename T, int UB, bool GENERAL, int THREADS = 64 * RowsCfg<T, UB>::NW>
-__global__ __launch_bounds__(THREADS)
-void paged_rows_kernel(AttendArgs a)
+int64_t paged_workspace(const PagedArgs& p)
 {
-    using C = RowsCfg<T, UB>;
-    using L = RowLayout<UB>;
-    constexpr bool F32 = C::F32;
-    constexpr int NW = C::NW, KT = C::KT, DB = C::DB, CPR = C::CPR, TILE = C::TILE, XFERS = C::XFERS, CB = C::CB, NK = KT / 16, PITCH = C::PITCH;
-    __shared__ __align__(1024) char lds[C::LDS];
-    int32_t* const ids = reinterpret_cast<int32_t*>(lds + C::STAGES);
-    float* const stats = reinterpret_cast<float*>(lds + C::STAGES + kIds * 4);   // [wave][row]{maximum, sum}
-
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
-    char* const stage = lds + wave * 4 * TILE;    // K, V of one tile, K, V of the next
-    const uint32_t stage_at = lds_offset_of(stage);
-    const int rb = a.cache.row_bytes;
-
-    const Counted count{a};
-    const int64_t total = plan_total(a.cache.batch, lane, count);
-    const int64_t per = places_each(a.plan, total);
-    const int64_t w = xcd_contiguous_block_id(blockIdx.x, gridDim.x);
-    int64_t at = w * per;
-    const int64_t end = at + per < total ? at + per : total;
-    if (at >= end) return;
-    int32_t b;
-    int64_t before;
-    plan_find(a.cache.batch, lane, at, count, b, before);
-
-    const ScoreMap<false, F32> plain(a.rule);
-    bool first_segment = true;
-    for (; at < end && b < a.cache.batch; first_segment = false) {
-        const Sequence seq = sequence_at(a.cache, a.starts, a.tokens, b);
-        const int32_t prefix = a.rule.prefix ? max(0, min(a.rule.prefix[b], seq.length)) : 0;
-        const SequencePlan plan = sequence_plan(a.plan, seq, prefix, a.rule.window);
-        const int64_t in_head = (int64_t)plan.blocks * plan.units, here = at - before;
-        if (here >= in_head * a.cache.kv_heads) {
-            before += in_head * a.cache.kv_heads;
-            ++b;
-            continue;
-        }
-        const int kv_head = (int)(here / in_head);
-        const int64_t rest = here - kv_head * in_head;
-        const int block = (int)(rest / plan.units);
-        const int v0 = (int)(rest - (int64_t)block * plan.units);
-        const int v1 = (int)min((int64_t)plan.units, v0 + (end - at));
-        at += v1 - v0;
-
-        // ---- the rows of the block ------------------------------------------------------------------------------------------------
-        const int64_t all_rows = (int64_t)seq.tokens * a.group;
-        const int64_t row0 = (int64_t)block * kRows;
-        const int rows = (int)min((int64_t)kRows, all_rows - row0);
-        const int base = seq.length - seq.tokens;              // slot of the first new token
-        const int first = base + (int)(row0 / a.group), last = base + (int)((row0 + rows - 1) / a.group);
-        const int64_t row = row0 + min(l16, rows - 1);
-        const int token = (int)(row / a.group), head = kv_head * a.group + (int)(row - (int64_t)token * a.group);
-        const int query = base + token;   // sees the slots query - window + 1 .. query
-        const float slope = GENERAL && a.rule.slopes ? a.rule.slopes[head] * kLog2e : 0.0f;
-
-        u32x4 qf[UB];
-        {
-            const char* q = a.Q + (int64_t)(seq.first + token) * a.q_stride + (int64_t)head * rb;
-#pragma unroll
-            for (int g = 0; g < UB; ++g) {
-                const int ch = 4 * g + quarter;
-                qf[g] = ch * 16 < rb ? *reinterpret_cast<const u32x4*>(q + ch * 16) : u32x4{0u, 0u, 0u, 0u};
-            }
-        }
-        f32x4 oacc[CB];
-#pragma unroll
-        for (int c = 0; c < CB; ++c) oacc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        float m_run = -__builtin_inff(), l_run = 0.0f;
-
-        // ---- the keys of places v0 .. v1 - 1 -----------------------------------------------------------------------------------------
-        const Span span = visible_span(C::UNIT, first, last, seq.length, prefix, a.rule.window);
-        const int units = last < 0 && span.head == 0 ? 0 : span.count();
-        const int u0 = (int)((int64_t)v0 * units / plan.units), u1 = (int)((int64_t)v1 * units / plan.units);
-        const int seen = min(seq.length, max(prefix, last + 1));
-        const int32_t* const pages_of = a.cache.table + (int64_t)b * a.cache.max_pages;
-
-        auto sweep = [&](int from, int to) __attribute__((always_inline)) {   // keys
-            const int64_t most = min((int64_t)(kIds - 1) * a.cache.page.d, (int64_t)1 << 30);
-            for (int k0 = from; k0 < to;) {
-                // (whole places at a time, so that the waves' tiles stay where they are)
-                const int k1 = (int)min((int64_t)to, k0 + max((int64_t)C::UNIT, most / C::UNIT * C::UNIT));
-                const int p0 = quotient(k0, a.cache.page), p1 = quotient(k1 - 1, a.cache.page);
-                __syncthreads();
-                for (int p = p0 + threadIdx.x; p <= p1; p += 64 * NW) ids[p - p0] = max(0, min(pages_of[p], a.cache.pages - 1));
-                if (rb < DB)
-                    for (int i = lane; i < 4 * TILE / 16; i += 64) *reinterpret_cast<u32x4*>(stage + i * 16) = u32x4{0u, 0u, 0u, 0u};
-                wait_vmem();
-                __syncthreads();
-
-                auto issue = [&](int key0, int s) __attribute__((always_inline)) {
-                    // a lane's key of the tile (lanes KT .. again the same ones), past the end the last
-                    const int slot = min(key0 + (lane & (KT - 1)), k1 - 1);
-                    const uint32_t p = quotient(slot, a.cache.page);
-                    const int64_t off = (int64_t)((uint64_t)(uint32_t)ids[p - p0] * a.cache.page_bytes) + (uint32_t)(slot - (int)(p * a.cache.page.d)) * (uint32_t)rb +
-                                        (uint32_t)kv_head * a.cache.head_bytes;
-                    const int lo = (int)(uint32_t)off, hi = (int)(off >> 32);
-#pragma unroll
-                    for (int v = 0; v < 2; ++v)
-#pragma unroll
-                        for (int j = 0; j < XFERS; ++j) {
-                            const int x = j * 64 + lane, key = x / CPR, c = x - key * CPR;
-                            const int ch = v == 0 ? c ^ L::k_chunk(key)
-                                         : F32 ? c ^ ((UB % 4 == 0 ? (key >> 2) & 3 : UB % 4 == 2 ? (key >> 2) & 1 : 0) * 4)
-                                               : c ^ (L::v16_block(key) * 2);
-                            const int64_t o = (int64_t)(uint32_t)__shfl(lo, key, 64) | (int64_t)__shfl(hi, key, 64) << 32;
-                            if (ch * 16 < rb) dma16_untracked((v ? a.cache.V : a.cache.K) + o + ch * 16, stage_at + (2 * s + v) * TILE + j * 1024);
-                        }
-                };
-                auto compute = [&](int key0, int s, bool more) __attribute__((always_inline)) {
-                    const char* const kt = stage + 2 * s * TILE;
-                    const char* const vt = kt + TILE;
-                    if (more) arrived<3 * XFERS>();
-                    else arrived<XFERS>();
-                    float x[NK * 4];
-#pragma unroll
-                    for (int k = 0; k < NK; ++k) {
-                        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int g = 0; g < UB; ++g) {
-                            const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + (16 * k + l16) * DB + ((4 * g + quarter) ^ L::k_chunk(l16)) * 16);
-                            if constexpr (F32) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i]), __uint_as_float(qf[g][i]), acc, 0, 0, 0);
-                            } else {
-                                mma16(acc, kf, qf[g]);
-                            }
-                        }
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x[4 * k + r] = acc[r];
-                    }
-                    if (GENERAL && a.rule.cap > 0.0f) {
-                        const ScoreMap<true, F32> capped(a.rule);
-#pragma unroll
-                        for (int i = 0; i < NK * 4; ++i) x[i] = capped(x[i]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < NK * 4; ++i) x[i] = plain(x[i]);
-                    }
-                    const int key = key0 + 4 * quarter;        // + 16 k + r
-                    if constexpr (GENERAL) {
-#pragma unroll
-                        for (int i = 0; i < NK * 4; ++i) x[i] -= slope * (float)abs(query - (key + 16 * (i / 4) + i % 4));
-                    }
-                    const bool whole = key0 + KT <= k1 && ((key0 + KT - 1 <= first && key0 > last - a.rule.window) || key0 + KT <= prefix);
-                    if (!whole) {
-#pragma unroll
-                        for (int i = 0; i < NK * 4; ++i) {
-                            const int j = key + 16 * (i / 4) + i % 4;
-                            if (j >= k1 || ((uint32_t)(query - j) >= (uint32_t)a.rule.window && j >= prefix)) x[i] = -__builtin_inff();
-                        }
-                    }
-                    float top = x[0];
-#pragma unroll
-                    for (int i = 1; i < NK * 4; ++i) top = fmaxf(top, x[i]);
-                    top = quarter_wave_max(top);
-                    if (__builtin_amdgcn_ballot_w64(top > m_run) != 0) {
-                        const float m = fmaxf(m_run, top), alpha = m == -__builtin_inff() ? 1.0f : fast_exp2(m_run - m);
-                        l_run *= alpha;
-#pragma unroll
-                        for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
-                        m_run = m;
-                    }
-                    const float ref = m_run == -__builtin_inff() ? 0.0f : m_run;   // (nothing seen yet: all weights 0)
-                    float p[NK * 4];
-#pragma unroll
-                    for (int i = 0; i < NK * 4; ++i) {
-                        p[i] = fast_exp2(x[i] - ref);
-                        l_run += p[i];
-                    }
-                    if (more) arrived<2 * XFERS>();
-                    else arrived<0>();
-                    // fragments of V: 16 columns x the keys of this lane's weights
-                    const int vkey = 4 * quarter + (l16 >> 2);
-                    const auto v_frag = [&](int c) __attribute__((always_inline)) {
-                        if constexpr (F32) {
-                            const int turn = UB % 4 == 0 ? quarter & 3 : UB % 4 == 2 ? quarter & 1 : 0;
-                            u32x4 v;
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const uint32_t*>(vt + (4 * quarter + r) * DB + (c ^ turn) * 64 + l16 * 4);
-                            return v;
-                        } else {
-                            const char* const v = vt + vkey * DB + (lane & 3) * 8 + (c ^ L::v16_block(vkey)) * 32;
-                            return u32x4_of(lds_read_tr16(v), lds_read_tr16(v + 16 * DB));
-                        }
-                    };
-                    const auto multiply = [&](f32x4& acc, const u32x4& v, const u32x4& w) __attribute__((always_inline)) {
-                        if constexpr (F32) {
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r]), __uint_as_float(w[r]), acc, 0, 0, 0);
-                        } else {
-                            mma16(acc, v, w);
-                        }
-                    };
-                    const auto operand = [&](const float (&y)[NK * 4]) __attribute__((always_inline)) {
-                        if constexpr (F32) return u32x4{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
-                        else return u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
-                    };
-                    const u32x4 pw = operand(p);
-                    if (!whole) {
-                        // A value that is no number must not reach the rows that do not see it, by way of a weight of 0: such values
-                        // count as 0, and make the columns of the rows that do see them NaN.
-                        uint32_t bad = 0;
-#pragma unroll
-                        for (int c = 0; c < CB; ++c) bad |= any_lost<T>(v_frag(c));
-                        if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
-                            float saw[NK * 4];
-#pragma unroll
-                            for (int i = 0; i < NK * 4; ++i) saw[i] = x[i] == -__builtin_inff() ? 0.0f : 1.0f;
-                            const u32x4 sw = operand(saw);
-#pragma unroll
-                            for (int c = 0; c < CB; ++c) {
-                                const u32x4 v = v_frag(c), lost = lost_as_one<T>(v);
-                                f32x4 hits = {0.0f, 0.0f, 0.0f, 0.0f};
-                                multiply(hits, lost, sw);
-                                multiply(oacc[c], without_lost<T>(v), pw);
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (hits[r] > 0.0f) oacc[c][r] = __builtin_nanf("");
-                            }
-                            return;
-                        }
-                    }
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) multiply(oacc[c], v_frag(c), pw);
-                };
-                int key = k0 + wave * KT, s = 0;
-                if (key < k1) issue(key, 0);
-                for (; key < k1; key += C::UNIT, s ^= 1) {
-                    const bool more = key + C::UNIT < k1;
-                    if (more) issue(key + C::UNIT, s ^ 1);
-                    compute(key, s, more);
-                    wait_lds();                   // (the fragments have left the stage that is filled next)
-                }
-                k0 = k1;
-            }
-        };
-#pragma clang loop unroll(disable)
-        for (int part = 0; part < 2; ++part) {    // of the prefix, of what is near
-            const int f = part == 0 ? u0 : max(u0, span.head), t = part == 0 ? min(u1, span.head) : u1;
-            if (f < t) sweep(span.unit(f) * C::UNIT, min(seen, (span.unit(t - 1) + 1) * C::UNIT));
-        }
-        l_run = quarter_wave_sum(l_run);
-
-        // ---- the waves' results into one -----------------------------------------------------------------------------------------------
-        __syncthreads();
-        if (quarter == 0) {
-            stats[(wave * kRows + l16) * 2] = m_run;
-            stats[(wave * kRows + l16) * 2 + 1] = l_run;
-        }
-        float* const mine = reinterpret_cast<float*>(stage);
-#pragma unroll
-        for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4*>(mine + l16 * PITCH + 16 * c + 4 * quarter) = oacc[c];
-        __syncthreads();
-        const bool complete = v0 == 0 && v1 == plan.units;
-        float* const out = a.partial + (2 * w + (first_segment ? 0 : 1)) * (int64_t)(kRows * (C::COLS + 2));
-        constexpr int QUADS = C::COLS / 4;
-        for (int i = threadIdx.x; i < rows * QUADS; i += 64 * NW) {
-            const int r = i / QUADS, c = (i - r * QUADS) * 4;
-            float top = -__builtin_inff();
-#pragma unroll
-            for (int n = 0; n < NW; ++n) top = fmaxf(top, stats[(n * kRows + r) * 2]);
-            const float ref = top == -__builtin_inff() ? 0.0f : top;
-            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-            float l = 0.0f;
-#pragma unroll
-            for (int n = 0; n < NW; ++n) {
-                const float f = fast_exp2(stats[(n * kRows + r) * 2] - ref);
-                l += f * stats[(n * kRows + r) * 2 + 1];
-                sum += *reinterpret_cast<const f32x4*>(lds + n * 4 * TILE + (r * PITCH + c) * 4) * f;
-            }
-            if (complete) {
-                const int64_t rr = row0 + r;
-                const int tk = (int)(rr / a.group), h = kv_head * a.group + (int)(rr - (int64_t)tk * a.group);
-                const int64_t o = (int64_t)(seq.first + tk) * a.heads + h;
-                store_output<T>(a.O, o, rb, c, sum, l);
-                if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
-            } else {
-                *reinterpret_cast<f32x4*>(out + r * C::COLS + c) = sum;
-                if (c == 0) {
-                    out[kRows * C::COLS + 2 * r] = top;
-                    out[kRows * C::COLS + 2 * r + 1] = l;
-                }
-            }
-        }
-    }
+    return p.dt == DType::F32 ? paged_rows_workspace_f32(p) : prefers_paged_tiles(p) ? paged_tiles_workspace(p) : rows_workspace<uint16_t>(p);
 }
-
-template <typename T, int UB> PlanShape plan_of(const PagedArgs& p)
-{
-    using C = RowsCfg<T, UB>;
-    return {kRows, C::UNIT, (int32_t)(p.heads / p.cache.kv_heads), (compute_units() * C::PER_CU + 7) & ~7, 1};
-}
-
-template <typename T, int UB> hipError_t launch(const PagedArgs& p, hipStream_t stream)
-{
-    using C = RowsCfg<T, UB>;
-    const AttendArgs a = attend_args(p, plan_of<T, UB>(p), sizeof(T));
-    if (p.rule.cap > 0.0f || p.rule.slopes)
-        paged_rows_kernel<T, UB, true><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a);
-    else
-        paged_rows_kernel<T, UB, false><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a);
-    const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_join<T>(a, C::COLS, stream);
-}
-
-template <typename T, int UB> int64_t workspace(const PagedArgs& p) { return partial_bytes(plan_of<T, UB>(p), RowsCfg<T, UB>::COLS); }
-
-template <typename T, typename F> auto by_row(int row_bytes, F&& f)
-{
-    const int ub = (row_bytes + 63) / 64;
-    if (ub <= 1) return f(IC<1>{});
-    if (ub <= 2) return f(IC<2>{});
-    if constexpr (sizeof(T) == 2) if (ub <= 3) return f(IC<3>{});
-    if (ub <= 4) return f(IC<4>{});
-    if constexpr (sizeof(T) == 2) if (ub <= 5) return f(IC<5>{});
-    if (ub <= 6) return f(IC<6>{});
-    if constexpr (sizeof(T) == 2) {
-        if (ub <= 7) return f(IC<7>{});
-        return f(IC<8>{});
-    } else {
-        if (ub <= 8) return f(IC<8>{});
-        if (ub <= 12) return f(IC<12>{});
-        return f(IC<16>{});
-    }
-}
-
-}  // namespace
-
-int64_t paged_rows_workspace(const PagedArgs& p)
-{
-    if (p.dt == DType::F32) return by_row<float>(p.cache.row_bytes, [&](auto ub) { return workspace<float, decltype(ub)::value>(p); });
-    return by_row<uint16_t>(p.cache.row_bytes, [&](auto ub) { return workspace<uint16_t, decltype(ub)::value>(p); });
-}
-
-hipError_t launch_paged_rows(const PagedArgs& p, hipStream_t stream)
-{
-    if (p.dt == DType::F32) return by_row<float>(p.cache.row_bytes, [&](auto ub) { return launch<float, decltype(ub)::value>(p, stream); });
-    return by_row<uint16_t>(p.cache.row_bytes, [&](auto ub) { return launch<uint16_t, decltype(ub)::value>(p, stream); });
-}
-
-int64_t paged_workspace(const PagedArgs& p) { return prefers_paged_tiles(p) ? paged_tiles_workspace(p) : paged_rows_workspace(p); }
 
 hipError_t launch_paged_attention(const PagedArgs& p, hipStream_t stream)
 {
-    return prefers_paged_tiles(p) ? launch_paged_tiles(p, stream) : launch_paged_rows(p, stream);
+    return p.dt == DType::F32 ? launch_paged_rows_f32(p, stream) : prefers_paged_tiles(p) ? launch_paged_tiles(p, stream) : launch_rows<uint16_t>(p, stream);
 }
 
 }  // namespace attnw

@@ -1,643 +1,10 @@
-// Attention of new tokens over a paged cache, bf16, blocks of 128 or 256 rows: chunks of prompts.
-//
-//     O = softmax(s) V over the slots that a token sees (paged_rows.hip), one sweep with a running exponent and sum
-//
-// A row is one query head of one token; the heads of a kv head share a block with their tokens, so that a block of 128 rows spans few tokens and few of its
-// tiles are seen in part.  A wave has 32 rows and all keys pass by, tiles of 32 of them, in LDS for all waves of the workgroup, 16 bytes a lane straight from
-// their pages.
-//
-// What bounds it: the matrix unit, beside a vector unit that makes an exponential for every 4 d operations.
-#include "paged_attention.h"
+// Attention over a paged cache by blocks of 128 rows (paged_tiles.h): scores as they are; and when.
+#include "paged_tiles.h"
 
 #include <cstdlib>
 #include <cstring>
 
 namespace attnw {
-namespace {
-
-// Where keys are, 8 bytes for `1 << grain` of them (16 at most, so many that they lie in one page), is kept on chip for so many of these at a time.
-constexpr int kPlaces = 1024;
-
-template <int UB> struct TilesCfg {
-    static constexpr int NX = UB <= 5 ? 2 : 1;    // blocks of 16 rows of a wave
-    static constexpr int NW = UB <= 5 ? 4 : 8;    // waves
-    static constexpr int ROWS = 16 * NX * NW, UNIT = 128;
-    static constexpr int DB = UB * 64, CPR = UB * 4, TILE = 32 * DB, XFERS = TILE / 1024, XW = (XFERS + NW - 1) / NW;
-    static constexpr int COLS = DB / 2, CB = COLS / 16;
-    static constexpr bool PIPE = NX == 2;         // registers for the scores of two tiles
-    static constexpr int RING = 4;                // tiles of K, and of V, on chip
-    static constexpr int LDS = 2 * RING * TILE + kPlaces * 8;
-    static constexpr int PER_CU = NW == 4 && LDS <= 80 * 1024 ? 2 : 1;
-    static_assert(2 * RING * TILE <= kDirectLds, "reach of direct transfers");
-};
-
-// SHORT: by how many bytes a row in memory is shorter than on chip (up to d = 160: 0 or 32; beyond, -1: known at run time).
-template <int UB, int SHORT, bool GENERAL, bool UNIFORM, int THREADS = 64 * TilesCfg<UB>::NW, int BLOCKS = TilesCfg<UB>::NW == 4 ? 2 : 1>
-__global__ __launch_bounds__(THREADS, BLOCKS)
-void paged_tiles_kernel(AttendArgs a, int grain)
-{
-    using C = TilesCfg<UB>;
-    using L = RowLayout<UB>;
-    constexpr int NW = C::NW, DB = C::DB, CPR = C::CPR, TILE = C::TILE, XFERS = C::XFERS, XW = C::XW, CB = C::CB, RING = C::RING, G = UB, NX = C::NX;
-    __shared__ __align__(1024) char lds[C::LDS];
-    char* const k_lds = lds;
-    char* const v_lds = lds + RING * TILE;
-    int64_t* const places = reinterpret_cast<int64_t*>(lds + 2 * RING * TILE);
-    if constexpr (UNIFORM) grain = 4;
-
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
-    const uint32_t k_at = lds_offset_of(k_lds), v_at = lds_offset_of(v_lds);
-    const int rb = SHORT >= 0 ? DB - SHORT : a.cache.row_bytes;
-
-    const Counted count{a};
-    const int64_t total = plan_total(a.cache.batch, lane, count);
-    const int64_t per = places_each(a.plan, total);
-    const int64_t w = xcd_contiguous_block_id(blockIdx.x, gridDim.x);
-    int64_t at = w * per;
-    const int64_t end = at + per < total ? at + per : total;
-    if (at >= end) return;
-    int32_t b;
-    int64_t before;
-    plan_find(a.cache.batch, lane, at, count, b, before);
-
-    if (rb < DB) {                                // (columns that no transfer touches)
-        for (int i = threadIdx.x; i < 2 * RING * TILE / 16; i += 64 * NW) *reinterpret_cast<u32x4*>(lds + i * 16) = u32x4{0u, 0u, 0u, 0u};
-    }
-    // A score as exponent of 2: c times the product (a negative scale negates Q), or by the map.
-    const float c = GENERAL ? 1.0f : fabsf(a.rule.scale) * kLog2e;
-    const uint32_t sign_flip = !GENERAL && a.rule.scale < 0.0f ? Mma<uint16_t>::kSignMask : 0u;
-    const ScoreMap<false, false> plain(a.rule);
-    const ScoreMap<true, false> capped(a.rule);
-
-    // ---- per-lane places of the operand fragments ------------------------------------------------------------------------
-    const char* const krow = k_lds + l16 * DB;
-    constexpr int KPERIOD = UB % 4 == 0 ? 4 : UB % 4 == 2 ? 2 : 1, VPERIOD = L::V16PERIOD;
-    int koff[KPERIOD];
-#pragma unroll
-    for (int g = 0; g < KPERIOD; ++g) koff[g] = ((4 * g + quarter) ^ L::k_chunk(l16)) * 16;
-    // keys 16 (f % 2) .. + 15 x columns 32 (f / 2) .. + 31 (8 a lane)
-    auto k_frag = [&](int buf, int f) __attribute__((always_inline)) {
-        const int g = f / 2;
-        return *reinterpret_cast<const u32x4*>(krow + buf * TILE + (f % 2) * 16 * DB + (g / KPERIOD) * KPERIOD * 64 + koff[g % KPERIOD]);
-    };
-    const int vkey = 4 * quarter + (l16 >> 2);    // a lane's row of the 16 keys that it reads
-    const char* const vrow = v_lds + vkey * DB + (lane & 3) * 8;
-    int voff[VPERIOD];
-#pragma unroll
-    for (int x = 0; x < VPERIOD; ++x) voff[x] = (x ^ L::v16_block(vkey)) * 32;
-    // 16 columns x 32 keys: of a lane keys 4 quarter .. + 3 and 16 more than these, as its weights
-    auto v_frag = [&](int buf, int x) __attribute__((always_inline)) {
-        const char* p = vrow + buf * TILE + (x / VPERIOD) * VPERIOD * 32 + voff[x % VPERIOD];
-        return u32x4_of(lds_read_tr16(p), lds_read_tr16(p + 16 * DB));
-    };
-
-    bool first_segment = true;
-    for (; at < end && b < a.cache.batch; first_segment = false) {
-        const Sequence seq = sequence_at(a.cache, a.starts, a.tokens, b);
-        const int32_t prefix = a.rule.prefix ? max(0, min(a.rule.prefix[b], seq.length)) : 0;
-        const SequencePlan plan = sequence_plan(a.plan, seq, prefix, a.rule.window);
-        const int64_t in_head = (int64_t)plan.blocks * plan.units, here = at - before;
-        if (here >= in_head * a.cache.kv_heads) {
-            before += in_head * a.cache.kv_heads;
-            ++b;
-            continue;
-        }
-        const int kv_head = (int)(here / in_head);
-        const int64_t rest = here - kv_head * in_head;
-        const int block = (int)(rest / plan.units);
-        const int v0 = (int)(rest - (int64_t)block * plan.units);
-        const int v1 = (int)min((int64_t)plan.units, v0 + (end - at));
-        at += v1 - v0;
-
-        // ---- the rows of the block ------------------------------------------------------------------------------------------------
-        const int64_t row0 = (int64_t)block * C::ROWS;
-        const int rows = (int)min((int64_t)C::ROWS, (int64_t)seq.tokens * a.group - row0);
-        const int base = seq.length - seq.tokens;              // slot of the first new token
-        const int first = base + (int)(row0 / a.group), last = base + (int)((row0 + rows - 1) / a.group);
-        const bool active = wave * 16 * NX < rows;
-        int query[NX];
-        float slope[NX];
-        u32x4 qf[NX][G];
-#pragma unroll
-        for (int x = 0; x < NX; ++x) {
-            const int64_t row = row0 + min(wave * 16 * NX + 16 * x + l16, rows - 1);
-            const int token = (int)(row / a.group), head = kv_head * a.group + (int)(row - (int64_t)token * a.group);
-            query[x] = base + token;
-            slope[x] = GENERAL && a.rule.slopes ? a.rule.slopes[head] * kLog2e : 0.0f;
-            const char* q = a.Q + (int64_t)(seq.first + token) * a.q_stride + (int64_t)head * rb;
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const int ch = 4 * g + quarter;
-                qf[x][g] = ch * 16 < rb ? *reinterpret_cast<const u32x4*>(q + ch * 16) ^ sign_flip : u32x4{0u, 0u, 0u, 0u};
-            }
-        }
-        f32x4 oacc[CB][NX];                        // columns 16 i + 4 quarter .. + 3 of rows l16, 16 + l16
-#pragma unroll
-        for (int i = 0; i < CB; ++i)
-#pragma unroll
-            for (int x = 0; x < NX; ++x) oacc[i][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        // the exponent that weights are taken against, the sum of a lane's weights.  (Finite before any score: masked ones are -infinity.)
-        float m_run[NX], l_run[NX];
-#pragma unroll
-        for (int x = 0; x < NX; ++x) m_run[x] = kNegBig, l_run[x] = 0.0f;
-
-        const Span span = visible_span(C::UNIT, first, last, seq.length, prefix, a.rule.window);
-        const int units = last < 0 && span.head == 0 ? 0 : span.count();
-        const int u0 = (int)((int64_t)v0 * units / plan.units), u1 = (int)((int64_t)v1 * units / plan.units);
-        const int seen = min(seq.length, max(prefix, last + 1));
-        const int32_t* const pages_of = a.cache.table + (int64_t)b * a.cache.max_pages;
-
-        // a tile out of buffer `buf`, one step after the other
-        auto tile_alone = [&](int buf, int key0, int past) __attribute__((always_inline)) {
-            float y[NX][8];
-            {
-                f32x4 s[2][NX];                   // keys 16 k + 4 quarter .. + 3, rows 16 x + l16
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int x = 0; x < NX; ++x) s[k][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int f = 0; f < 2 * G; ++f) {
-                    const u32x4 kf = k_frag(buf, f);
-#pragma unroll
-                    for (int x = 0; x < NX; ++x) mma16(s[f % 2][x], kf, qf[x][f / 2]);
-                }
-#pragma unroll
-                for (int x = 0; x < NX; ++x)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[x][i] = s[i / 4][x][i % 4];
-            }
-            const int key = key0 + 4 * quarter;
-#pragma unroll
-            for (int x = 0; x < NX; ++x)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if constexpr (GENERAL) {
-                        y[x][i] = a.rule.cap > 0.0f ? capped(y[x][i]) : plain(y[x][i]);
-                        y[x][i] -= slope[x] * (float)abs(query[x] - (key + 16 * (i / 4) + i % 4));
-                    } else {
-                        y[x][i] *= c;
-                    }
-                }
-            const bool whole = key0 + 32 <= past && ((key0 + 31 <= first && key0 > last - a.rule.window) || key0 + 32 <= prefix);
-            if (!whole) {
-#pragma unroll
-                for (int x = 0; x < NX; ++x)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int j = key + 16 * (i / 4) + i % 4;
-                        if (j >= past || ((uint32_t)(query[x] - j) >= (uint32_t)a.rule.window && j >= prefix)) y[x][i] = -__builtin_inff();
-                    }
-            }
-            float p[NX][8];
-            u32x4 pw[NX];
-#pragma unroll
-            for (int x = 0; x < NX; ++x) {
-                const float top = fmaxf(max3(max3(y[x][0], y[x][1], y[x][2]), max3(y[x][3], y[x][4], y[x][5]), y[x][6]), y[x][7]);
-                if (__builtin_amdgcn_ballot_w64(top > m_run[x]) != 0) {
-                    const float m = fmaxf(m_run[x], quarter_wave_max(top)), alpha = fast_exp2(m_run[x] - m);
-                    l_run[x] *= alpha;
-#pragma unroll
-                    for (int i = 0; i < CB; ++i) oacc[i][x] *= alpha;
-                    m_run[x] = m;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    p[x][i] = fast_exp2(y[x][i] - m_run[x]);
-                    l_run[x] += p[x][i];
-                }
-                pw[x] = u32x4{pack_bf16x2(p[x][0], p[x][1]), pack_bf16x2(p[x][2], p[x][3]), pack_bf16x2(p[x][4], p[x][5]), pack_bf16x2(p[x][6], p[x][7])};
-            }
-            if (!whole) {
-                // (a value that is no number must not reach the rows that do not see it: paged_rows.hip)
-                uint32_t bad = 0;
-#pragma unroll
-                for (int i = 0; i < CB; ++i) bad |= any_lost<uint16_t>(v_frag(buf, i));
-                if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
-                    u32x4 sw[NX];
-#pragma unroll
-                    for (int x = 0; x < NX; ++x) {
-                        float saw[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) saw[i] = y[x][i] == -__builtin_inff() ? 0.0f : 1.0f;
-                        sw[x] = u32x4{pack_bf16x2(saw[0], saw[1]), pack_bf16x2(saw[2], saw[3]), pack_bf16x2(saw[4], saw[5]), pack_bf16x2(saw[6], saw[7])};
-                    }
-#pragma unroll
-                    for (int i = 0; i < CB; ++i) {
-                        const u32x4 v = v_frag(buf, i), lost = lost_as_one<uint16_t>(v), rest_of = without_lost<uint16_t>(v);
-#pragma unroll
-                        for (int x = 0; x < NX; ++x) {
-                            f32x4 hits = {0.0f, 0.0f, 0.0f, 0.0f};
-                            mma16(hits, lost, sw[x]);
-                            mma16(oacc[i][x], rest_of, pw[x]);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (hits[r] > 0.0f) oacc[i][x][r] = __builtin_nanf("");
-                        }
-                    }
-                    return;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < CB; ++i) {
-                const u32x4 v = v_frag(buf, i);
-#pragma unroll
-                for (int x = 0; x < NX; ++x) mma16(oacc[i][x], v, pw[x]);
-            }
-        };
-
-        // Tiles wa .. wb - 1 (six at least), all rows seeing all of them: in the time of tile t the vector unit makes its weights while the matrix unit makes
-        // the output of tile t - 1 and the scores of tile t + 1 (attention_pipe.hip says why).  One barrier for two tiles.
-        auto run_piped = [&](int wa, int wb, int k0) __attribute__((always_inline)) {
-            if constexpr (C::PIPE) {
-            const int n_tiles = wb - wa;
-            // ---- transfers.  UNIFORM: the keys of one lie in one page, its place a number of the wave -----------------------------------------
-            // (The places of 32 tiles wait in a lane each.  One transfer's keys are among 16 of a tile; where rows are no power of two they are all in one page.)
-            constexpr bool HALVES = 64 % CPR == 0;
-            constexpr int OFFS = UB == 4 ? 1 : XW;             // (the keys of transfers j and j + 1 of d = 128 are 16 apart)
-            int64_t place = 0;
-            int place_base = 0;
-            int lane_off[2][OFFS];
-            if constexpr (UNIFORM) {
-#pragma unroll
-                for (int v = 0; v < 2; ++v)
-#pragma unroll
-                    for (int j = 0; j < OFFS; ++j) {
-                        const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
-                        lane_off[v][j] = (HALVES ? key & 15 : key) * rb + ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
-                    }
-            }
-            auto look_up = [&](int t) __attribute__((always_inline)) {   // for the requests from tile t on, 15 tiles at least
-                if constexpr (UNIFORM) {
-                    place_base = 2 * t;
-                    place = places[((wa * 32 - k0) >> 4) + min(2 * t + lane, 2 * n_tiles - 1)];
-                }
-            };
-            auto transfer = [&](int t, int j, int i) __attribute__((always_inline)) {   // i: which of the four tiles of a pair's requests
-                if (XFERS % NW != 0 && wave + NW * j >= XFERS) return;
-                const bool v = i >= 2;
-                const int ahead = t + (i < 2 ? 4 + i : i - 1), tile = min(ahead, n_tiles - 1);
-                const uint32_t to = uniform((int)((v ? v_at : k_at) + (ahead & (RING - 1)) * TILE + (wave + NW * j) * 1024));
-                const char* const where = v ? a.cache.V : a.cache.K;
-                if constexpr (UNIFORM) {
-                    const int half = HALVES ? ((wave + NW * j) * 64 / CPR) >> 4 : 0, from = 2 * tile + half - place_base;
-                    const int64_t off = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)place, from) |
-                                        (int64_t)__builtin_amdgcn_readlane((int)(place >> 32), from) << 32;
-                    dma16_untracked(where + off, (uint32_t)lane_off[v][j % OFFS], to);
-                } else {
-                    const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
-                    const int ch = ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
-                    const int slot = (wa + tile) * 32 + key - k0;
-                    const char* src = where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + ch;
-                    if (SHORT == 0 || ch < rb) dma16_untracked(src, to);
-                }
-            };
-            auto request = [&](int t, int i) __attribute__((always_inline)) {
-#pragma unroll
-                for (int j = 0; j < XW; ++j) transfer(t, j, i);
-            };
-            auto end_of_pair = [&]() __attribute__((always_inline)) {
-                wait_vmem();
-                __syncthreads();                  // (and the wave's fragments have left the buffers)
-            };
-            __syncthreads();                      // (what the ring held has been read)
-            look_up(0);
-            request(-4, 0);                       // K of tiles 0, 1
-            request(-4, 1);
-            request(-2, 0);                       // 2, 3
-            request(-2, 1);
-            request(-1, 2);                       // V of tile 0
-            end_of_pair();
-            if (!active) {                        // (a wave without rows only moves tiles)
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) request(0, i);
-                for (int t = 1; t < n_tiles - 1; ++t) {
-                    if (t % 16 == 0) look_up(t);
-                    if (t % 2 == 0) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) request(t, i);
-                    } else {
-                        end_of_pair();
-                    }
-                }
-                end_of_pair();
-                return;
-            }
-            struct Scores { f32x4 s[2][2]; };     // keys 16 k + 4 quarter .. + 3, rows 16 x + l16
-            struct Weights { u32x4 w[2]; };
-            constexpr int KF = 2 * G, RV = G == 1 ? 2 : 4;   // fragments of K of a tile; those of V held at a time
-            float p[2][8];                        // the weights of the tile before the one whose scores are s
-            // scores of tile t as they count: by the rule, as exponents
-            auto ruled = [&](Scores& r, int t) __attribute__((always_inline)) {
-                if constexpr (GENERAL) {
-                    const int key = (wa + t) * 32 + 4 * quarter;
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float y = r.s[i / 4][x][i % 4];
-                            y = a.rule.cap > 0.0f ? capped(y) : plain(y);
-                            r.s[i / 4][x][i % 4] = y - slope[x] * (float)abs(query[x] - (key + 16 * (i / 4) + i % 4));
-                        }
-                }
-            };
-            auto scores = [&](int buf, int t) __attribute__((always_inline)) {
-                Scores r;
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) r.s[k][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int f = 0; f < KF; ++f) {
-                    const u32x4 kf = k_frag(buf, f);
-                    const int k = f % 2;
-                    mma16(r.s[k][k], kf, qf[k][f / 2]);
-                    mma16(r.s[k][1 - k], kf, qf[1 - k][f / 2]);
-                }
-                ruled(r, t);
-                return r;
-            };
-            auto output = [&](int buf, const Weights& pw) __attribute__((always_inline)) {
-#pragma unroll
-                for (int i = 0; i < CB; ++i) {
-                    const u32x4 v = v_frag(buf, i);
-                    mma16(oacc[i][i & 1], v, pw.w[i & 1]);
-                    mma16(oacc[i][1 - (i & 1)], v, pw.w[1 - (i & 1)]);
-                }
-            };
-            auto pack = [&]() __attribute__((always_inline)) {
-                Weights pw;
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) pw.w[x][i] = pack_bf16x2(p[x][2 * i], p[x][2 * i + 1]);
-                return pw;
-            };
-            auto largest = [&](const Scores& r, int x) __attribute__((always_inline)) {
-                return fmaxf(max3(max3(max3(r.s[0][x][0], r.s[0][x][1], r.s[0][x][2]), r.s[0][x][3], r.s[1][x][0]), r.s[1][x][1], r.s[1][x][2]), r.s[1][x][3]);
-            };
-            // The exponents move where the largest score of some row is far above (or above at all: ahead > far), and with them the weights p and all before them.
-            constexpr float kLazy = 6.0f;         // binades that the maximum may run ahead of the exponent
-            auto follow = [&](const float (&top)[2], float far, bool weights) __attribute__((always_inline)) {
-                const float ahead[2] = {__builtin_fmaf(top[0], c, -m_run[0]), __builtin_fmaf(top[1], c, -m_run[1])};
-                if (__builtin_amdgcn_ballot_w64(fmaxf(ahead[0], ahead[1]) > far) == 0) return;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (__builtin_amdgcn_ballot_w64(ahead[x] > far) == 0) continue;
-                    const float m = fmaxf(m_run[x], reference_exponent(quarter_wave_max(top[x]), c));
-                    const float alpha = fast_exp2(m_run[x] - m);     // exactly 1 for lanes whose exponent stands
-                    l_run[x] *= alpha;
-#pragma unroll
-                    for (int i = 0; i < CB; ++i) oacc[i][x] *= alpha;
-                    if (weights) {
-#pragma unroll
-                        for (int r = 0; r < 8; ++r) p[x][r] *= alpha;
-                    }
-                    m_run[x] = m;
-                }
-            };
-            Scores s = scores(0, 0), sn = scores(1, 1);
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 4; ++i) request(0, i);
-            {
-                const float top[2] = {fmaxf(largest(s, 0), largest(sn, 0)), fmaxf(largest(s, 1), largest(sn, 1))};
-                follow(top, 0.0f, false);
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    p[x][r] = fast_exp2(__builtin_fmaf(s.s[r / 4][x][r % 4], c, -m_run[x]));
-                    l_run[x] += p[x][r];
-                }
-            }
-            s = sn;
-            u32x4 kf[KF], vf[RV];
-#pragma unroll
-            for (int f = 0; f < KF; ++f) kf[f] = k_frag(2, f);
-
-            // ---- Tile t: its weights, the output of tile t - 1, the scores of tile t + 1 ------------------------------------------------------
-            auto tile = [&](int t, auto bufc) __attribute__((always_inline)) {
-                constexpr int BUF = decltype(bufc)::value;         // t mod 4
-                constexpr int STEPS = 2 * (KF + CB), OPS = 8 + 32 + 16 + (GENERAL ? 0 : 8);
-                Weights pw;
-                float pn[2][8], sum[2], top[2];
-                auto vector_op = [&](auto oc) __attribute__((always_inline)) {
-                    constexpr int I = decltype(oc)::value;
-                    if constexpr (I < 8) {
-                        constexpr int X = I / 4, J = I % 4;
-                        pw.w[X][J] = pack_bf16x2(p[X][2 * J], p[X][2 * J + 1]);
-                    } else if constexpr (I < 40) {
-                        // (f0 f1 e0 f2 e1 .. f15 e14 e15: an exponential does not wait for the product right before it)
-                        constexpr int J = I - 8;
-                        constexpr bool EXP = J == 31 || (J >= 2 && J % 2 == 0);
-                        constexpr int E = J == 31 ? 15 : EXP ? J / 2 - 1 : (J + 1) / 2;
-                        constexpr int X = E / 8, R = E % 8;
-                        if constexpr (EXP) pn[X][R] = fast_exp2(pn[X][R]);
-                        else pn[X][R] = __builtin_fmaf(s.s[R / 4][X][R % 4], c, -m_run[X]);
-                    } else if constexpr (I < 56) {
-                        constexpr int X = (I - 40) % 2, R = (I - 40) / 2;
-                        if constexpr (R == 0) sum[X] = pn[X][0];
-                        else sum[X] += pn[X][R];
-                        if constexpr (R == 7) l_run[X] += sum[X];
-                    } else {
-                        constexpr int X = (I - 56) % 2, J = (I - 56) / 2;
-                        if constexpr (J == 0) top[X] = max3(sn.s[0][X][0], sn.s[0][X][1], sn.s[0][X][2]);
-                        if constexpr (J == 1) top[X] = max3(top[X], sn.s[0][X][3], sn.s[1][X][0]);
-                        if constexpr (J == 2) top[X] = max3(top[X], sn.s[1][X][1], sn.s[1][X][2]);
-                        if constexpr (J == 3) top[X] = fmaxf(top[X], sn.s[1][X][3]);
-                    }
-                };
-                static_for<STEPS>([&](auto ic) __attribute__((always_inline)) {
-                    constexpr int I = decltype(ic)::value, F = I / 2, SECOND = I % 2;
-                    if constexpr (F < KF) {
-                        constexpr int GR = F / 2, KB = F % 2, X = SECOND ? 1 - KB : KB;
-                        if constexpr (GR == 0) sn.s[KB][X] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                        mma16(sn.s[KB][X], kf[F], qf[X][GR]);
-                        if constexpr (SECOND && F >= KF - RV) vf[F - (KF - RV)] = v_frag((BUF + 3) % 4, F - (KF - RV));
-                    } else {
-                        constexpr int B = F - KF, X = SECOND ? 1 - B % 2 : B % 2, NEXT = I - 2 * KF;
-                        mma16(oacc[B][X], vf[B % RV], pw.w[X]);
-                        if constexpr (SECOND && B + RV < CB) vf[B % RV] = v_frag((BUF + 3) % 4, B + RV);
-                        if constexpr (NEXT < KF) kf[NEXT] = k_frag((BUF + 2) % 4, NEXT);      // (in the first of these steps: arrived by the end of the tile)
-                    }
-                    static_for<(I + 1) * OPS / STEPS - I * OPS / STEPS>([&](auto jc) __attribute__((always_inline)) {
-                        vector_op(IC<I * OPS / STEPS + decltype(jc)::value>{});
-                    });
-                    // (transfers between the steps: a wave that issues them in a row waits 50 cycles for each)
-                    if constexpr (BUF % 2 == 0 && I % 2 == 0 && I / 2 < 4 * XW) transfer(t, I / 2 % XW, I / 2 / XW);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-                static_assert(2 * CB >= KF && 8 * XW <= STEPS);
-                if constexpr (GENERAL) {
-                    ruled(sn, t + 1);
-                    top[0] = largest(sn, 0);
-                    top[1] = largest(sn, 1);
-                }
-                s = sn;
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) p[x][r] = pn[x][r];
-                follow(top, kLazy, true);
-                if constexpr (BUF % 2 == 1) end_of_pair();
-            };
-            for (int t = 1;;) {
-                if (t >= n_tiles - 1) break;
-                tile(t++, IC<1>{});
-                if (t >= n_tiles - 1) break;
-                tile(t++, IC<2>{});
-                if (t >= n_tiles - 1) break;
-                tile(t++, IC<3>{});
-                if (t >= n_tiles - 1) break;
-                if (t % 16 == 0) look_up(t);
-                tile(t++, IC<0>{});
-            }
-            end_of_pair();
-            // ---- the last two tiles ---------------------------------------------------------------------------------------------------------
-            output((n_tiles - 2) & 3, pack());
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    p[x][r] = fast_exp2(__builtin_fmaf(s.s[r / 4][x][r % 4], c, -m_run[x]));
-                    l_run[x] += p[x][r];
-                }
-            output((n_tiles - 1) & 3, pack());
-            }
-        };
-
-        // keys from .. to - 1, which begin a place
-        auto sweep = [&](int from, int to, bool near) __attribute__((always_inline)) {
-            const int most = kPlaces << grain;    // (a whole number of places of the plan)
-            for (int k0 = from; k0 < to;) {
-                const int k1 = min(to, k0 + most);
-                __syncthreads();                  // (the places, and the tiles, of what was before have been read)
-                for (int i = threadIdx.x; i < (k1 - k0 + (1 << grain) - 1) >> grain; i += 64 * NW)
-                    places[i] = slot_offset(a.cache, pages_of, kv_head, k0 + (i << grain));
-                wait_vmem();
-                __syncthreads();
-                // a transfer of tile t, by lanes: any pages; slots past the end are read as the last
-                auto transfer = [&](const char* from_where, uint32_t to, int t, int j, bool v) __attribute__((always_inline)) {
-                    if (XFERS % NW != 0 && wave + NW * j >= XFERS) return;
-                    const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
-                    const int ch = ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
-                    const int slot = min(t * 32 + key, k1 - 1) - k0;
-                    const char* src = from_where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + ch;
-                    if (SHORT == 0 || ch < rb) dma16_untracked(src, to + (wave + NW * j) * 1024);
-                };
-                // tiles ta .. tb - 1 one after the other
-                auto run_alone = [&](int ta, int tb) __attribute__((always_inline)) {
-                    auto issue = [&](int i) __attribute__((always_inline)) {
-#pragma unroll
-                        for (int j = 0; j < XW; ++j) {
-                            transfer(a.cache.K, uniform((int)(k_at + (i & (RING - 1)) * TILE)), ta + i, j, false);
-                            transfer(a.cache.V, uniform((int)(v_at + (i & (RING - 1)) * TILE)), ta + i, j, true);
-                        }
-                    };
-                    const int n = tb - ta;
-                    __syncthreads();
-                    issue(0);
-                    if (1 < n) issue(1);
-#pragma clang loop unroll(disable)
-                    for (int i = 0; i < n; ++i) {
-                        if (i % 2 == 0) {
-                            wait_vmem();
-                            __syncthreads();      // two tiles are there, and nobody reads the two before them any more
-                            if (i + 2 < n) issue(i + 2);
-                            if (i + 3 < n) issue(i + 3);
-                        }
-                        if (active) tile_alone(i & (RING - 1), (ta + i) * 32, k1);
-                    }
-                };
-                // Tiles that all rows of the block see whole go through run_piped, those before and behind them, with masks, one by one.
-                int f0 = k0 / 32, f1 = (k1 + 31) / 32, w0 = f1, w1 = f1;
-                if constexpr (C::PIPE) {
-                    if (near) w0 = max(f0, (max(0, last - a.rule.window + 1) + 31) / 32), w1 = min(k1, max(0, first + 1)) / 32;
-                    else w0 = f0, w1 = min(k1, prefix) / 32;
-                    if (w1 - w0 < 6) w0 = w1 = f1;
-                }
-#pragma clang loop unroll(disable)
-                for (int side = 0; side < 2; ++side) {
-                    const int ta = side == 0 ? f0 : w1, tb = side == 0 ? w0 : f1;
-                    if constexpr (C::PIPE) {
-                        if (side == 1 && w0 < w1) run_piped(w0, w1, k0);
-                    }
-                    if (ta < tb) run_alone(ta, tb);
-                }
-                k0 = k1;
-            }
-        };
-#pragma clang loop unroll(disable)
-        for (int part = 0; part < 2; ++part) {    // of the prefix, of what is near
-            const int f = part == 0 ? u0 : max(u0, span.head), t = part == 0 ? min(u1, span.head) : u1;
-            if (f < t) sweep(span.unit(f) * C::UNIT, min(seen, (span.unit(t - 1) + 1) * C::UNIT), part == 1);
-        }
-
-        // ---- normalise, round once, store; or leave sums and exponents to the join --------------------------------------------------------
-        const bool complete = v0 == 0 && v1 == plan.units;
-        float* const out = a.partial + (2 * w + (first_segment ? 0 : 1)) * (int64_t)(C::ROWS * (C::COLS + 2));
-        if (active) {
-#pragma unroll
-            for (int x = 0; x < NX; ++x) {
-                const float l = quarter_wave_sum(l_run[x]);
-                const int r = wave * 16 * NX + 16 * x + l16;
-                if (r >= rows) continue;
-                if (complete) {
-                    const int64_t row = row0 + r;
-                    const int token = (int)(row / a.group), head = kv_head * a.group + (int)(row - (int64_t)token * a.group);
-                    const int64_t o = (int64_t)(seq.first + token) * a.heads + head;
-#pragma unroll
-                    for (int i = 0; i < CB; ++i) store_output<uint16_t>(a.O, o, rb, 16 * i + 4 * quarter, oacc[i][x], l);
-                    if (quarter == 0 && a.lse) a.lse[o] = log_sum(m_run[x], l);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < CB; ++i) *reinterpret_cast<f32x4*>(out + r * C::COLS + 16 * i + 4 * quarter) = oacc[i][x];
-                    if (quarter == 0) {
-                        out[C::ROWS * C::COLS + 2 * r] = m_run[x];
-                        out[C::ROWS * C::COLS + 2 * r + 1] = l;
-                    }
-                }
-            }
-        }
-    }
-}
-
-template <int UB> PlanShape plan_of(const PagedArgs& p)
-{
-    using C = TilesCfg<UB>;
-    return {C::ROWS, C::UNIT, (int32_t)(p.heads / p.cache.kv_heads), (compute_units() * C::PER_CU + 7) & ~7, 1};
-}
-
-template <int UB, int SHORT, bool GENERAL> hipError_t launch(const PagedArgs& p, hipStream_t stream)
-{
-    using C = TilesCfg<UB>;
-    const AttendArgs a = attend_args(p, plan_of<UB>(p), 2);
-    const int page = (int)a.cache.page.d, grain = page % 16 == 0 ? 4 : page % 8 == 0 ? 3 : page % 4 == 0 ? 2 : page % 2 == 0 ? 1 : 0;
-    constexpr bool CAN = C::PIPE && SHORT == 0;
-    if (CAN && page % (64 % C::CPR == 0 ? 16 : 32) == 0) paged_tiles_kernel<UB, SHORT, GENERAL, CAN><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
-    else paged_tiles_kernel<UB, SHORT, GENERAL, false><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
-    const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_join<uint16_t>(a, C::COLS, stream);
-}
-
-template <typename F> auto by_row(int row_bytes, F&& f)
-{
-    switch ((row_bytes + 63) / 64) {
-    case 1: return f(IC<1>{});
-    case 2: return f(IC<2>{});
-    case 3: return f(IC<3>{});
-    case 4: return f(IC<4>{});
-    case 5: return f(IC<5>{});
-    case 6: return f(IC<6>{});
-    default: return f(IC<8>{});
-    }
-}
-
-}  // namespace
 
 bool prefers_paged_tiles(const PagedArgs& p)
 {
@@ -657,16 +24,12 @@ int64_t paged_tiles_workspace(const PagedArgs& p)
 
 hipError_t launch_paged_tiles(const PagedArgs& p, hipStream_t stream)
 {
-    return by_row(p.cache.row_bytes, [&](auto ubc) {
-        constexpr int UB = decltype(ubc)::value;
-        const bool general = p.rule.cap > 0.0f || p.rule.slopes;
-        if constexpr (UB <= 5) {
-            if (p.cache.row_bytes == UB * 64) return general ? launch<UB, 0, true>(p, stream) : launch<UB, 0, false>(p, stream);
-            return general ? launch<UB, 32, true>(p, stream) : launch<UB, 32, false>(p, stream);
-        } else {
-            return general ? launch<UB, -1, true>(p, stream) : launch<UB, -1, false>(p, stream);
-        }
-    });
+    switch (rule_mode(p.rule)) {
+    case kPlain: return launch_tiles<kPlain>(p, stream);
+    case kCap: return launch_paged_tiles_cap(p, stream);
+    case kBias: return launch_paged_tiles_bias(p, stream);
+    default: return launch_paged_tiles_both(p, stream);
+    }
 }
 
 }  // namespace attnw

@@ -1,0 +1,8 @@
+// Attention over a paged cache by blocks of 128 rows (paged_tiles.h): scores with a bias by distance.
+#include "paged_tiles.h"
+
+namespace attnw {
+
+hipError_t launch_paged_tiles_bias(const PagedArgs& p, hipStream_t stream) { return launch_tiles<kBias>(p, stream); }
+
+}  // namespace attnw
