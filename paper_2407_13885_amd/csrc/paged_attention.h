@@ -17,25 +17,136 @@ template <int N> __device__ __forceinline__ void arrived()
 #endif
 }
 
+// (also: how many workgroups the work is dealt to)
 struct AttendArgs {
     const char* Q;
     char* O;
     float *lse, *partial;
+    struct Joint* joints;                         // one for each workgroup
     const int32_t* starts;
     int64_t q_stride;                             // bytes of a token's row of Q
-    int32_t tokens, heads, group;
+    int32_t tokens, heads;
+    FastDiv group;
     CacheView cache;
     RuleView rule;
-    PlanShape plan;
+    int32_t workgroups;
 };
 
-struct Counted {
+// A piece of a block that several workgroups work on ends in a workgroup that did not begin it: what the join, a workgroup for each, has to know.
+struct Joint {
+    int32_t first;                                // the workgroup that the block begins in, -1: nothing to join
+    int32_t later;                                // which of its two places: 1 if it had another block before
+    int32_t rows, kv_head, row0, token0;
+};
+
+// The work of a ragged batch as one list: a block (ROWS rows of one kv head of one sequence) is `units` places of it, one for each UNIT keys that its last rows
+// see.  A workgroup takes as many consecutive places as any other, so that long and short sequences load all of them alike; a block whose
+// places fall to several of them leaves partial results, which a second launch joins.  Every block of a sequence has the same number of places: a
+// block whose rows see fewer keys has them spread over its places.
+struct Segment {                                  // the places of one block that are a workgroup's
+    Sequence seq;
+    int32_t b, prefix, kv_head, row0, rows;       // (row0: the block's first, of the kv head's rows of the sequence)
+    int32_t v0, v1, units;                        // places v0 .. v1 - 1 of its `units`
+    int32_t slot;                                 // where partial results go, -1: the block is all here
+};
+
+// A workgroup's way through its places.  (Sequences: of up to 64 each lane of a wave holds one, read once.)
+template <int ROWS, int UNIT> struct Walk {
     const AttendArgs& a;
-    __device__ __forceinline__ int64_t operator()(int b) const
+    bool held, begun;
+    Sequence own;
+    int32_t own_prefix;
+    Deal deal;
+    int32_t w, b;                                 // workgroup, sequence
+    int64_t at, end, before;                      // places: next, behind the last, of the sequences before b
+
+    struct Plan { int32_t blocks, units; };       // of a kv head
+    __device__ __forceinline__ Plan plan(const Sequence& s, int32_t prefix) const
     {
-        const Sequence s = sequence_at(a.cache, a.starts, a.tokens, b);
-        const SequencePlan p = sequence_plan(a.plan, s, a.rule.prefix ? a.rule.prefix[b] : 0, a.rule.window);
-        return (int64_t)p.blocks * p.units * a.cache.kv_heads;
+        // a block's rows belong to so many tokens at most, which together see a window and so many keys more
+        const int32_t span = min((int32_t)quotient(ROWS - 2 + a.group.d, a.group) + 1, s.tokens);
+        const int32_t near = (int32_t)(((int64_t)a.rule.window + span + UNIT - 2) / UNIT) + 2, first = (prefix + UNIT - 1) / UNIT;
+        return {(int32_t)((uint32_t)(s.tokens * (int32_t)a.group.d + ROWS - 1) / ROWS), max(1, min((s.length + UNIT - 1) / UNIT, first + near))};
+    }
+    __device__ __forceinline__ int32_t prefix_at(int i, const Sequence& s) const { return a.rule.prefix ? max(0, min(a.rule.prefix[i], s.length)) : 0; }
+    __device__ __forceinline__ int64_t places(const Plan& p) const { return (int64_t)p.blocks * p.units * a.cache.kv_heads; }
+    __device__ __forceinline__ Walk(const AttendArgs& args, int lane) : a(args), held(args.cache.batch <= 64), begun(false)
+    {
+        const auto of = [&](int i) __attribute__((always_inline)) {
+            const Sequence s = sequence_at(a.cache, a.starts, a.tokens, i);
+            return places(plan(s, prefix_at(i, s)));
+        };
+        own = Sequence{0, 0, 0};
+        own_prefix = 0;
+        int64_t mine = 0, upto = 0;
+        if (held) {
+            if (lane < a.cache.batch) {
+                own = sequence_at(a.cache, a.starts, a.tokens, lane);
+                own_prefix = prefix_at(lane, own);
+                mine = places(plan(own, own_prefix));
+            }
+            upto = wave_inclusive_sum(mine, lane, a.cache.batch);
+            deal = deal_out(uniform(__shfl(upto, a.cache.batch - 1, 64)), a.workgroups);
+        } else {
+            deal = deal_out(plan_total(a.cache.batch, lane, of), a.workgroups);
+        }
+        w = dealt_workgroup(deal);
+        if (threadIdx.x == 0) a.joints[w].first = -1;          // (unless a block ends here)
+        at = end = 0;
+        if (w >= deal.workgroups) return;
+        at = deal.first(w);
+        end = deal.first(w + 1);
+        if (held) {
+            b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < a.cache.batch && upto > at));
+            before = uniform(__shfl(upto - mine, b, 64));
+        } else {
+            plan_find(a.cache.batch, lane, at, of, b, before);
+        }
+    }
+    // The next segment, if there is one.
+    __device__ __forceinline__ bool next(Segment& g)
+    {
+        for (;; ++b) {
+            if (at >= end || b >= a.cache.batch) return false;
+            g.seq = held ? Sequence{__builtin_amdgcn_readlane(own.length, b), __builtin_amdgcn_readlane(own.tokens, b), __builtin_amdgcn_readlane(own.first, b)}
+                         : sequence_at(a.cache, a.starts, a.tokens, b);
+            g.prefix = held ? __builtin_amdgcn_readlane(own_prefix, b) : prefix_at(b, g.seq);
+            const Plan p = plan(g.seq, g.prefix);
+            const int64_t here = at - before;
+            if (here >= places(p)) {
+                before += places(p);
+                continue;
+            }
+            const int64_t block = divide(here, p.units);       // (kv_head, block) of the sequence's
+            const int kv_head = uniform((int32_t)divide(block, p.blocks)), row0 = uniform((int32_t)(block - (int64_t)kv_head * p.blocks)) * ROWS;
+            g.b = b;
+            g.units = p.units;
+            g.kv_head = kv_head;
+            g.row0 = row0;
+            g.rows = min(ROWS, g.seq.tokens * (int32_t)a.group.d - row0);
+            g.v0 = uniform((int32_t)(here - block * p.units));
+            g.v1 = (int)min((int64_t)g.units, g.v0 + (end - at));
+            g.slot = g.v0 == 0 && g.v1 == g.units ? -1 : 2 * w + (begun ? 1 : 0);
+            if (!begun && g.v0 > 0 && g.v1 == g.units && threadIdx.x == 0) {
+                const int64_t began = at - g.v0;
+                Joint j;
+                j.first = (int32_t)deal.owner(began);
+                j.later = deal.first(j.first) != began ? 1 : 0;
+                j.rows = g.rows;
+                j.kv_head = kv_head;
+                j.row0 = row0;
+                j.token0 = g.seq.first;
+                a.joints[w] = j;
+            }
+            at += g.v1 - g.v0;
+            begun = true;
+            return true;
+        }
+    }
+    // Of n units of keys (which may be fewer than the segment's block has places) the first that are a segment's, or behind its last.
+    __device__ __forceinline__ int32_t share(const Segment& g, int32_t v, int32_t n) const
+    {
+        return n == g.units ? v : uniform((int32_t)divide((int64_t)v * n, g.units));
     }
 };
 
@@ -50,90 +161,92 @@ template <typename T> __device__ __forceinline__ void store_output(char* O, int6
 // log of a sum l of weights 2^(x - top)
 __device__ __forceinline__ float log_sum(float top, float l) { return l == 0.0f ? -__builtin_inff() : (top + fast_log2(l)) * (1.0f / kLog2e); }
 
-// The partial results of blocks that several workgroups worked on.  A workgroup per (block, kv head).
+// The partial results of the blocks that end in a workgroup's stretch and did not begin there.  Two loads one after the other bound it: its threads read the
+// parts' exponents at once, then share the columns and the parts.
 template <typename T>
 __global__ __launch_bounds__(256)
-void paged_join_kernel(AttendArgs a, int32_t cols)
+void paged_join_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
 {
-    const int lane = threadIdx.x & 63;
-    const Counted count{a};
-    const int64_t total = plan_total(a.cache.batch, lane, count);
-    const Deal deal = deal_out(total, a.plan.workgroups, a.plan.least);
-    const auto blocks = [&](int i) __attribute__((always_inline)) {
-        const Sequence s = sequence_at(a.cache, a.starts, a.tokens, i);
-        return (((int64_t)s.tokens * a.group + a.plan.rows - 1) / a.plan.rows) * a.cache.kv_heads;
-    };
-    for (int64_t x = blockIdx.x;; x += gridDim.x) {
-        int32_t b;
-        int64_t before;
-        plan_find(a.cache.batch, lane, x, blocks, b, before);
-            if (b < 0) return;
-        const Sequence seq = sequence_at(a.cache, a.starts, a.tokens, b);
-        const SequencePlan plan = sequence_plan(a.plan, seq, a.rule.prefix ? a.rule.prefix[b] : 0, a.rule.window);
-        const int64_t mine = x - before;
-        const int kv_head = (int)(mine / plan.blocks), block = (int)(mine - (int64_t)kv_head * plan.blocks);
-        int64_t x0 = 0;
-        for (int i = lane; i < b; i += 64) x0 += count(i);
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) x0 += __shfl_xor(x0, off, 64);
-        x0 = uniform(x0) + mine * plan.units;
-        const int64_t w0 = deal.owner(x0), w1 = deal.owner(x0 + plan.units - 1);
-        if (w0 == w1) continue;
-        const int64_t row0 = (int64_t)block * a.plan.rows;
-        const int rows = (int)min((int64_t)a.plan.rows, (int64_t)seq.tokens * a.group - row0);
-        const int64_t slot = (int64_t)a.plan.rows * (cols + 2);
-        const bool later = deal.first(w0) != x0;   // (the first of them began with another block)
-        const auto part = [&](int64_t w) __attribute__((always_inline)) { return a.partial + (2 * w + (w == w0 && later ? 1 : 0)) * slot; };
-        const int quads = cols / 4, rb = a.cache.row_bytes;
-        for (int i = threadIdx.x; i < rows * quads; i += 256) {
-            const int r = i / quads, c = (i - r * quads) * 4;
-            float top = -__builtin_inff();
-            for (int64_t w = w0; w <= w1; ++w) top = fmaxf(top, part(w)[a.plan.rows * cols + 2 * r]);
-            const float ref = top == -__builtin_inff() ? 0.0f : top;
-            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-            float l = 0.0f;
-#pragma unroll 4
-            for (int64_t w = w0; w <= w1; ++w) {
-                const float* p = part(w);
-                const float f = fast_exp2(p[a.plan.rows * cols + 2 * r] - ref);
-                l += f * p[a.plan.rows * cols + 2 * r + 1];
-                sum += *reinterpret_cast<const f32x4*>(p + r * cols + c) * f;
-            }
-            const int64_t rr = row0 + r;
-            const int tk = (int)(rr / a.group), h = kv_head * a.group + (int)(rr - (int64_t)tk * a.group);
-            const int64_t o = (int64_t)(seq.first + tk) * a.heads + h;
-            store_output<T>(a.O, o, rb, c, sum, l);
-            if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
+    __shared__ float tops[256];
+    __shared__ float sums[256][5];
+    const Joint j = a.joints[blockIdx.x];
+    if (j.first < 0) return;
+    const int w = blockIdx.x, parts = w - j.first + 1, tid = threadIdx.x, per_row = 256 / block_rows;
+    const int64_t slot = (int64_t)block_rows * (cols + 2);
+    const float* const p0 = a.partial + (2 * (int64_t)j.first + j.later) * slot;         // the first part; the others are 2 places apart
+    const float* const p1 = a.partial + 2 * (int64_t)j.first * slot;
+    const auto part = [&](int k) __attribute__((always_inline)) { return k == 0 ? p0 : p1 + 2 * (int64_t)k * slot; };
+    {
+        const int r = tid % block_rows;
+        float top = -__builtin_inff();
+        if (r < j.rows)
+#pragma unroll 8
+            for (int k = tid / block_rows; k < parts; k += per_row) top = fmaxf(top, part(k)[block_rows * cols + 2 * r]);
+        tops[tid] = top;
+    }
+    __syncthreads();
+    const int quads = cols / 4, items = j.rows * quads, rb = a.cache.row_bytes;
+    int share = 1;                                // threads that share an item
+    while (share < 16 && share * 2 * items <= 256) share *= 2;
+    const int step = 256 / share, mine = tid / step;
+    for (int i0 = 0; i0 < items; i0 += step) {
+        const int i = i0 + tid % step, r = min(i / quads, j.rows - 1), c = (i - i / quads * quads) * 4;
+        float top = tops[r];
+        for (int k = 1; k < per_row; ++k) top = fmaxf(top, tops[r + k * block_rows]);
+        const float ref = top == -__builtin_inff() ? 0.0f : top;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        float l = 0.0f;
+#pragma unroll 8
+        for (int k = mine; k < parts; k += share) {
+            const float* p = part(k);
+            const float f = fast_exp2(p[block_rows * cols + 2 * r] - ref);
+            l += f * p[block_rows * cols + 2 * r + 1];
+            sum += *reinterpret_cast<const f32x4*>(p + r * cols + c) * f;
         }
+        if (share > 1) {                          // (then one round is enough: no barrier in front)
+            float* const s = sums[tid];
+            s[0] = sum[0], s[1] = sum[1], s[2] = sum[2], s[3] = sum[3], s[4] = l;
+            __syncthreads();
+            if (mine != 0) return;
+            for (int k = 1; k < share; ++k) {
+                const float* const o = sums[tid + k * step];
+                sum += f32x4{o[0], o[1], o[2], o[3]};
+                l += o[4];
+            }
+        }
+        if (i >= items) continue;
+        const uint32_t tk = quotient(j.row0 + r, a.group);
+        const int64_t o = (int64_t)(j.token0 + (int)tk) * a.heads + j.kv_head * (int)a.group.d + (int)(j.row0 + r - tk * a.group.d);
+        store_output<T>(a.O, o, rb, c, sum, l);
+        if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
     }
 }
 
-inline AttendArgs attend_args(const PagedArgs& p, const PlanShape& plan, int64_t size)
+inline AttendArgs attend_args(const PagedArgs& p, int workgroups, int64_t size)
 {
     AttendArgs a;
     a.Q = static_cast<const char*>(p.Q);
     a.O = static_cast<char*>(p.O);
     a.lse = p.lse;
-    a.partial = p.workspace;
+    a.joints = reinterpret_cast<Joint*>(p.workspace);
+    a.partial = p.workspace + workgroups * sizeof(Joint) / 4;
     a.starts = p.starts;
     a.q_stride = p.q_stride * size;
     a.tokens = (int32_t)p.tokens;
     a.heads = (int32_t)p.heads;
-    a.group = plan.group;
+    a.group = fast_div((uint32_t)(p.heads / p.cache.kv_heads));
     a.cache = p.cache;
     a.rule = p.rule;
-    a.plan = plan;
+    a.workgroups = workgroups;
     return a;
 }
 
 // Two places for every workgroup: of the block that its stretch begins in, and of the one that it ends in.
-inline int64_t partial_bytes(const PlanShape& plan, int cols) { return (int64_t)plan.workgroups * 2 * plan.rows * (cols + 2) * 4; }
+inline int64_t partial_bytes(int workgroups, int rows, int cols) { return (int64_t)workgroups * (2 * rows * (cols + 2) * 4 + (int64_t)sizeof(Joint)); }
 
-template <typename T> hipError_t launch_join(const AttendArgs& a, int cols, hipStream_t stream)
+template <typename T> hipError_t launch_join(const AttendArgs& a, int rows, int cols, hipStream_t stream)
 {
-    // (every sequence may have one block that is not full)
-    const int64_t blocks = ((int64_t)a.tokens * a.group / a.plan.rows + a.cache.batch) * a.cache.kv_heads;
-    paged_join_kernel<T><<<(uint32_t)(blocks < 1 << 20 ? blocks : 1 << 20), 256, 0, stream>>>(a, cols);
+    paged_join_kernel<T><<<a.workgroups, 256, 0, stream>>>(a, rows, cols);
     return hipGetLastError();
 }
 

@@ -121,39 +121,27 @@ __device__ __forceinline__ int64_t uniform(int64_t x)
     return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)x) | (int64_t)__builtin_amdgcn_readfirstlane((int32_t)(x >> 32)) << 32;
 }
 
-__device__ __forceinline__ int64_t wave_inclusive_sum(int64_t v, int lane)
+// (of the first n lanes)
+__device__ __forceinline__ int64_t wave_inclusive_sum(int64_t v, int lane, int n = 64)
 {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
+    for (int off = 1; off < n; off <<= 1) {
         const int64_t o = __shfl_up(v, off, 64);
         if (lane >= off) v += o;
     }
     return v;
 }
 
-// The work of a ragged batch as one list: a query block (rows of one kv head of one sequence) is `units` places of it, one for each `unit` keys
-// that its last rows see.  A workgroup takes as many consecutive places as any other (Deal), so that long and short sequences load all of them alike; a block whose
-// places fall to several of them leaves partial results, which a second launch joins.  Every block of a sequence has the same
-// number of places: a block whose rows see fewer keys has them spread over its places.
-struct PlanShape {
-    int32_t rows, unit, group;                    // rows of a block, keys of a place, query heads of a kv head
-    int32_t workgroups, least;                    // to deal to; places worth a workgroup of its own
-};
-struct SequencePlan {
-    int32_t blocks;                               // of one kv head
-    int32_t units;                                // places of a block
-};
-__device__ __forceinline__ SequencePlan sequence_plan(const PlanShape& p, const Sequence& s, int32_t prefix, int32_t window)
+// a / b rounded down, 0 <= a < 2^51, 0 < b < 2^51: by way of a reciprocal of 53 bits, whose error moves the quotient by one at most.  (The compiler's own 64-bit
+// division is 150 instructions, and a kernel for single tokens is no longer than a few of these.)
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
 {
-    SequencePlan r;
-    r.blocks = (int32_t)(((int64_t)s.tokens * p.group + p.rows - 1) / p.rows);
-    const int32_t all = (s.length + p.unit - 1) / p.unit;
-    // a block's rows belong to at most this many tokens, which together see a window and so many keys more
-    const int32_t span = min((p.rows + p.group - 2) / p.group + 1, s.tokens);
-    const int32_t near = (int32_t)(((int64_t)window + span + p.unit - 2) / p.unit) + 2;
-    const int32_t first = (max(0, min(prefix, s.length)) + p.unit - 1) / p.unit;
-    r.units = max(1, min(all, first + near));
-    return r;
+    const double d = (double)b;
+    double r = __builtin_amdgcn_rcp(d);
+    r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
+    r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
+    int64_t q = (int64_t)((double)a * r);
+    const int64_t rest = a - q * b;
+    return rest < 0 ? q - 1 : rest >= b ? q + 1 : q;
 }
 
 // All places of a batch (a wave's lanes count the sequences), `count(b)` being those of sequence b.
@@ -187,29 +175,31 @@ __device__ __forceinline__ void plan_find(int batch, int lane, int64_t at, Count
     before = base;
 }
 
-// The list dealt out: workgroup w has the places first(w) .. first(w + 1) - 1, numbers of `least` but at the end; all of them have some.
+// A list of places dealt out: workgroup w has first(w) .. first(w + 1) - 1, `each` of them or one more; all workgroups have some.
 struct Deal {
-    int64_t total;
-    int32_t workgroups, least;
-    __device__ __forceinline__ int64_t first(int64_t w) const { return w >= workgroups ? total : w * total / ((int64_t)workgroups * least) * least; }
+    int64_t total, each, more;                    // the first `more` have one more
+    int32_t workgroups;
+    __device__ __forceinline__ int64_t first(int64_t w) const { return w * each + (w < more ? w : more); }
     __device__ __forceinline__ int64_t owner(int64_t x) const   // whose place x is
     {
-        const int64_t w = ((x / least + 1) * workgroups * least - 1) / total;
-        return w < workgroups ? w : workgroups - 1;
+        const int64_t those = more * (each + 1);
+        return x < those ? divide(x, each + 1) : more + divide(x - those, each);
     }
 };
-__device__ __forceinline__ Deal deal_out(int64_t total, int32_t workgroups, int32_t least)
+__device__ __forceinline__ Deal deal_out(int64_t total, int32_t most)
 {
-    const int64_t most = total / least;
-    return {total, most < 1 ? 1 : most < workgroups ? (int32_t)most : workgroups, least};
+    Deal d;
+    d.total = total;
+    d.workgroups = total < most ? (int32_t)total : most;
+    d.each = total < most ? 1 : uniform(divide(total, most));
+    d.more = total < most ? 0 : total - d.each * most;
+    return d;
 }
-// Which workgroup a block of the launch is (-1: none): neighbours on one XCD, also where there are fewer than were launched.
+// Which workgroup a block of the launch is (from d.workgroups on: none): neighbours on one XCD, also where there are fewer than were launched.
 __device__ __forceinline__ int32_t dealt_workgroup(const Deal& d)
 {
     const uint32_t padded = (d.workgroups + 7) & ~7u;
-    if (blockIdx.x >= padded) return -1;
-    const int32_t w = (int32_t)xcd_contiguous_block_id(blockIdx.x, padded);
-    return w < d.workgroups ? w : -1;
+    return (int32_t)(blockIdx.x >= padded ? blockIdx.x : xcd_contiguous_block_id(blockIdx.x, padded));
 }
 
 // Keys that the rows at positions first .. last of a sequence see, as places of `unit` keys: [0, head) and [tail, end).

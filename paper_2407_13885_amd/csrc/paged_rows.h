@@ -54,45 +54,19 @@ void paged_rows_kernel(AttendArgs a)
     const uint32_t stage_at = lds_offset_of(stage);
     const int rb = a.cache.row_bytes;
 
-    const Counted count{a};
-    const int64_t total = plan_total(a.cache.batch, lane, count);
-    const Deal deal = deal_out(total, a.plan.workgroups, a.plan.least);
-    const int64_t w = dealt_workgroup(deal);
-    if (w < 0) return;
-    int64_t at = deal.first(w);
-    const int64_t end = deal.first(w + 1);
-    if (at >= end) return;
-    int32_t b;
-    int64_t before;
-    plan_find(a.cache.batch, lane, at, count, b, before);
+    Walk<kRows, C::UNIT> walk(a, lane);
+    if (walk.at >= walk.end) return;
 
     const ScoreMap<(MODE & kCap) != 0, F32> map(a.rule);
-    bool first_segment = true;
-    for (; at < end && b < a.cache.batch; first_segment = false) {
-        const Sequence seq = sequence_at(a.cache, a.starts, a.tokens, b);
-        const int32_t prefix = a.rule.prefix ? max(0, min(a.rule.prefix[b], seq.length)) : 0;
-        const SequencePlan plan = sequence_plan(a.plan, seq, prefix, a.rule.window);
-        const int64_t in_head = (int64_t)plan.blocks * plan.units, here = at - before;
-        if (here >= in_head * a.cache.kv_heads) {
-            before += in_head * a.cache.kv_heads;
-            ++b;
-            continue;
-        }
-        const int kv_head = (int)(here / in_head);
-        const int64_t rest = here - kv_head * in_head;
-        const int block = (int)(rest / plan.units);
-        const int v0 = (int)(rest - (int64_t)block * plan.units);
-        const int v1 = (int)min((int64_t)plan.units, v0 + (end - at));
-        at += v1 - v0;
-
+    Segment seg;
+    while (walk.next(seg)) {
+        const Sequence& seq = seg.seq;
+        const int prefix = seg.prefix, kv_head = seg.kv_head, row0 = seg.row0, rows = seg.rows;
         // ---- the rows of the block ------------------------------------------------------------------------------------------------
-        const int64_t all_rows = (int64_t)seq.tokens * a.group;
-        const int64_t row0 = (int64_t)block * kRows;
-        const int rows = (int)min((int64_t)kRows, all_rows - row0);
-        const int base = seq.length - seq.tokens;              // slot of the first new token
-        const int first = base + (int)(row0 / a.group), last = base + (int)((row0 + rows - 1) / a.group);
-        const int64_t row = row0 + min(l16, rows - 1);
-        const int token = (int)(row / a.group), head = kv_head * a.group + (int)(row - (int64_t)token * a.group);
+        const int group = a.group.d, base = seq.length - seq.tokens;              // slot of the first new token
+        const int first = base + (int)quotient(row0, a.group), last = base + (int)quotient(row0 + rows - 1, a.group);
+        const int row = row0 + min(l16, rows - 1);
+        const int token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
         const int query = base + token;   // sees the slots query - window + 1 .. query
         const float slope = MODE & kBias ? a.rule.slopes[head] * kLog2e : 0.0f;
 
@@ -113,9 +87,9 @@ void paged_rows_kernel(AttendArgs a)
         // ---- the keys of places v0 .. v1 - 1 -----------------------------------------------------------------------------------------
         const Span span = visible_span(C::UNIT, first, last, seq.length, prefix, a.rule.window);
         const int units = last < 0 && span.head == 0 ? 0 : span.count();
-        const int u0 = (int)((int64_t)v0 * units / plan.units), u1 = (int)((int64_t)v1 * units / plan.units);
+        const int u0 = walk.share(seg, seg.v0, units), u1 = walk.share(seg, seg.v1, units);
         const int seen = min(seq.length, max(prefix, last + 1));
-        const int32_t* const pages_of = a.cache.table + (int64_t)b * a.cache.max_pages;
+        const int32_t* const pages_of = a.cache.table + (int64_t)seg.b * a.cache.max_pages;
 
         auto sweep = [&](int from, int to) __attribute__((always_inline)) {   // keys
             const int64_t most = min((int64_t)(kIds - 1) * a.cache.page.d, (int64_t)1 << 30);
@@ -125,8 +99,6 @@ void paged_rows_kernel(AttendArgs a)
                 const int p0 = quotient(k0, a.cache.page), p1 = quotient(k1 - 1, a.cache.page);
                 __syncthreads();
                 for (int p = p0 + threadIdx.x; p <= p1; p += 64 * NW) ids[p - p0] = max(0, min(pages_of[p], a.cache.pages - 1));
-                if (rb < DB)
-                    for (int i = lane; i < 4 * TILE / 16; i += 64) *reinterpret_cast<u32x4*>(stage + i * 16) = u32x4{0u, 0u, 0u, 0u};
                 wait_vmem();
                 __syncthreads();
 
@@ -146,7 +118,8 @@ void paged_rows_kernel(AttendArgs a)
                                          : F32 ? c ^ ((UB % 4 == 0 ? (key >> 2) & 3 : UB % 4 == 2 ? (key >> 2) & 1 : 0) * 4)
                                                : c ^ (L::v16_block(key) * 2);
                             const int64_t o = (int64_t)(uint32_t)__shfl(lo, key, 64) | (int64_t)__shfl(hi, key, 64) << 32;
-                            if (ch * 16 < rb) dma16_untracked((v ? a.cache.V : a.cache.K) + o + ch * 16, stage_at + (2 * s + v) * TILE + j * 1024);
+                            // (behind a row's end on chip: its first chunk, which meets zeros of Q and columns that nobody stores)
+                            dma16_untracked((v ? a.cache.V : a.cache.K) + o + (ch * 16 < rb ? ch * 16 : 0), stage_at + (2 * s + v) * TILE + j * 1024);
                         }
                 };
                 auto compute = [&](int key0, int s, bool more) __attribute__((always_inline)) {
@@ -290,8 +263,8 @@ void paged_rows_kernel(AttendArgs a)
 #pragma unroll
         for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4*>(mine + l16 * PITCH + 16 * c + 4 * quarter) = oacc[c];
         __syncthreads();
-        const bool complete = v0 == 0 && v1 == plan.units;
-        float* const out = a.partial + (2 * w + (first_segment ? 0 : 1)) * (int64_t)(kRows * (C::COLS + 2));
+        const bool complete = seg.slot < 0;
+        float* const out = a.partial + max(seg.slot, 0) * (int64_t)(kRows * (C::COLS + 2));
         constexpr int QUADS = C::COLS / 4;
         for (int i = threadIdx.x; i < rows * QUADS; i += 64 * NW) {
             const int r = i / QUADS, c = (i - r * QUADS) * 4;
@@ -308,8 +281,7 @@ void paged_rows_kernel(AttendArgs a)
                 sum += *reinterpret_cast<const f32x4*>(lds + n * 4 * TILE + (r * PITCH + c) * 4) * f;
             }
             if (complete) {
-                const int64_t rr = row0 + r;
-                const int tk = (int)(rr / a.group), h = kv_head * a.group + (int)(rr - (int64_t)tk * a.group);
+                const int tk = (int)quotient(row0 + r, a.group), h = kv_head * group + row0 + r - tk * group;
                 const int64_t o = (int64_t)(seq.first + tk) * a.heads + h;
                 store_output<T>(a.O, o, rb, c, sum, l);
                 if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
@@ -324,22 +296,18 @@ void paged_rows_kernel(AttendArgs a)
     }
 }
 
-template <typename T, int UB> PlanShape plan_of(const PagedArgs& p)
-{
-    using C = RowsCfg<T, UB>;
-    return {kRows, C::UNIT, (int32_t)(p.heads / p.cache.kv_heads), (compute_units() * C::PER_CU + 7) & ~7, 1};
-}
+template <typename T, int UB> int workgroups() { return (compute_units() * RowsCfg<T, UB>::PER_CU + 7) & ~7; }
 
 template <typename T, int UB, int MODE> hipError_t launch(const PagedArgs& p, hipStream_t stream)
 {
     using C = RowsCfg<T, UB>;
-    const AttendArgs a = attend_args(p, plan_of<T, UB>(p), sizeof(T));
-    paged_rows_kernel<T, UB, MODE><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a);
+    const AttendArgs a = attend_args(p, workgroups<T, UB>(), sizeof(T));
+    paged_rows_kernel<T, UB, MODE><<<a.workgroups, 64 * C::NW, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_join<T>(a, C::COLS, stream);
+    return e != hipSuccess ? e : launch_join<T>(a, kRows, C::COLS, stream);
 }
 
-template <typename T, int UB> int64_t workspace(const PagedArgs& p) { return partial_bytes(plan_of<T, UB>(p), RowsCfg<T, UB>::COLS); }
+template <typename T, int UB> int64_t workspace() { return partial_bytes(workgroups<T, UB>(), kRows, RowsCfg<T, UB>::COLS); }
 
 template <typename T, typename F> auto by_row(int row_bytes, F&& f)
 {
@@ -362,7 +330,7 @@ template <typename T, typename F> auto by_row(int row_bytes, F&& f)
 
 template <typename T> int64_t rows_workspace(const PagedArgs& p)
 {
-    return by_row<T>(p.cache.row_bytes, [&](auto ub) { return workspace<T, decltype(ub)::value>(p); });
+    return by_row<T>(p.cache.row_bytes, [&](auto ub) { return workspace<T, decltype(ub)::value>(); });
 }
 
 template <typename T> hipError_t launch_rows(const PagedArgs& p, hipStream_t stream)

@@ -49,9 +49,9 @@ void paged_sums_kernel(SumsKernelArgs a)
         return (int64_t)((n + KEYS - 1) / KEYS) * a.cache.kv_heads;
     };
     const int64_t total = plan_total(a.cache.batch, lane, count);
-    const Deal deal = deal_out(total, (int32_t)gridDim.x, 1);
+    const Deal deal = deal_out(total, (int32_t)gridDim.x);
     const int64_t w = dealt_workgroup(deal);
-    if (w < 0) return;
+    if (w >= deal.workgroups) return;
     int64_t at = deal.first(w);
     const int64_t end = deal.first(w + 1);
     if (at >= end) return;
@@ -70,7 +70,7 @@ void paged_sums_kernel(SumsKernelArgs a)
             continue;
         }
         ++at;
-        const int kv_head = (int)(here / blocks), key0 = (int)(here - (int64_t)kv_head * blocks) * KEYS;
+        const int kv_head = uniform((int32_t)divide(here, blocks)), key0 = (int)(here - (int64_t)kv_head * blocks) * KEYS;
         const int prefix = a.rule.prefix ? max(0, min(a.rule.prefix[b], seq.length)) : 0;
         const int base = seq.length - seq.tokens;
         const int mine = key0 + (TURNS ? 0 : wave * 16 * NK);  // the first of the wave's keys

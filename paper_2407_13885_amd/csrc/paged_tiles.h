@@ -49,21 +49,9 @@ void paged_tiles_kernel(AttendArgs a, int grain)
     const uint32_t k_at = lds_offset_of(k_lds), v_at = lds_offset_of(v_lds);
     const int rb = SHORT >= 0 ? DB - SHORT : a.cache.row_bytes;
 
-    const Counted count{a};
-    const int64_t total = plan_total(a.cache.batch, lane, count);
-    const Deal deal = deal_out(total, a.plan.workgroups, a.plan.least);
-    const int64_t w = dealt_workgroup(deal);
-    if (w < 0) return;
-    int64_t at = deal.first(w);
-    const int64_t end = deal.first(w + 1);
-    if (at >= end) return;
-    int32_t b;
-    int64_t before;
-    plan_find(a.cache.batch, lane, at, count, b, before);
+    Walk<C::ROWS, C::UNIT> walk(a, lane);
+    if (walk.at >= walk.end) return;
 
-    if (rb < DB) {                                // (columns that no transfer touches)
-        for (int i = threadIdx.x; i < 2 * RING * TILE / 16; i += 64 * NW) *reinterpret_cast<u32x4*>(lds + i * 16) = u32x4{0u, 0u, 0u, 0u};
-    }
     // A score as exponent of 2: c times the product (a negative scale negates Q), or by the map.
     const float c = MODE != kPlain ? 1.0f : fabsf(a.rule.scale) * kLog2e;
     const uint32_t sign_flip = MODE == kPlain && a.rule.scale < 0.0f ? Mma<uint16_t>::kSignMask : 0u;
@@ -91,37 +79,21 @@ void paged_tiles_kernel(AttendArgs a, int grain)
         return u32x4_of(lds_read_tr16(p), lds_read_tr16(p + 16 * DB));
     };
 
-    bool first_segment = true;
-    for (; at < end && b < a.cache.batch; first_segment = false) {
-        const Sequence seq = sequence_at(a.cache, a.starts, a.tokens, b);
-        const int32_t prefix = a.rule.prefix ? max(0, min(a.rule.prefix[b], seq.length)) : 0;
-        const SequencePlan plan = sequence_plan(a.plan, seq, prefix, a.rule.window);
-        const int64_t in_head = (int64_t)plan.blocks * plan.units, here = at - before;
-        if (here >= in_head * a.cache.kv_heads) {
-            before += in_head * a.cache.kv_heads;
-            ++b;
-            continue;
-        }
-        const int kv_head = (int)(here / in_head);
-        const int64_t rest = here - kv_head * in_head;
-        const int block = (int)(rest / plan.units);
-        const int v0 = (int)(rest - (int64_t)block * plan.units);
-        const int v1 = (int)min((int64_t)plan.units, v0 + (end - at));
-        at += v1 - v0;
-
+    Segment seg;
+    while (walk.next(seg)) {
+        const Sequence& seq = seg.seq;
+        const int prefix = seg.prefix, kv_head = seg.kv_head, row0 = seg.row0, rows = seg.rows;
         // ---- the rows of the block ------------------------------------------------------------------------------------------------
-        const int64_t row0 = (int64_t)block * C::ROWS;
-        const int rows = (int)min((int64_t)C::ROWS, (int64_t)seq.tokens * a.group - row0);
-        const int base = seq.length - seq.tokens;              // slot of the first new token
-        const int first = base + (int)(row0 / a.group), last = base + (int)((row0 + rows - 1) / a.group);
+        const int group = a.group.d, base = seq.length - seq.tokens;              // slot of the first new token
+        const int first = base + (int)quotient(row0, a.group), last = base + (int)quotient(row0 + rows - 1, a.group);
         const bool active = wave * 16 * NX < rows;
         int query[NX];
         float slope[NX];
         u32x4 qf[NX][G];
 #pragma unroll
         for (int x = 0; x < NX; ++x) {
-            const int64_t row = row0 + min(wave * 16 * NX + 16 * x + l16, rows - 1);
-            const int token = (int)(row / a.group), head = kv_head * a.group + (int)(row - (int64_t)token * a.group);
+            const int row = row0 + min(wave * 16 * NX + 16 * x + l16, rows - 1);
+            const int token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
             query[x] = base + token;
             slope[x] = MODE & kBias ? a.rule.slopes[head] * kLog2e : 0.0f;
             const char* q = a.Q + (int64_t)(seq.first + token) * a.q_stride + (int64_t)head * rb;
@@ -143,9 +115,9 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 
         const Span span = visible_span(C::UNIT, first, last, seq.length, prefix, a.rule.window);
         const int units = last < 0 && span.head == 0 ? 0 : span.count();
-        const int u0 = (int)((int64_t)v0 * units / plan.units), u1 = (int)((int64_t)v1 * units / plan.units);
+        const int u0 = walk.share(seg, seg.v0, units), u1 = walk.share(seg, seg.v1, units);
         const int seen = min(seq.length, max(prefix, last + 1));
-        const int32_t* const pages_of = a.cache.table + (int64_t)b * a.cache.max_pages;
+        const int32_t* const pages_of = a.cache.table + (int64_t)seg.b * a.cache.max_pages;
 
         // a tile out of buffer `buf`, one step after the other
         auto tile_alone = [&](int buf, int key0, int past) __attribute__((always_inline)) {
@@ -261,7 +233,8 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 #pragma unroll
                     for (int j = 0; j < OFFS; ++j) {
                         const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
-                        lane_off[v][j] = (HALVES ? key & 15 : key) * rb + ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
+                        const int ch = ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
+                        lane_off[v][j] = (HALVES ? key & 15 : key) * rb + (SHORT == 0 || ch < rb ? ch : 0);
                     }
             }
             auto look_up = [&](int t) __attribute__((always_inline)) {   // for the requests from tile t on, 15 tiles at least
@@ -285,8 +258,8 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
                     const int ch = ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
                     const int slot = (wa + tile) * 32 + key - k0;
-                    const char* src = where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + ch;
-                    if (SHORT == 0 || ch < rb) dma16_untracked(src, to);
+                    const char* src = where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 || ch < rb ? ch : 0);   // (behind a row's end: paged_rows.h)
+                    dma16_untracked(src, to);
                 }
             };
             auto request = [&](int t, int i) __attribute__((always_inline)) {
@@ -522,8 +495,8 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
                     const int ch = ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
                     const int slot = min(t * 32 + key, k1 - 1) - k0;
-                    const char* src = from_where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + ch;
-                    if (SHORT == 0 || ch < rb) dma16_untracked(src, to + (wave + NW * j) * 1024);
+                    const char* src = from_where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 || ch < rb ? ch : 0);   // (behind a row's end: paged_rows.h)
+                    dma16_untracked(src, to + (wave + NW * j) * 1024);
                 };
                 // tiles ta .. tb - 1 one after the other
                 auto run_alone = [&](int ta, int tb) __attribute__((always_inline)) {
@@ -574,8 +547,8 @@ void paged_tiles_kernel(AttendArgs a, int grain)
         }
 
         // ---- normalise, round once, store; or leave sums and exponents to the join --------------------------------------------------------
-        const bool complete = v0 == 0 && v1 == plan.units;
-        float* const out = a.partial + (2 * w + (first_segment ? 0 : 1)) * (int64_t)(C::ROWS * (C::COLS + 2));
+        const bool complete = seg.slot < 0;
+        float* const out = a.partial + max(seg.slot, 0) * (int64_t)(C::ROWS * (C::COLS + 2));
         if (active) {
 #pragma unroll
             for (int x = 0; x < NX; ++x) {
@@ -583,8 +556,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 const int r = wave * 16 * NX + 16 * x + l16;
                 if (r >= rows) continue;
                 if (complete) {
-                    const int64_t row = row0 + r;
-                    const int token = (int)(row / a.group), head = kv_head * a.group + (int)(row - (int64_t)token * a.group);
+                    const int row = row0 + r, token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
                     const int64_t o = (int64_t)(seq.first + token) * a.heads + head;
 #pragma unroll
                     for (int i = 0; i < CB; ++i) store_output<uint16_t>(a.O, o, rb, 16 * i + 4 * quarter, oacc[i][x], l);
@@ -602,22 +574,18 @@ void paged_tiles_kernel(AttendArgs a, int grain)
     }
 }
 
-template <int UB> PlanShape plan_of(const PagedArgs& p)
-{
-    using C = TilesCfg<UB>;
-    return {C::ROWS, C::UNIT, (int32_t)(p.heads / p.cache.kv_heads), (compute_units() * C::PER_CU + 7) & ~7, 1};
-}
+template <int UB> int workgroups() { return (compute_units() * TilesCfg<UB>::PER_CU + 7) & ~7; }
 
 template <int UB, int SHORT, int MODE> hipError_t launch(const PagedArgs& p, hipStream_t stream)
 {
     using C = TilesCfg<UB>;
-    const AttendArgs a = attend_args(p, plan_of<UB>(p), 2);
+    const AttendArgs a = attend_args(p, workgroups<UB>(), 2);
     const int page = (int)a.cache.page.d, grain = page % 16 == 0 ? 4 : page % 8 == 0 ? 3 : page % 4 == 0 ? 2 : page % 2 == 0 ? 1 : 0;
-    constexpr bool CAN = C::PIPE && SHORT == 0;
-    if (CAN && page % (64 % C::CPR == 0 ? 16 : 32) == 0) paged_tiles_kernel<UB, SHORT, MODE, CAN><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
-    else paged_tiles_kernel<UB, SHORT, MODE, false><<<a.plan.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
+    constexpr bool CAN = C::PIPE;
+    if (CAN && page % (64 % C::CPR == 0 ? 16 : 32) == 0) paged_tiles_kernel<UB, SHORT, MODE, CAN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
+    else paged_tiles_kernel<UB, SHORT, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_join<uint16_t>(a, C::COLS, stream);
+    return e != hipSuccess ? e : launch_join<uint16_t>(a, C::ROWS, C::COLS, stream);
 }
 
 template <typename F> auto by_row(int row_bytes, F&& f)

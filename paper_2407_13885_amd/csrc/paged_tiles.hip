@@ -19,7 +19,7 @@ bool prefers_paged_tiles(const PagedArgs& p)
 
 int64_t paged_tiles_workspace(const PagedArgs& p)
 {
-    return by_row(p.cache.row_bytes, [&](auto ub) { return partial_bytes(plan_of<decltype(ub)::value>(p), TilesCfg<decltype(ub)::value>::COLS); });
+    return by_row(p.cache.row_bytes, [&](auto ub) { return partial_bytes(workgroups<decltype(ub)::value>(), TilesCfg<decltype(ub)::value>::ROWS, TilesCfg<decltype(ub)::value>::COLS); });
 }
 
 hipError_t launch_paged_tiles(const PagedArgs& p, hipStream_t stream)
