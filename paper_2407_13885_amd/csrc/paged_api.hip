@@ -107,7 +107,7 @@ int check_call_support(const attnw_cache* c, const attnw_rule* r, int64_t tokens
 
 RuleView view(const attnw_rule* r)
 {
-    return {r->scale, r->cap, r->slopes, r->prefix, (int32_t)(r->window == 0 || r->window > kMostSlots ? kMostSlots : r->window)};
+    return {r->scale, r->cap, r->slopes, r->prefix, (int32_t)(r->window == 0 || r->window > attnw::kNoWindow ? attnw::kNoWindow : r->window)};
 }
 
 int status(hipError_t e) { return e == hipSuccess ? ATTNW_OK : ATTNW_ERR_LAUNCH; }
@@ -315,7 +315,7 @@ int attnw_paged_sums(const attnw_cache* cache, const attnw_rule* rule, const voi
     // (no tokens: the sums from before, still)
     if (!sums || !starts || (tokens > 0 && heads > 0 && (!Q || !lse))) return ATTNW_ERR_NULL;
     if ((e = check_call_support(cache, rule, tokens, heads, q_stride)) != ATTNW_OK) return e;
-    if (heads == 0) return ATTNW_ERR_UNSUPPORTED;
+    if (heads == 0 || elems > (int64_t)1 << 38) return ATTNW_ERR_UNSUPPORTED;   // (places of 64 slots: fewer than 2^31)
     if (!aligned(cache->K, 16) || !aligned(cache->table, 4) || !aligned(cache->lengths, 4) || !aligned(Q, 16) || !aligned(lse, 4) || !aligned(before, 4) ||
         !aligned(sums, 4) || !aligned(starts, 4) || !aligned(rule->slopes, 4) || !aligned(rule->prefix, 4))
         return ATTNW_ERR_ALIGN;

@@ -29,7 +29,7 @@ struct AttendArgs {
     FastDiv group;
     CacheView cache;
     RuleView rule;
-    int32_t workgroups;
+    int32_t workgroups, unit_log;
 };
 
 // A piece of a block that several workgroups work on ends in a workgroup that did not begin it: what the join, a workgroup for each, has to know.
@@ -39,7 +39,7 @@ struct Joint {
     int32_t rows, kv_head, row0, token0;
 };
 
-// The work of a ragged batch as one list: a block (ROWS rows of one kv head of one sequence) is `units` places of it, one for each UNIT keys that its last rows
+// The work of a ragged batch as one list: a block (ROWS rows of one kv head of one sequence) is `units` places of it, one for each 2^unit_log keys that its last rows
 // see.  A workgroup takes as many consecutive places as any other, so that long and short sequences load all of them alike; a block whose
 // places fall to several of them leaves partial results, which a second launch joins.  Every block of a sequence has the same number of places: a
 // block whose rows see fewer keys has them spread over its places.
@@ -50,26 +50,33 @@ struct Segment {                                  // the places of one block tha
     int32_t slot;                                 // where partial results go, -1: the block is all here
 };
 
-// A workgroup's way through its places.  (Sequences: of up to 64 each lane of a wave holds one, read once.)
-template <int ROWS, int UNIT> struct Walk {
+// A workgroup's way through its places.  (Sequences: of up to 64 each lane of a wave holds one, read once.  What a kernel for single tokens does before its first
+// load counts: 32 bits throughout, the host makes places of more keys where there would be 2^31.)
+template <int ROWS> struct Walk {
     const AttendArgs& a;
     bool held, begun;
     Sequence own;
     int32_t own_prefix;
     Deal deal;
     int32_t w, b;                                 // workgroup, sequence
-    int64_t at, end, before;                      // places: next, behind the last, of the sequences before b
+    int32_t at, end, before;                      // places: next, behind the last, of the sequences before b
 
     struct Plan { int32_t blocks, units; };       // of a kv head
+    __device__ __forceinline__ int32_t units_of(uint32_t keys) const { return (int32_t)((keys + (1u << a.unit_log) - 1) >> a.unit_log); }
     __device__ __forceinline__ Plan plan(const Sequence& s, int32_t prefix) const
     {
-        // a block's rows belong to so many tokens at most, which together see a window and so many keys more
-        const int32_t span = min((int32_t)quotient(ROWS - 2 + a.group.d, a.group) + 1, s.tokens);
-        const int32_t near = (int32_t)(((int64_t)a.rule.window + span + UNIT - 2) / UNIT) + 2, first = (prefix + UNIT - 1) / UNIT;
-        return {(int32_t)((uint32_t)(s.tokens * (int32_t)a.group.d + ROWS - 1) / ROWS), max(1, min((s.length + UNIT - 1) / UNIT, first + near))};
+        Plan p;
+        p.blocks = (int32_t)((uint32_t)(s.tokens * (int32_t)a.group.d + ROWS - 1) / ROWS);
+        p.units = max(1, units_of(s.length));
+        if (a.rule.window < kNoWindow) {
+            // a block's rows belong to so many tokens at most, which together see a window and so many keys more
+            const uint32_t span = min((int32_t)quotient(ROWS - 2 + a.group.d, a.group) + 1, s.tokens);
+            p.units = min(p.units, units_of(prefix) + units_of(a.rule.window + span) + 2);
+        }
+        return p;
     }
     __device__ __forceinline__ int32_t prefix_at(int i, const Sequence& s) const { return a.rule.prefix ? max(0, min(a.rule.prefix[i], s.length)) : 0; }
-    __device__ __forceinline__ int64_t places(const Plan& p) const { return (int64_t)p.blocks * p.units * a.cache.kv_heads; }
+    __device__ __forceinline__ int32_t places(const Plan& p) const { return p.blocks * p.units * a.cache.kv_heads; }
     __device__ __forceinline__ Walk(const AttendArgs& args, int lane) : a(args), held(args.cache.batch <= 64), begun(false)
     {
         const auto of = [&](int i) __attribute__((always_inline)) {
@@ -78,7 +85,7 @@ template <int ROWS, int UNIT> struct Walk {
         };
         own = Sequence{0, 0, 0};
         own_prefix = 0;
-        int64_t mine = 0, upto = 0;
+        int32_t mine = 0, upto = 0;
         if (held) {
             if (lane < a.cache.batch) {
                 own = sequence_at(a.cache, a.starts, a.tokens, lane);
@@ -86,7 +93,7 @@ template <int ROWS, int UNIT> struct Walk {
                 mine = places(plan(own, own_prefix));
             }
             upto = wave_inclusive_sum(mine, lane, a.cache.batch);
-            deal = deal_out(uniform(__shfl(upto, a.cache.batch - 1, 64)), a.workgroups);
+            deal = deal_out(__builtin_amdgcn_readlane(upto, a.cache.batch - 1), a.workgroups);
         } else {
             deal = deal_out(plan_total(a.cache.batch, lane, of), a.workgroups);
         }
@@ -98,7 +105,7 @@ template <int ROWS, int UNIT> struct Walk {
         end = deal.first(w + 1);
         if (held) {
             b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < a.cache.batch && upto > at));
-            before = uniform(__shfl(upto - mine, b, 64));
+            before = __builtin_amdgcn_readlane(upto - mine, b);
         } else {
             plan_find(a.cache.batch, lane, at, of, b, before);
         }
@@ -112,29 +119,27 @@ template <int ROWS, int UNIT> struct Walk {
                          : sequence_at(a.cache, a.starts, a.tokens, b);
             g.prefix = held ? __builtin_amdgcn_readlane(own_prefix, b) : prefix_at(b, g.seq);
             const Plan p = plan(g.seq, g.prefix);
-            const int64_t here = at - before;
+            const int32_t here = at - before;
             if (here >= places(p)) {
                 before += places(p);
                 continue;
             }
-            const int64_t block = divide(here, p.units);       // (kv_head, block) of the sequence's
-            const int kv_head = uniform((int32_t)divide(block, p.blocks)), row0 = uniform((int32_t)(block - (int64_t)kv_head * p.blocks)) * ROWS;
+            const int32_t block = p.units == 1 ? here : uniform((int32_t)((uint32_t)here / (uint32_t)p.units));
+            g.kv_head = p.blocks == 1 ? block : uniform((int32_t)((uint32_t)block / (uint32_t)p.blocks));
+            g.row0 = (block - g.kv_head * p.blocks) * ROWS;
             g.b = b;
             g.units = p.units;
-            g.kv_head = kv_head;
-            g.row0 = row0;
-            g.rows = min(ROWS, g.seq.tokens * (int32_t)a.group.d - row0);
-            g.v0 = uniform((int32_t)(here - block * p.units));
-            g.v1 = (int)min((int64_t)g.units, g.v0 + (end - at));
+            g.rows = min(ROWS, g.seq.tokens * (int32_t)a.group.d - g.row0);
+            g.v0 = here - block * p.units;
+            g.v1 = min(g.units, g.v0 + (end - at));
             g.slot = g.v0 == 0 && g.v1 == g.units ? -1 : 2 * w + (begun ? 1 : 0);
             if (!begun && g.v0 > 0 && g.v1 == g.units && threadIdx.x == 0) {
-                const int64_t began = at - g.v0;
                 Joint j;
-                j.first = (int32_t)deal.owner(began);
-                j.later = deal.first(j.first) != began ? 1 : 0;
+                j.first = deal.owner(at - g.v0);
+                j.later = deal.first(j.first) != at - g.v0 ? 1 : 0;
                 j.rows = g.rows;
-                j.kv_head = kv_head;
-                j.row0 = row0;
+                j.kv_head = g.kv_head;
+                j.row0 = g.row0;
                 j.token0 = g.seq.first;
                 a.joints[w] = j;
             }
@@ -146,7 +151,7 @@ template <int ROWS, int UNIT> struct Walk {
     // Of n units of keys (which may be fewer than the segment's block has places) the first that are a segment's, or behind its last.
     __device__ __forceinline__ int32_t share(const Segment& g, int32_t v, int32_t n) const
     {
-        return n == g.units ? v : uniform((int32_t)divide((int64_t)v * n, g.units));
+        return n == g.units ? v : uniform((int32_t)((uint64_t)v * n / (uint32_t)g.units));
     }
 };
 
@@ -222,7 +227,7 @@ void paged_join_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
     }
 }
 
-inline AttendArgs attend_args(const PagedArgs& p, int workgroups, int64_t size)
+inline AttendArgs attend_args(const PagedArgs& p, int workgroups, int rows, int unit, int64_t size)
 {
     AttendArgs a;
     a.Q = static_cast<const char*>(p.Q);
@@ -238,6 +243,9 @@ inline AttendArgs attend_args(const PagedArgs& p, int workgroups, int64_t size)
     a.cache = p.cache;
     a.rule = p.rule;
     a.workgroups = workgroups;
+    a.unit_log = 31 - __builtin_clz(unit);
+    const int64_t blocks = (p.tokens * a.group.d / rows + p.cache.batch) * p.cache.kv_heads;
+    while (blocks * ((p.cache.slots >> a.unit_log) + 1) >= (int64_t)1 << 31) ++a.unit_log;
     return a;
 }
 

@@ -62,8 +62,9 @@ struct RuleView {
     float scale, cap;
     const float* slopes;
     const int32_t* prefix;
-    int32_t window;                               // at most 2^30 (no window: 2^30, more than any sequence has)
+    int32_t window;                               // kNoWindow: none
 };
+constexpr int32_t kNoWindow = 1 << 30;            // (as many slots as a sequence can have)
 
 // What a rule has beside the scale: kernels are built for each.
 enum : int { kPlain = 0, kCap = 1, kBias = 2 };
@@ -116,82 +117,61 @@ template <typename T> __device__ __forceinline__ u32x4 without_lost(const u32x4&
 
 // A value that all lanes of a wave have, as one that the compiler knows they have.
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x)
-{
-    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)x) | (int64_t)__builtin_amdgcn_readfirstlane((int32_t)(x >> 32)) << 32;
-}
 
 // (of the first n lanes)
-__device__ __forceinline__ int64_t wave_inclusive_sum(int64_t v, int lane, int n = 64)
+__device__ __forceinline__ int32_t wave_inclusive_sum(int32_t v, int lane, int n = 64)
 {
     for (int off = 1; off < n; off <<= 1) {
-        const int64_t o = __shfl_up(v, off, 64);
+        const int32_t o = __shfl_up(v, off, 64);
         if (lane >= off) v += o;
     }
     return v;
 }
 
-// a / b rounded down, 0 <= a < 2^51, 0 < b < 2^51: by way of a reciprocal of 53 bits, whose error moves the quotient by one at most.  (The compiler's own 64-bit
-// division is 150 instructions, and a kernel for single tokens is no longer than a few of these.)
-__device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
-{
-    const double d = (double)b;
-    double r = __builtin_amdgcn_rcp(d);
-    r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
-    r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
-    int64_t q = (int64_t)((double)a * r);
-    const int64_t rest = a - q * b;
-    return rest < 0 ? q - 1 : rest >= b ? q + 1 : q;
-}
-
 // All places of a batch (a wave's lanes count the sequences), `count(b)` being those of sequence b.
-template <typename Count>
-__device__ __forceinline__ int64_t plan_total(int batch, int lane, Count&& count)
+template <typename Count> __device__ __forceinline__ int32_t plan_total(int batch, int lane, Count&& count)
 {
-    int64_t sum = 0;
+    int32_t sum = 0;
     for (int b = lane; b < batch; b += 64) sum += count(b);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
     return uniform(sum);
 }
-// (the sequence that holds place `at` of the total, and the places before it)
-template <typename Count>
-__device__ __forceinline__ void plan_find(int batch, int lane, int64_t at, Count&& count, int32_t& found, int64_t& before)
+// The sequence that holds place `at` of the total, and the places before it.
+template <typename Count> __device__ __forceinline__ void plan_find(int batch, int lane, int32_t at, Count&& count, int32_t& found, int32_t& before)
 {
-    int64_t base = 0;
+    int32_t base = 0;
     for (int b0 = 0; b0 < batch; b0 += 64) {
-        const int64_t mine = b0 + lane < batch ? count(b0 + lane) : 0;
-        const int64_t end = base + wave_inclusive_sum(mine, lane);
+        const int32_t mine = b0 + lane < batch ? count(b0 + lane) : 0;
+        const int32_t end = base + wave_inclusive_sum(mine, lane);
         const uint64_t past = __builtin_amdgcn_ballot_w64(end > at);
         if (past) {
             const int first = __builtin_ctzll(past);
             found = b0 + first;
-            before = uniform(__shfl(end - mine, first, 64));
+            before = __builtin_amdgcn_readlane(end - mine, first);
             return;
         }
-        base = uniform(__shfl(end, 63, 64));
+        base = __builtin_amdgcn_readlane(end, 63);
     }
-    found = -1;
+    found = batch;
     before = base;
 }
 
 // A list of places dealt out: workgroup w has first(w) .. first(w + 1) - 1, `each` of them or one more; all workgroups have some.
 struct Deal {
-    int64_t total, each, more;                    // the first `more` have one more
-    int32_t workgroups;
-    __device__ __forceinline__ int64_t first(int64_t w) const { return w * each + (w < more ? w : more); }
-    __device__ __forceinline__ int64_t owner(int64_t x) const   // whose place x is
+    int32_t each, more, workgroups;               // the first `more` have one more
+    __device__ __forceinline__ int32_t first(int32_t w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int32_t owner(int32_t x) const   // whose place x is
     {
-        const int64_t those = more * (each + 1);
-        return x < those ? divide(x, each + 1) : more + divide(x - those, each);
+        const int32_t those = more * (each + 1);
+        return x < those ? (int32_t)((uint32_t)x / (uint32_t)(each + 1)) : more + (int32_t)((uint32_t)(x - those) / (uint32_t)each);
     }
 };
-__device__ __forceinline__ Deal deal_out(int64_t total, int32_t most)
+__device__ __forceinline__ Deal deal_out(int32_t total, int32_t most)
 {
     Deal d;
-    d.total = total;
-    d.workgroups = total < most ? (int32_t)total : most;
-    d.each = total < most ? 1 : uniform(divide(total, most));
+    d.workgroups = min(total, most);
+    d.each = total < most ? 1 : uniform((int32_t)((uint32_t)total / (uint32_t)most));
     d.more = total < most ? 0 : total - d.each * most;
     return d;
 }
@@ -202,19 +182,18 @@ __device__ __forceinline__ int32_t dealt_workgroup(const Deal& d)
     return (int32_t)(blockIdx.x >= padded ? blockIdx.x : xcd_contiguous_block_id(blockIdx.x, padded));
 }
 
-// Keys that the rows at positions first .. last of a sequence see, as places of `unit` keys: [0, head) and [tail, end).
+// Keys that the rows at positions first .. last of a sequence see, as units of 2^log keys: [0, head) and [tail, end).
 struct Span {
     int32_t head, tail, end;
     __device__ __forceinline__ int32_t count() const { return head + end - tail; }
     __device__ __forceinline__ int32_t unit(int32_t i) const { return i < head ? i : tail + (i - head); }
 };
-__device__ __forceinline__ Span visible_span(int32_t unit, int32_t first, int32_t last, int32_t length, int32_t prefix, int32_t window)
+__device__ __forceinline__ Span visible_span(int32_t log, int32_t first, int32_t last, int32_t length, int32_t prefix, int32_t window)
 {
     Span s;
-    s.head = (min(prefix, length) + unit - 1) / unit;
-    const int32_t low = max(0, first - window + 1);
-    s.tail = max(s.head, low / unit);
-    s.end = max(s.tail, (last + unit) / unit);    // (last + 1 + unit - 1) / unit; last >= -1 rounded towards zero gives 0 there
+    s.head = (int32_t)((uint32_t)(min(prefix, length) + (1 << log) - 1) >> log);
+    s.tail = max(s.head, max(0, first - window + 1) >> log);
+    s.end = max(s.tail, (int32_t)((uint32_t)(max(0, last + 1) + (1 << log) - 1) >> log));
     return s;
 }
 

@@ -17,7 +17,8 @@ namespace attnw {
 namespace {
 
 constexpr int kRows = 16;                         // of a block
-constexpr int kIds = 1024;                        // page ids kept on chip at a time
+// Where keys are, 8 bytes for `1 << grain` of them (16 at most, so many that they lie in one page), is kept on chip for so many of these at a time.
+constexpr int kPlaces = 1024;
 
 // UB: 64-byte groups of a row on chip.
 template <typename T, int UB> struct RowsCfg {
@@ -30,31 +31,32 @@ template <typename T, int UB> struct RowsCfg {
     static constexpr int UNIT = KT * NW;          // keys of a place
     static constexpr int PITCH = COLS + 4;        // floats of a row of partial results
     static constexpr int STAGES = NW * 4 * TILE;
-    static constexpr int LDS = STAGES + kIds * 4 + NW * kRows * 8;
+    static constexpr int LDS = STAGES + kPlaces * 8 + NW * kRows * 8;
     static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;
     static_assert(4 * TILE >= kRows * PITCH * 4, "partial results of a wave in its stages");
     static_assert(STAGES <= kDirectLds && FIT >= 2);
 };
 
-template <typename T, int UB, int MODE, int THREADS = 64 * RowsCfg<T, UB>::NW>
-__global__ __launch_bounds__(THREADS)
-void paged_rows_kernel(AttendArgs a)
+// EXACT: rows fill their place on chip.
+template <typename T, int UB, int MODE, bool EXACT, int THREADS = 64 * RowsCfg<T, UB>::NW, int WAVES = UB <= (sizeof(T) == 4 ? 8 : 5) ? 2 : 1>
+__global__ __launch_bounds__(THREADS, WAVES)
+void paged_rows_kernel(AttendArgs a, int grain)
 {
     using C = RowsCfg<T, UB>;
     using L = RowLayout<UB>;
     constexpr bool F32 = C::F32;
     constexpr int NW = C::NW, KT = C::KT, DB = C::DB, CPR = C::CPR, TILE = C::TILE, XFERS = C::XFERS, CB = C::CB, NK = KT / 16, PITCH = C::PITCH;
     __shared__ __align__(1024) char lds[C::LDS];
-    int32_t* const ids = reinterpret_cast<int32_t*>(lds + C::STAGES);
-    float* const stats = reinterpret_cast<float*>(lds + C::STAGES + kIds * 4);   // [wave][row]{maximum, sum}
+    int64_t* const places = reinterpret_cast<int64_t*>(lds + C::STAGES);
+    float* const stats = reinterpret_cast<float*>(lds + C::STAGES + kPlaces * 8);   // [wave][row]{maximum, sum}
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
     char* const stage = lds + wave * 4 * TILE;    // K, V of one tile, K, V of the next
     const uint32_t stage_at = lds_offset_of(stage);
-    const int rb = a.cache.row_bytes;
+    const int rb = EXACT ? DB : a.cache.row_bytes;
 
-    Walk<kRows, C::UNIT> walk(a, lane);
+    Walk<kRows> walk(a, lane);
     if (walk.at >= walk.end) return;
 
     const ScoreMap<(MODE & kCap) != 0, F32> map(a.rule);
@@ -76,7 +78,8 @@ void paged_rows_kernel(AttendArgs a)
 #pragma unroll
             for (int g = 0; g < UB; ++g) {
                 const int ch = 4 * g + quarter;
-                qf[g] = ch * 16 < rb ? *reinterpret_cast<const u32x4*>(q + ch * 16) : u32x4{0u, 0u, 0u, 0u};
+                qf[g] = *reinterpret_cast<const u32x4*>(q + (EXACT || ch * 16 < rb ? ch * 16 : 0));
+                if (!EXACT && ch * 16 >= rb) qf[g] = u32x4{0u, 0u, 0u, 0u};
             }
         }
         f32x4 oacc[CB];
@@ -85,30 +88,29 @@ void paged_rows_kernel(AttendArgs a)
         float m_run = -__builtin_inff(), l_run = 0.0f;
 
         // ---- the keys of places v0 .. v1 - 1 -----------------------------------------------------------------------------------------
-        const Span span = visible_span(C::UNIT, first, last, seq.length, prefix, a.rule.window);
+        const Span span = visible_span(a.unit_log, first, last, seq.length, prefix, a.rule.window);
         const int units = last < 0 && span.head == 0 ? 0 : span.count();
         const int u0 = walk.share(seg, seg.v0, units), u1 = walk.share(seg, seg.v1, units);
         const int seen = min(seq.length, max(prefix, last + 1));
         const int32_t* const pages_of = a.cache.table + (int64_t)seg.b * a.cache.max_pages;
 
         auto sweep = [&](int from, int to) __attribute__((always_inline)) {   // keys
-            const int64_t most = min((int64_t)(kIds - 1) * a.cache.page.d, (int64_t)1 << 30);
+            const int most = kPlaces << grain;    // (a whole number of units: the waves' tiles stay where they are)
             for (int k0 = from; k0 < to;) {
-                // (whole places at a time, so that the waves' tiles stay where they are)
-                const int k1 = (int)min((int64_t)to, k0 + max((int64_t)C::UNIT, most / C::UNIT * C::UNIT));
-                const int p0 = quotient(k0, a.cache.page), p1 = quotient(k1 - 1, a.cache.page);
+                const int k1 = min(to, k0 + most);
                 __syncthreads();
-                for (int p = p0 + threadIdx.x; p <= p1; p += 64 * NW) ids[p - p0] = max(0, min(pages_of[p], a.cache.pages - 1));
+                for (int i = threadIdx.x; i < (k1 - k0 + (1 << grain) - 1) >> grain; i += 64 * NW)
+                    places[i] = slot_offset(a.cache, pages_of, kv_head, k0 + (i << grain));
                 wait_vmem();
                 __syncthreads();
 
                 auto issue = [&](int key0, int s) __attribute__((always_inline)) {
-                    // a lane's key of the tile (lanes KT .. again the same ones), past the end the last
-                    const int slot = min(key0 + (lane & (KT - 1)), k1 - 1);
-                    const uint32_t p = quotient(slot, a.cache.page);
-                    const int64_t off = (int64_t)((uint64_t)(uint32_t)ids[p - p0] * a.cache.page_bytes) + (uint32_t)(slot - (int)(p * a.cache.page.d)) * (uint32_t)rb +
-                                        (uint32_t)kv_head * a.cache.head_bytes;
-                    const int lo = (int)(uint32_t)off, hi = (int)(off >> 32);
+                    int64_t row[XFERS];
+#pragma unroll
+                    for (int j = 0; j < XFERS; ++j) {          // (past the end the last slot)
+                        const int slot = min(key0 + (j * 64 + lane) / CPR, k1 - 1) - k0;
+                        row[j] = places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb;
+                    }
 #pragma unroll
                     for (int v = 0; v < 2; ++v)
 #pragma unroll
@@ -117,9 +119,8 @@ void paged_rows_kernel(AttendArgs a)
                             const int ch = v == 0 ? c ^ L::k_chunk(key)
                                          : F32 ? c ^ ((UB % 4 == 0 ? (key >> 2) & 3 : UB % 4 == 2 ? (key >> 2) & 1 : 0) * 4)
                                                : c ^ (L::v16_block(key) * 2);
-                            const int64_t o = (int64_t)(uint32_t)__shfl(lo, key, 64) | (int64_t)__shfl(hi, key, 64) << 32;
                             // (behind a row's end on chip: its first chunk, which meets zeros of Q and columns that nobody stores)
-                            dma16_untracked((v ? a.cache.V : a.cache.K) + o + (ch * 16 < rb ? ch * 16 : 0), stage_at + (2 * s + v) * TILE + j * 1024);
+                            dma16_untracked((v ? a.cache.V : a.cache.K) + row[j] + (EXACT || ch * 16 < rb ? ch * 16 : 0), stage_at + (2 * s + v) * TILE + j * 1024);
                         }
                 };
                 auto compute = [&](int key0, int s, bool more) __attribute__((always_inline)) {
@@ -249,7 +250,7 @@ void paged_rows_kernel(AttendArgs a)
 #pragma clang loop unroll(disable)
         for (int part = 0; part < 2; ++part) {    // of the prefix, of what is near
             const int f = part == 0 ? u0 : max(u0, span.head), t = part == 0 ? min(u1, span.head) : u1;
-            if (f < t) sweep(span.unit(f) * C::UNIT, min(seen, (span.unit(t - 1) + 1) * C::UNIT));
+            if (f < t) sweep(span.unit(f) << a.unit_log, (int)min((int64_t)seen, (int64_t)(span.unit(t - 1) + 1) << a.unit_log));
         }
         l_run = quarter_wave_sum(l_run);
 
@@ -301,8 +302,12 @@ template <typename T, int UB> int workgroups() { return (compute_units() * RowsC
 template <typename T, int UB, int MODE> hipError_t launch(const PagedArgs& p, hipStream_t stream)
 {
     using C = RowsCfg<T, UB>;
-    const AttendArgs a = attend_args(p, workgroups<T, UB>(), sizeof(T));
-    paged_rows_kernel<T, UB, MODE><<<a.workgroups, 64 * C::NW, 0, stream>>>(a);
+    const AttendArgs a = attend_args(p, workgroups<T, UB>(), kRows, C::UNIT, sizeof(T));
+    const int page = (int)a.cache.page.d, grain = page % 16 == 0 ? 4 : page % 8 == 0 ? 3 : page % 4 == 0 ? 2 : page % 2 == 0 ? 1 : 0;
+    // (rows that fill their place: kernels of their own for the usual sizes)
+    constexpr bool OWN = UB == 2 || UB == 4 || UB == 8;
+    if (OWN && a.cache.row_bytes == C::DB) paged_rows_kernel<T, UB, MODE, OWN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
+    else paged_rows_kernel<T, UB, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : launch_join<T>(a, kRows, C::COLS, stream);
 }

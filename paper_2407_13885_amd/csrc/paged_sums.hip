@@ -46,31 +46,29 @@ void paged_sums_kernel(SumsKernelArgs a)
     const int rb = a.cache.row_bytes, group = a.group.d;
     const auto count = [&](int b) __attribute__((always_inline)) {
         const int32_t n = max(0, min(a.cache.lengths[b], a.cache.slots));
-        return (int64_t)((n + KEYS - 1) / KEYS) * a.cache.kv_heads;
+        return ((n + KEYS - 1) / KEYS) * a.cache.kv_heads;
     };
-    const int64_t total = plan_total(a.cache.batch, lane, count);
+    const int32_t total = plan_total(a.cache.batch, lane, count);
     const Deal deal = deal_out(total, (int32_t)gridDim.x);
-    const int64_t w = dealt_workgroup(deal);
+    const int w = dealt_workgroup(deal);
     if (w >= deal.workgroups) return;
-    int64_t at = deal.first(w);
-    const int64_t end = deal.first(w + 1);
-    if (at >= end) return;
-    int32_t b;
-    int64_t before;
+    int32_t at = deal.first(w);
+    const int32_t end = deal.first(w + 1);
+    int32_t b, before;
     plan_find(a.cache.batch, lane, at, count, b, before);
     const ScoreMap<(MODE & kCap) != 0, F32> map(a.rule);
 
     while (at < end && b < a.cache.batch) {
         const Sequence seq = sequence_at(a.cache, a.starts, a.tokens, b);
         const int blocks = (seq.length + KEYS - 1) / KEYS;
-        const int64_t here = at - before;
-        if (here >= (int64_t)blocks * a.cache.kv_heads) {
-            before += (int64_t)blocks * a.cache.kv_heads;
+        const int32_t here = at - before;
+        if (here >= blocks * a.cache.kv_heads) {
+            before += blocks * a.cache.kv_heads;
             ++b;
             continue;
         }
         ++at;
-        const int kv_head = uniform((int32_t)divide(here, blocks)), key0 = (int)(here - (int64_t)kv_head * blocks) * KEYS;
+        const int kv_head = uniform((int32_t)((uint32_t)here / (uint32_t)blocks)), key0 = (here - kv_head * blocks) * KEYS;
         const int prefix = a.rule.prefix ? max(0, min(a.rule.prefix[b], seq.length)) : 0;
         const int base = seq.length - seq.tokens;
         const int mine = key0 + (TURNS ? 0 : wave * 16 * NK);  // the first of the wave's keys

@@ -49,7 +49,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
     const uint32_t k_at = lds_offset_of(k_lds), v_at = lds_offset_of(v_lds);
     const int rb = SHORT >= 0 ? DB - SHORT : a.cache.row_bytes;
 
-    Walk<C::ROWS, C::UNIT> walk(a, lane);
+    Walk<C::ROWS> walk(a, lane);
     if (walk.at >= walk.end) return;
 
     // A score as exponent of 2: c times the product (a negative scale negates Q), or by the map.
@@ -113,7 +113,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 #pragma unroll
         for (int x = 0; x < NX; ++x) m_run[x] = kNegBig, l_run[x] = 0.0f;
 
-        const Span span = visible_span(C::UNIT, first, last, seq.length, prefix, a.rule.window);
+        const Span span = visible_span(a.unit_log, first, last, seq.length, prefix, a.rule.window);
         const int units = last < 0 && span.head == 0 ? 0 : span.count();
         const int u0 = walk.share(seg, seg.v0, units), u1 = walk.share(seg, seg.v1, units);
         const int seen = min(seq.length, max(prefix, last + 1));
@@ -543,7 +543,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 #pragma clang loop unroll(disable)
         for (int part = 0; part < 2; ++part) {    // of the prefix, of what is near
             const int f = part == 0 ? u0 : max(u0, span.head), t = part == 0 ? min(u1, span.head) : u1;
-            if (f < t) sweep(span.unit(f) * C::UNIT, min(seen, (span.unit(t - 1) + 1) * C::UNIT), part == 1);
+            if (f < t) sweep(span.unit(f) << a.unit_log, (int)min((int64_t)seen, (int64_t)(span.unit(t - 1) + 1) << a.unit_log), part == 1);
         }
 
         // ---- normalise, round once, store; or leave sums and exponents to the join --------------------------------------------------------
@@ -579,7 +579,7 @@ template <int UB> int workgroups() { return (compute_units() * TilesCfg<UB>::PER
 template <int UB, int SHORT, int MODE> hipError_t launch(const PagedArgs& p, hipStream_t stream)
 {
     using C = TilesCfg<UB>;
-    const AttendArgs a = attend_args(p, workgroups<UB>(), 2);
+    const AttendArgs a = attend_args(p, workgroups<UB>(), C::ROWS, C::UNIT, 2);
     const int page = (int)a.cache.page.d, grain = page % 16 == 0 ? 4 : page % 8 == 0 ? 3 : page % 4 == 0 ? 2 : page % 2 == 0 ? 1 : 0;
     constexpr bool CAN = C::PIPE;
     if (CAN && page % (64 % C::CPR == 0 ? 16 : 32) == 0) paged_tiles_kernel<UB, SHORT, MODE, CAN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
