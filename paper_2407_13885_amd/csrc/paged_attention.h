@@ -166,47 +166,50 @@ template <typename T> __device__ __forceinline__ void store_output(char* O, int6
 // log of a sum l of weights 2^(x - top)
 __device__ __forceinline__ float log_sum(float top, float l) { return l == 0.0f ? -__builtin_inff() : (top + fast_log2(l)) * (1.0f / kLog2e); }
 
-// The partial results of the blocks that end in a workgroup's stretch and did not begin there.  Two loads one after the other bound it: its threads read the
-// parts' exponents at once, then share the columns and the parts.
-template <typename T>
+// The partial results of the blocks that end in a workgroup's stretch and did not begin there, ROWS rows of a block a workgroup.  Two loads one after the other bound
+// it: its threads read the parts' exponents at once, then share the columns and the parts.
+template <typename T, int ROWS>
 __global__ __launch_bounds__(256)
 void paged_join_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
 {
     __shared__ float tops[256];
     __shared__ float sums[256][5];
     const Joint j = a.joints[blockIdx.x];
-    if (j.first < 0) return;
-    const int w = blockIdx.x, parts = w - j.first + 1, tid = threadIdx.x, per_row = 256 / block_rows;
+    const int first = blockIdx.y * ROWS, rows = min(ROWS, j.rows - first);   // of the block
+    if (j.first < 0 || rows <= 0) return;
+    const int w = blockIdx.x, parts = w - j.first + 1, tid = threadIdx.x;
     const int64_t slot = (int64_t)block_rows * (cols + 2);
     const float* const p0 = a.partial + (2 * (int64_t)j.first + j.later) * slot;         // the first part; the others are 2 places apart
     const float* const p1 = a.partial + 2 * (int64_t)j.first * slot;
     const auto part = [&](int k) __attribute__((always_inline)) { return k == 0 ? p0 : p1 + 2 * (int64_t)k * slot; };
+    const int stats = block_rows * cols + 2 * first;
     {
-        const int r = tid % block_rows;
+        const int r = tid % ROWS;
         float top = -__builtin_inff();
-        if (r < j.rows)
+        if (r < rows)
 #pragma unroll 8
-            for (int k = tid / block_rows; k < parts; k += per_row) top = fmaxf(top, part(k)[block_rows * cols + 2 * r]);
+            for (int k = tid / ROWS; k < parts; k += 256 / ROWS) top = fmaxf(top, part(k)[stats + 2 * r]);
         tops[tid] = top;
     }
     __syncthreads();
-    const int quads = cols / 4, items = j.rows * quads, rb = a.cache.row_bytes;
+    const int quads = cols / 4, items = rows * quads, rb = a.cache.row_bytes;
     int share = 1;                                // threads that share an item
     while (share < 16 && share * 2 * items <= 256) share *= 2;
     const int step = 256 / share, mine = tid / step;
     for (int i0 = 0; i0 < items; i0 += step) {
-        const int i = i0 + tid % step, r = min(i / quads, j.rows - 1), c = (i - i / quads * quads) * 4;
+        const int i = i0 + tid % step, r = min(i / quads, rows - 1), c = (i - i / quads * quads) * 4;
         float top = tops[r];
-        for (int k = 1; k < per_row; ++k) top = fmaxf(top, tops[r + k * block_rows]);
+#pragma unroll
+        for (int k = 1; k < 256 / ROWS; ++k) top = fmaxf(top, tops[r + k * ROWS]);
         const float ref = top == -__builtin_inff() ? 0.0f : top;
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         float l = 0.0f;
 #pragma unroll 8
         for (int k = mine; k < parts; k += share) {
             const float* p = part(k);
-            const float f = fast_exp2(p[block_rows * cols + 2 * r] - ref);
-            l += f * p[block_rows * cols + 2 * r + 1];
-            sum += *reinterpret_cast<const f32x4*>(p + r * cols + c) * f;
+            const float f = fast_exp2(p[stats + 2 * r] - ref);
+            l += f * p[stats + 2 * r + 1];
+            sum += *reinterpret_cast<const f32x4*>(p + (first + r) * cols + c) * f;
         }
         if (share > 1) {                          // (then one round is enough: no barrier in front)
             float* const s = sums[tid];
@@ -220,8 +223,9 @@ void paged_join_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
             }
         }
         if (i >= items) continue;
-        const uint32_t tk = quotient(j.row0 + r, a.group);
-        const int64_t o = (int64_t)(j.token0 + (int)tk) * a.heads + j.kv_head * (int)a.group.d + (int)(j.row0 + r - tk * a.group.d);
+        const int row = j.row0 + first + r;
+        const uint32_t tk = quotient(row, a.group);
+        const int64_t o = (int64_t)(j.token0 + (int)tk) * a.heads + j.kv_head * (int)a.group.d + (int)(row - tk * a.group.d);
         store_output<T>(a.O, o, rb, c, sum, l);
         if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
     }
@@ -254,7 +258,10 @@ inline int64_t partial_bytes(int workgroups, int rows, int cols) { return (int64
 
 template <typename T> hipError_t launch_join(const AttendArgs& a, int rows, int cols, hipStream_t stream)
 {
-    paged_join_kernel<T><<<a.workgroups, 256, 0, stream>>>(a, rows, cols);
+    // few blocks are in many parts each: then more workgroups to a block
+    const int64_t blocks = ((int64_t)a.tokens * a.group.d / rows + a.cache.batch) * a.cache.kv_heads;
+    if (blocks * 8 <= a.workgroups) paged_join_kernel<T, 4><<<dim3(a.workgroups, rows / 4), 256, 0, stream>>>(a, rows, cols);
+    else paged_join_kernel<T, 16><<<dim3(a.workgroups, rows / 16), 256, 0, stream>>>(a, rows, cols);
     return hipGetLastError();
 }
 

@@ -57,6 +57,14 @@ __device__ __forceinline__ int64_t slot_offset(const CacheView& c, const int32_t
     return (int64_t)((uint64_t)(uint32_t)id * c.page_bytes) + (uint32_t)kv_head * c.head_bytes + (uint32_t)(j - (int)(p * c.page.d)) * (uint32_t)c.row_bytes;
 }
 
+// Kernels keep on chip where keys are, 8 bytes for 2^grain of them (16 at most, so many that they lie in one page), for so many of these at a time.
+constexpr int kPlaces = 1024;
+inline int key_grain(const CacheView& c)
+{
+    const uint32_t page = c.page.d;
+    return page % 16 == 0 ? 4 : page % 8 == 0 ? 3 : page % 4 == 0 ? 2 : page % 2 == 0 ? 1 : 0;
+}
+
 // What the scores are made of beside the products.
 struct RuleView {
     float scale, cap;
@@ -227,10 +235,12 @@ hipError_t launch_paged_attention(const PagedArgs& a, hipStream_t stream);
 // Blocks of 16 rows, each wave with keys of its own: any call.
 int64_t paged_rows_workspace_f32(const PagedArgs& a);
 hipError_t launch_paged_rows_f32(const PagedArgs& a, hipStream_t stream);
-// bf16, blocks of 128 or 256 rows, which share the keys: any call, for chunks.
+// Blocks of 128 rows (fp32: 64), which share the keys: any call, for chunks.
 bool prefers_paged_tiles(const PagedArgs& a);
 int64_t paged_tiles_workspace(const PagedArgs& a);
 hipError_t launch_paged_tiles(const PagedArgs& a, hipStream_t stream);
+int64_t paged_tiles_workspace_f32(const PagedArgs& a);
+hipError_t launch_paged_tiles_f32(const PagedArgs& a, hipStream_t stream);
 hipError_t launch_paged_tiles_cap(const PagedArgs& a, hipStream_t stream);
 hipError_t launch_paged_tiles_bias(const PagedArgs& a, hipStream_t stream);
 hipError_t launch_paged_tiles_both(const PagedArgs& a, hipStream_t stream);

@@ -17,8 +17,6 @@ namespace attnw {
 namespace {
 
 constexpr int kRows = 16;                         // of a block
-// Where keys are, 8 bytes for `1 << grain` of them (16 at most, so many that they lie in one page), is kept on chip for so many of these at a time.
-constexpr int kPlaces = 1024;
 
 // UB: 64-byte groups of a row on chip.
 template <typename T, int UB> struct RowsCfg {
@@ -303,7 +301,7 @@ template <typename T, int UB, int MODE> hipError_t launch(const PagedArgs& p, hi
 {
     using C = RowsCfg<T, UB>;
     const AttendArgs a = attend_args(p, workgroups<T, UB>(), kRows, C::UNIT, sizeof(T));
-    const int page = (int)a.cache.page.d, grain = page % 16 == 0 ? 4 : page % 8 == 0 ? 3 : page % 4 == 0 ? 2 : page % 2 == 0 ? 1 : 0;
+    const int grain = key_grain(a.cache);
     // (rows that fill their place: kernels of their own for the usual sizes)
     constexpr bool OWN = UB == 2 || UB == 4 || UB == 8;
     if (OWN && a.cache.row_bytes == C::DB) paged_rows_kernel<T, UB, MODE, OWN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);

@@ -5,12 +5,12 @@ namespace attnw {
 
 int64_t paged_workspace(const PagedArgs& p)
 {
-    return p.dt == DType::F32 ? paged_rows_workspace_f32(p) : prefers_paged_tiles(p) ? paged_tiles_workspace(p) : rows_workspace<uint16_t>(p);
+    return prefers_paged_tiles(p) ? paged_tiles_workspace(p) : p.dt == DType::F32 ? paged_rows_workspace_f32(p) : rows_workspace<uint16_t>(p);
 }
 
 hipError_t launch_paged_attention(const PagedArgs& p, hipStream_t stream)
 {
-    return p.dt == DType::F32 ? launch_paged_rows_f32(p, stream) : prefers_paged_tiles(p) ? launch_paged_tiles(p, stream) : launch_rows<uint16_t>(p, stream);
+    return prefers_paged_tiles(p) ? launch_paged_tiles(p, stream) : p.dt == DType::F32 ? launch_paged_rows_f32(p, stream) : launch_rows<uint16_t>(p, stream);
 }
 
 }  // namespace attnw

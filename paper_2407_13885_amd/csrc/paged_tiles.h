@@ -14,15 +14,14 @@
 namespace attnw {
 namespace {
 
-// Where keys are, 8 bytes for `1 << grain` of them (16 at most, so many that they lie in one page), is kept on chip for so many of these at a time.
-constexpr int kPlaces = 1024;
 
-template <int UB> struct TilesCfg {
-    static constexpr int NX = UB <= 5 ? 2 : 1;    // blocks of 16 rows of a wave
-    static constexpr int NW = UB <= 5 ? 4 : 8;    // waves
-    static constexpr int ROWS = 16 * NX * NW, UNIT = 128;
-    static constexpr int DB = UB * 64, CPR = UB * 4, TILE = 32 * DB, XFERS = TILE / 1024, XW = (XFERS + NW - 1) / NW;
-    static constexpr int COLS = DB / 2, CB = COLS / 16;
+template <typename T, int UB> struct TilesCfg {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int NX = !F32 && UB <= 5 ? 2 : 1;         // blocks of 16 rows of a wave
+    static constexpr int NW = F32 || UB <= 5 ? 4 : 8;          // waves
+    static constexpr int ROWS = 16 * NX * NW, UNIT = F32 ? 64 : 128, KT = F32 ? 16 : 32;   // keys of a tile
+    static constexpr int DB = UB * 64, CPR = UB * 4, TILE = KT * DB, XFERS = TILE / 1024, XW = (XFERS + NW - 1) / NW;
+    static constexpr int COLS = DB / (int)sizeof(T), CB = COLS / 16;
     static constexpr bool PIPE = NX == 2;         // registers for the scores of two tiles
     static constexpr int RING = 4;                // tiles of K, and of V, on chip
     static constexpr int LDS = 2 * RING * TILE + kPlaces * 8;
@@ -31,13 +30,14 @@ template <int UB> struct TilesCfg {
 };
 
 // SHORT: by how many bytes a row in memory is shorter than on chip (up to d = 160: 0 or 32; beyond, -1: known at run time).
-template <int UB, int SHORT, int MODE, bool UNIFORM, int THREADS = 64 * TilesCfg<UB>::NW, int BLOCKS = TilesCfg<UB>::NW == 4 ? 2 : 1>
+template <typename T, int UB, int SHORT, int MODE, bool UNIFORM, int THREADS = 64 * TilesCfg<T, UB>::NW, int BLOCKS = (UB > (TilesCfg<T, UB>::F32 ? 8 : 5)) ? 1 : 2>
 __global__ __launch_bounds__(THREADS, BLOCKS)
 void paged_tiles_kernel(AttendArgs a, int grain)
 {
-    using C = TilesCfg<UB>;
+    using C = TilesCfg<T, UB>;
     using L = RowLayout<UB>;
-    constexpr int NW = C::NW, DB = C::DB, CPR = C::CPR, TILE = C::TILE, XFERS = C::XFERS, XW = C::XW, CB = C::CB, RING = C::RING, G = UB, NX = C::NX;
+    constexpr int NW = C::NW, DB = C::DB, CPR = C::CPR, TILE = C::TILE, XFERS = C::XFERS, XW = C::XW, CB = C::CB, RING = C::RING, G = UB, NX = C::NX, KT = C::KT, NK = KT / 16;
+    constexpr bool F32 = C::F32;
     __shared__ __align__(1024) char lds[C::LDS];
     char* const k_lds = lds;
     char* const v_lds = lds + RING * TILE;
@@ -54,8 +54,8 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 
     // A score as exponent of 2: c times the product (a negative scale negates Q), or by the map.
     const float c = MODE != kPlain ? 1.0f : fabsf(a.rule.scale) * kLog2e;
-    const uint32_t sign_flip = MODE == kPlain && a.rule.scale < 0.0f ? Mma<uint16_t>::kSignMask : 0u;
-    const ScoreMap<(MODE & kCap) != 0, false> map(a.rule);
+    const uint32_t sign_flip = MODE == kPlain && a.rule.scale < 0.0f ? Mma<T>::kSignMask : 0u;
+    const ScoreMap<(MODE & kCap) != 0, F32> map(a.rule);
 
     // ---- per-lane places of the operand fragments ------------------------------------------------------------------------
     const char* const krow = k_lds + l16 * DB;
@@ -63,10 +63,10 @@ void paged_tiles_kernel(AttendArgs a, int grain)
     int koff[KPERIOD];
 #pragma unroll
     for (int g = 0; g < KPERIOD; ++g) koff[g] = ((4 * g + quarter) ^ L::k_chunk(l16)) * 16;
-    // keys 16 (f % 2) .. + 15 x columns 32 (f / 2) .. + 31 (8 a lane)
+    // keys 16 (f % NK) .. + 15 x 64 bytes of their rows (16 a lane)
     auto k_frag = [&](int buf, int f) __attribute__((always_inline)) {
-        const int g = f / 2;
-        return *reinterpret_cast<const u32x4*>(krow + buf * TILE + (f % 2) * 16 * DB + (g / KPERIOD) * KPERIOD * 64 + koff[g % KPERIOD]);
+        const int g = f / NK;
+        return *reinterpret_cast<const u32x4*>(krow + buf * TILE + (f % NK) * 16 * DB + (g / KPERIOD) * KPERIOD * 64 + koff[g % KPERIOD]);
     };
     const int vkey = 4 * quarter + (l16 >> 2);    // a lane's row of the 16 keys that it reads
     const char* const vrow = v_lds + vkey * DB + (lane & 3) * 8;
@@ -74,9 +74,29 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 #pragma unroll
     for (int x = 0; x < VPERIOD; ++x) voff[x] = (x ^ L::v16_block(vkey)) * 32;
     // 16 columns x 32 keys: of a lane keys 4 quarter .. + 3 and 16 more than these, as its weights
+    // (fp32: 16 columns, of a lane its column of keys 4 quarter .. + 3)
     auto v_frag = [&](int buf, int x) __attribute__((always_inline)) {
-        const char* p = vrow + buf * TILE + (x / VPERIOD) * VPERIOD * 32 + voff[x % VPERIOD];
-        return u32x4_of(lds_read_tr16(p), lds_read_tr16(p + 16 * DB));
+        if constexpr (F32) {
+            const int turn = UB % 4 == 0 ? quarter & 3 : UB % 4 == 2 ? quarter & 1 : 0;
+            const char* p = v_lds + buf * TILE + 4 * quarter * DB + (x ^ turn) * 64 + l16 * 4;
+            return u32x4{*reinterpret_cast<const uint32_t*>(p), *reinterpret_cast<const uint32_t*>(p + DB), *reinterpret_cast<const uint32_t*>(p + 2 * DB),
+                         *reinterpret_cast<const uint32_t*>(p + 3 * DB)};
+        } else {
+            const char* p = vrow + buf * TILE + (x / VPERIOD) * VPERIOD * 32 + voff[x % VPERIOD];
+            return u32x4_of(lds_read_tr16(p), lds_read_tr16(p + 16 * DB));
+        }
+    };
+    auto multiply = [&](f32x4& acc, const u32x4& x, const u32x4& y) __attribute__((always_inline)) {
+        if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[i]), __uint_as_float(y[i]), acc, 0, 0, 0);
+        } else {
+            mma16(acc, x, y);
+        }
+    };
+    // where chunk c of key's row lies in its place of V on chip
+    auto v_chunk = [&](int key, int c) __attribute__((always_inline)) {
+        return F32 ? c ^ ((UB % 4 == 0 ? (key >> 2) & 3 : UB % 4 == 2 ? (key >> 2) & 1 : 0) * 4) : c ^ (L::v16_block(key) * 2);
     };
 
     Segment seg;
@@ -119,50 +139,56 @@ void paged_tiles_kernel(AttendArgs a, int grain)
         const int seen = min(seq.length, max(prefix, last + 1));
         const int32_t* const pages_of = a.cache.table + (int64_t)seg.b * a.cache.max_pages;
 
+        // weights as the operand of the second product
+        auto operand = [&](const float (&y)[4 * NK]) __attribute__((always_inline)) {
+            if constexpr (F32) return u32x4{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
+            else return u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
+        };
         // a tile out of buffer `buf`, one step after the other
         auto tile_alone = [&](int buf, int key0, int past) __attribute__((always_inline)) {
-            float y[NX][8];
+            float y[NX][4 * NK];
             {
-                f32x4 s[2][NX];                   // keys 16 k + 4 quarter .. + 3, rows 16 x + l16
+                f32x4 s[NK][NX];                  // keys 16 k + 4 quarter .. + 3, rows 16 x + l16
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < NK; ++k)
 #pragma unroll
                     for (int x = 0; x < NX; ++x) s[k][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int f = 0; f < 2 * G; ++f) {
+                for (int f = 0; f < NK * G; ++f) {
                     const u32x4 kf = k_frag(buf, f);
 #pragma unroll
-                    for (int x = 0; x < NX; ++x) mma16(s[f % 2][x], kf, qf[x][f / 2]);
+                    for (int x = 0; x < NX; ++x) multiply(s[f % NK][x], kf, qf[x][f / NK]);
                 }
 #pragma unroll
                 for (int x = 0; x < NX; ++x)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) y[x][i] = s[i / 4][x][i % 4];
+                    for (int i = 0; i < 4 * NK; ++i) y[x][i] = s[i / 4][x][i % 4];
             }
             const int key = key0 + 4 * quarter;
 #pragma unroll
             for (int x = 0; x < NX; ++x)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 4 * NK; ++i) {
                     if constexpr (MODE != kPlain) y[x][i] = map(y[x][i]);
                     else y[x][i] *= c;
                     if constexpr ((MODE & kBias) != 0) y[x][i] -= slope[x] * (float)abs(query[x] - (key + 16 * (i / 4) + i % 4));
                 }
-            const bool whole = key0 + 32 <= past && ((key0 + 31 <= first && key0 > last - a.rule.window) || key0 + 32 <= prefix);
+            const bool whole = key0 + KT <= past && ((key0 + KT - 1 <= first && key0 > last - a.rule.window) || key0 + KT <= prefix);
             if (!whole) {
 #pragma unroll
                 for (int x = 0; x < NX; ++x)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < 4 * NK; ++i) {
                         const int j = key + 16 * (i / 4) + i % 4;
                         if (j >= past || ((uint32_t)(query[x] - j) >= (uint32_t)a.rule.window && j >= prefix)) y[x][i] = -__builtin_inff();
                     }
             }
-            float p[NX][8];
+            float p[NX][4 * NK];
             u32x4 pw[NX];
 #pragma unroll
             for (int x = 0; x < NX; ++x) {
-                const float top = fmaxf(max3(max3(y[x][0], y[x][1], y[x][2]), max3(y[x][3], y[x][4], y[x][5]), y[x][6]), y[x][7]);
+                float top = max3(y[x][0], y[x][1], fmaxf(y[x][2], y[x][3]));
+                if constexpr (NK == 2) top = max3(top, max3(y[x][4], y[x][5], y[x][6]), y[x][7]);
                 if (__builtin_amdgcn_ballot_w64(top > m_run[x]) != 0) {
                     const float m = fmaxf(m_run[x], quarter_wave_max(top)), alpha = fast_exp2(m_run[x] - m);
                     l_run[x] *= alpha;
@@ -171,34 +197,34 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     m_run[x] = m;
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 4 * NK; ++i) {
                     p[x][i] = fast_exp2(y[x][i] - m_run[x]);
                     l_run[x] += p[x][i];
                 }
-                pw[x] = u32x4{pack_bf16x2(p[x][0], p[x][1]), pack_bf16x2(p[x][2], p[x][3]), pack_bf16x2(p[x][4], p[x][5]), pack_bf16x2(p[x][6], p[x][7])};
+                pw[x] = operand(p[x]);
             }
             if (!whole) {
-                // (a value that is no number must not reach the rows that do not see it: paged_rows.hip)
+                // (a value that is no number must not reach the rows that do not see it: paged_rows.h)
                 uint32_t bad = 0;
 #pragma unroll
-                for (int i = 0; i < CB; ++i) bad |= any_lost<uint16_t>(v_frag(buf, i));
+                for (int i = 0; i < CB; ++i) bad |= any_lost<T>(v_frag(buf, i));
                 if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
                     u32x4 sw[NX];
 #pragma unroll
                     for (int x = 0; x < NX; ++x) {
-                        float saw[8];
+                        float saw[4 * NK];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) saw[i] = y[x][i] == -__builtin_inff() ? 0.0f : 1.0f;
-                        sw[x] = u32x4{pack_bf16x2(saw[0], saw[1]), pack_bf16x2(saw[2], saw[3]), pack_bf16x2(saw[4], saw[5]), pack_bf16x2(saw[6], saw[7])};
+                        for (int i = 0; i < 4 * NK; ++i) saw[i] = y[x][i] == -__builtin_inff() ? 0.0f : 1.0f;
+                        sw[x] = operand(saw);
                     }
 #pragma unroll
                     for (int i = 0; i < CB; ++i) {
-                        const u32x4 v = v_frag(buf, i), lost = lost_as_one<uint16_t>(v), rest_of = without_lost<uint16_t>(v);
+                        const u32x4 v = v_frag(buf, i), lost = lost_as_one<T>(v), rest_of = without_lost<T>(v);
 #pragma unroll
                         for (int x = 0; x < NX; ++x) {
                             f32x4 hits = {0.0f, 0.0f, 0.0f, 0.0f};
-                            mma16(hits, lost, sw[x]);
-                            mma16(oacc[i][x], rest_of, pw[x]);
+                            multiply(hits, lost, sw[x]);
+                            multiply(oacc[i][x], rest_of, pw[x]);
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
                                 if (hits[r] > 0.0f) oacc[i][x][r] = __builtin_nanf("");
@@ -211,7 +237,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
             for (int i = 0; i < CB; ++i) {
                 const u32x4 v = v_frag(buf, i);
 #pragma unroll
-                for (int x = 0; x < NX; ++x) mma16(oacc[i][x], v, pw[x]);
+                for (int x = 0; x < NX; ++x) multiply(oacc[i][x], v, pw[x]);
             }
         };
 
@@ -233,7 +259,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 #pragma unroll
                     for (int j = 0; j < OFFS; ++j) {
                         const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
-                        const int ch = ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
+                        const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
                         lane_off[v][j] = (HALVES ? key & 15 : key) * rb + (SHORT == 0 || ch < rb ? ch : 0);
                     }
             }
@@ -256,7 +282,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     dma16_untracked(where + off, (uint32_t)lane_off[v][j % OFFS], to);
                 } else {
                     const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
-                    const int ch = ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
+                    const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
                     const int slot = (wa + tile) * 32 + key - k0;
                     const char* src = where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 || ch < rb ? ch : 0);   // (behind a row's end: paged_rows.h)
                     dma16_untracked(src, to);
@@ -493,8 +519,8 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 auto transfer = [&](const char* from_where, uint32_t to, int t, int j, bool v) __attribute__((always_inline)) {
                     if (XFERS % NW != 0 && wave + NW * j >= XFERS) return;
                     const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
-                    const int ch = ((x - key * CPR) ^ (v ? L::v16_block(key) * 2 : L::k_chunk(key))) * 16;
-                    const int slot = min(t * 32 + key, k1 - 1) - k0;
+                    const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
+                    const int slot = min(t * KT + key, k1 - 1) - k0;
                     const char* src = from_where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 || ch < rb ? ch : 0);   // (behind a row's end: paged_rows.h)
                     dma16_untracked(src, to + (wave + NW * j) * 1024);
                 };
@@ -519,11 +545,11 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                             if (i + 2 < n) issue(i + 2);
                             if (i + 3 < n) issue(i + 3);
                         }
-                        if (active) tile_alone(i & (RING - 1), (ta + i) * 32, k1);
+                        if (active) tile_alone(i & (RING - 1), (ta + i) * KT, k1);
                     }
                 };
                 // Tiles that all rows of the block see whole go through run_piped, those before and behind them, with masks, one by one.
-                int f0 = k0 / 32, f1 = (k1 + 31) / 32, w0 = f1, w1 = f1;
+                int f0 = k0 / KT, f1 = (k1 + KT - 1) / KT, w0 = f1, w1 = f1;
                 if constexpr (C::PIPE) {
                     if (near) w0 = max(f0, (max(0, last - a.rule.window + 1) + 31) / 32), w1 = min(k1, max(0, first + 1)) / 32;
                     else w0 = f0, w1 = min(k1, prefix) / 32;
@@ -559,7 +585,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     const int row = row0 + r, token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
                     const int64_t o = (int64_t)(seq.first + token) * a.heads + head;
 #pragma unroll
-                    for (int i = 0; i < CB; ++i) store_output<uint16_t>(a.O, o, rb, 16 * i + 4 * quarter, oacc[i][x], l);
+                    for (int i = 0; i < CB; ++i) store_output<T>(a.O, o, rb, 16 * i + 4 * quarter, oacc[i][x], l);
                     if (quarter == 0 && a.lse) a.lse[o] = log_sum(m_run[x], l);
                 } else {
 #pragma unroll
@@ -574,39 +600,52 @@ void paged_tiles_kernel(AttendArgs a, int grain)
     }
 }
 
-template <int UB> int workgroups() { return (compute_units() * TilesCfg<UB>::PER_CU + 7) & ~7; }
+template <typename T, int UB> int workgroups() { return (compute_units() * TilesCfg<T, UB>::PER_CU + 7) & ~7; }
 
-template <int UB, int SHORT, int MODE> hipError_t launch(const PagedArgs& p, hipStream_t stream)
+template <typename T, int UB, int SHORT, int MODE> hipError_t launch(const PagedArgs& p, hipStream_t stream)
 {
-    using C = TilesCfg<UB>;
-    const AttendArgs a = attend_args(p, workgroups<UB>(), C::ROWS, C::UNIT, 2);
-    const int page = (int)a.cache.page.d, grain = page % 16 == 0 ? 4 : page % 8 == 0 ? 3 : page % 4 == 0 ? 2 : page % 2 == 0 ? 1 : 0;
+    using C = TilesCfg<T, UB>;
+    const AttendArgs a = attend_args(p, workgroups<T, UB>(), C::ROWS, C::UNIT, sizeof(T));
+    const int page = (int)a.cache.page.d, grain = key_grain(a.cache);
     constexpr bool CAN = C::PIPE;
-    if (CAN && page % (64 % C::CPR == 0 ? 16 : 32) == 0) paged_tiles_kernel<UB, SHORT, MODE, CAN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
-    else paged_tiles_kernel<UB, SHORT, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
+    if (CAN && page % (64 % C::CPR == 0 ? 16 : 32) == 0) paged_tiles_kernel<T, UB, SHORT, MODE, CAN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
+    else paged_tiles_kernel<T, UB, SHORT, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_join<uint16_t>(a, C::ROWS, C::COLS, stream);
+    return e != hipSuccess ? e : launch_join<T>(a, C::ROWS, C::COLS, stream);
 }
 
-template <typename F> auto by_row(int row_bytes, F&& f)
+template <typename T, typename F> auto by_row(int row_bytes, F&& f)
 {
-    switch ((row_bytes + 63) / 64) {
-    case 1: return f(IC<1>{});
-    case 2: return f(IC<2>{});
-    case 3: return f(IC<3>{});
-    case 4: return f(IC<4>{});
-    case 5: return f(IC<5>{});
-    case 6: return f(IC<6>{});
-    default: return f(IC<8>{});
+    const int ub = (row_bytes + 63) / 64;
+    if (ub <= 1) return f(IC<1>{});
+    if (ub <= 2) return f(IC<2>{});
+    if constexpr (sizeof(T) == 2) if (ub <= 3) return f(IC<3>{});
+    if (ub <= 4) return f(IC<4>{});
+    if constexpr (sizeof(T) == 2) if (ub <= 5) return f(IC<5>{});
+    if (ub <= 6) return f(IC<6>{});
+    if constexpr (sizeof(T) == 2) {
+        return f(IC<8>{});
+    } else {
+        if (ub <= 8) return f(IC<8>{});
+        if (ub <= 12) return f(IC<12>{});
+        return f(IC<16>{});
     }
 }
 
-template <int MODE> hipError_t launch_tiles(const PagedArgs& p, hipStream_t stream)
+template <typename T, int MODE> hipError_t launch_tiles(const PagedArgs& p, hipStream_t stream)
 {
-    return by_row(p.cache.row_bytes, [&](auto ubc) {
+    return by_row<T>(p.cache.row_bytes, [&](auto ubc) {
         constexpr int UB = decltype(ubc)::value;
-        if constexpr (UB > 5) return launch<UB, -1, MODE>(p, stream);
-        else return p.cache.row_bytes == UB * 64 ? launch<UB, 0, MODE>(p, stream) : launch<UB, 32, MODE>(p, stream);
+        if constexpr (sizeof(T) == 4 || UB > 5) return launch<T, UB, -1, MODE>(p, stream);
+        else return p.cache.row_bytes == UB * 64 ? launch<T, UB, 0, MODE>(p, stream) : launch<T, UB, 32, MODE>(p, stream);
+    });
+}
+
+template <typename T> int64_t tiles_workspace(const PagedArgs& p)
+{
+    return by_row<T>(p.cache.row_bytes, [&](auto ubc) {
+        constexpr int UB = decltype(ubc)::value;
+        return partial_bytes(workgroups<T, UB>(), TilesCfg<T, UB>::ROWS, TilesCfg<T, UB>::COLS);
     });
 }
 

@@ -3,6 +3,6 @@
 
 namespace attnw {
 
-hipError_t launch_paged_tiles_bias(const PagedArgs& p, hipStream_t stream) { return launch_tiles<kBias>(p, stream); }
+hipError_t launch_paged_tiles_bias(const PagedArgs& p, hipStream_t stream) { return launch_tiles<uint16_t, kBias>(p, stream); }
 
 }  // namespace attnw

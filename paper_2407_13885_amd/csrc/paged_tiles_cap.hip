@@ -3,6 +3,6 @@
 
 namespace attnw {
 
-hipError_t launch_paged_tiles_cap(const PagedArgs& p, hipStream_t stream) { return launch_tiles<kCap>(p, stream); }
+hipError_t launch_paged_tiles_cap(const PagedArgs& p, hipStream_t stream) { return launch_tiles<uint16_t, kCap>(p, stream); }
 
 }  // namespace attnw

@@ -84,6 +84,14 @@ __device__ __forceinline__ void dma16_untracked(const char* base, uint32_t offse
 #endif
 }
 
+// 4 bytes per lane (lane i lands at lds_base + 4 i).
+__device__ __forceinline__ void dma4_untracked(const char* src, uint32_t lds_base)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_base), "v"(src) : "memory", "m0");
+#endif
+}
+
 __device__ __forceinline__ uint32_t lds_offset_of(const void* p)
 {
     return (uint32_t)(uintptr_t)(lds_ptr)(p);
