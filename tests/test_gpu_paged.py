@@ -339,6 +339,9 @@ def _odd(b, h, m):
     ([900, 65], 2, 80, 48, 64, 3, _odd),
     ([4097], 1, 256, 1, 1, 0, _ties),
     ([2000], 2, 32, 128, 1999, 1000, _ties),
+    ([16385, 12000], 1, 16, 64, 5000, 77, _heavy),
+    ([40000], 1, 16, 64, 39990, 5, _ties),
+    ([65537], 1, 16, 128, 30001, 1, _odd),
 ])
 def test_eviction(dtype, lengths, kv_heads, d, page, keep, recent, sums):
     check_eviction(dtype, lengths, kv_heads, d, page, keep, recent, sums)
