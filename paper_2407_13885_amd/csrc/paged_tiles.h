@@ -24,7 +24,7 @@ template <typename T, int UB> struct TilesCfg {
     static constexpr int COLS = DB / (int)sizeof(T), CB = COLS / 16;
     static constexpr bool PIPE = NX == 2;         // registers for the scores of two tiles
     static constexpr int RING = 4;                // tiles of K, and of V, on chip
-    static constexpr int LDS = 2 * RING * TILE + kPlaces * 8;
+    static constexpr int LDS = 2 * RING * TILE + kPlaces * 8 + RING * 32;
     static constexpr int PER_CU = NW == 4 && LDS <= 80 * 1024 ? 2 : 1;
     static_assert(2 * RING * TILE <= kDirectLds, "reach of direct transfers");
 };
@@ -42,6 +42,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
     char* const k_lds = lds;
     char* const v_lds = lds + RING * TILE;
     int64_t* const places = reinterpret_cast<int64_t*>(lds + 2 * RING * TILE);
+    uint32_t* const lost_in = reinterpret_cast<uint32_t*>(lds + 2 * RING * TILE + kPlaces * 8);   // [tile of V][wave]: what is no number there
     if constexpr (UNIFORM) grain = 4;
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -205,10 +206,9 @@ void paged_tiles_kernel(AttendArgs a, int grain)
             }
             if (!whole) {
                 // (a value that is no number must not reach the rows that do not see it: paged_rows.h)
-                uint32_t bad = 0;
-#pragma unroll
-                for (int i = 0; i < CB; ++i) bad |= any_lost<T>(v_frag(buf, i));
-                if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
+                u32x4 bad = *reinterpret_cast<const u32x4*>(lost_in + buf * 8);
+                if constexpr (NW == 8) bad |= *reinterpret_cast<const u32x4*>(lost_in + buf * 8 + 4);
+                if (__builtin_amdgcn_readfirstlane(bad[0] | bad[1] | bad[2] | bad[3]) != 0) {
                     u32x4 sw[NX];
 #pragma unroll
                     for (int x = 0; x < NX; ++x) {
@@ -540,7 +540,19 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 #pragma clang loop unroll(disable)
                     for (int i = 0; i < n; ++i) {
                         if (i % 2 == 0) {
-                            wait_vmem();
+                            arrived<0>();
+                            // (what a wave brought of V it looks over itself)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int buf = (i + k) & (RING - 1);
+                                uint32_t bad = 0;
+#pragma unroll
+                                for (int j = 0; j < XW; ++j)
+                                    if (XFERS % NW == 0 || wave + NW * j < XFERS)
+                                        bad |= any_lost<T>(*reinterpret_cast<const u32x4*>(v_lds + buf * TILE + (wave + NW * j) * 1024 + lane * 16));
+                                const uint32_t some = __builtin_amdgcn_ballot_w64(bad != 0) != 0 ? 1u : 0u;
+                                if (lane == 0) lost_in[buf * 8 + wave] = some;
+                            }
                             __syncthreads();      // two tiles are there, and nobody reads the two before them any more
                             if (i + 2 < n) issue(i + 2);
                             if (i + 3 < n) issue(i + 3);
@@ -619,9 +631,9 @@ template <typename T, typename F> auto by_row(int row_bytes, F&& f)
     const int ub = (row_bytes + 63) / 64;
     if (ub <= 1) return f(IC<1>{});
     if (ub <= 2) return f(IC<2>{});
-    if constexpr (sizeof(T) == 2) if (ub <= 3) return f(IC<3>{});
+    if (ub <= 3) return f(IC<3>{});
     if (ub <= 4) return f(IC<4>{});
-    if constexpr (sizeof(T) == 2) if (ub <= 5) return f(IC<5>{});
+    if (ub <= 5) return f(IC<5>{});
     if (ub <= 6) return f(IC<6>{});
     if constexpr (sizeof(T) == 2) {
         return f(IC<8>{});
