@@ -123,6 +123,16 @@ template <typename T> __device__ __forceinline__ u32x4 without_lost(const u32x4&
     return r;
 }
 
+// Below 0 where a token at slot `query` does not see slot j, `past` the first that nobody sees: in numbers, as conditions the compiler makes a branch of each.
+struct Sight {
+    int32_t low, high, prefix;
+    __device__ __forceinline__ Sight(int32_t query, const RuleView& r, int32_t prefix_, int32_t past)
+        : low(query - r.window + 1), high(min(query, past - 1)), prefix(min(prefix_, past))
+    {
+    }
+    __device__ __forceinline__ int32_t hidden(int32_t j) const { return ((j - low) | (high - j)) & ~(j - prefix); }
+};
+
 // A value that all lanes of a wave have, as one that the compiler knows they have.
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 

@@ -153,11 +153,9 @@ void paged_rows_kernel(AttendArgs a, int grain)
                     }
                     const bool whole = key0 + KT <= k1 && ((key0 + KT - 1 <= first && key0 > last - a.rule.window) || key0 + KT <= prefix);
                     if (!whole) {
+                        const Sight sight(query, a.rule, prefix, k1);
 #pragma unroll
-                        for (int i = 0; i < NK * 4; ++i) {
-                            const int j = key + 16 * (i / 4) + i % 4;
-                            if (j >= k1 || ((uint32_t)(query - j) >= (uint32_t)a.rule.window && j >= prefix)) x[i] = -__builtin_inff();
-                        }
+                        for (int i = 0; i < NK * 4; ++i) x[i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? -__builtin_inff() : x[i];
                     }
                     float top = x[0];
 #pragma unroll

@@ -117,13 +117,11 @@ __device__ __forceinline__ void add_weights(f32x4 (&sum)[NK], const SumsKernelAr
             acc[k][e] = fast_exp2(y - lse);
         }
     if (!whole) {
+        const Sight sight(x.query, a.rule, prefix, seq.length);
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = mine + 16 * k + 4 * quarter + e;
-                if (j >= seq.length || ((uint32_t)(x.query - j) >= (uint32_t)a.rule.window && j >= prefix)) acc[k][e] = 0.0f;
-            }
+            for (int e = 0; e < 4; ++e) acc[k][e] = sight.hidden(mine + 16 * k + 4 * quarter + e) < 0 ? 0.0f : acc[k][e];
     }
 #pragma unroll
     for (int k = 0; k < NK; ++k) sum[k] += acc[k];

@@ -47,7 +47,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
-    const uint32_t k_at = lds_offset_of(k_lds), v_at = lds_offset_of(v_lds);
+    const uint32_t k_at = lds_offset_of(k_lds);
     const int rb = SHORT >= 0 ? DB - SHORT : a.cache.row_bytes;
 
     Walk<C::ROWS> walk(a, lane);
@@ -108,19 +108,20 @@ void paged_tiles_kernel(AttendArgs a, int grain)
         const int group = a.group.d, base = seq.length - seq.tokens;              // slot of the first new token
         const int first = base + (int)quotient(row0, a.group), last = base + (int)quotient(row0 + rows - 1, a.group);
         const bool active = wave * 16 * NX < rows;
+        const int lane_of_rows = apart(lane), row_of_lane = lane_of_rows & 15, chunk_of_lane = lane_of_rows >> 4 & 3;
         int query[NX];
         float slope[NX];
         u32x4 qf[NX][G];
 #pragma unroll
         for (int x = 0; x < NX; ++x) {
-            const int row = row0 + min(wave * 16 * NX + 16 * x + l16, rows - 1);
+            const int row = row0 + min(wave * 16 * NX + 16 * x + row_of_lane, rows - 1);
             const int token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
             query[x] = base + token;
             slope[x] = MODE & kBias ? a.rule.slopes[head] * kLog2e : 0.0f;
             const char* q = a.Q + (int64_t)(seq.first + token) * a.q_stride + (int64_t)head * rb;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const int ch = 4 * g + quarter;
+                const int ch = 4 * g + chunk_of_lane;
                 qf[x][g] = ch * 16 < rb ? *reinterpret_cast<const u32x4*>(q + ch * 16) ^ sign_flip : u32x4{0u, 0u, 0u, 0u};
             }
         }
@@ -177,12 +178,11 @@ void paged_tiles_kernel(AttendArgs a, int grain)
             const bool whole = key0 + KT <= past && ((key0 + KT - 1 <= first && key0 > last - a.rule.window) || key0 + KT <= prefix);
             if (!whole) {
 #pragma unroll
-                for (int x = 0; x < NX; ++x)
+                for (int x = 0; x < NX; ++x) {
+                    const Sight sight(query[x], a.rule, prefix, past);
 #pragma unroll
-                    for (int i = 0; i < 4 * NK; ++i) {
-                        const int j = key + 16 * (i / 4) + i % 4;
-                        if (j >= past || ((uint32_t)(query[x] - j) >= (uint32_t)a.rule.window && j >= prefix)) y[x][i] = -__builtin_inff();
-                    }
+                    for (int i = 0; i < 4 * NK; ++i) y[x][i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? -__builtin_inff() : y[x][i];
+                }
             }
             float p[NX][4 * NK];
             u32x4 pw[NX];
@@ -245,7 +245,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
         // the output of tile t - 1 and the scores of tile t + 1 (attention_pipe.hip says why).  One barrier for two tiles.
         auto run_piped = [&](int wa, int wb, int k0) __attribute__((always_inline)) {
             if constexpr (C::PIPE) {
-            const int n_tiles = wb - wa;
+            const int n_tiles = wb - wa, wave_here = apart_uniform(wave), k_here = apart_uniform((int)k_at), v_here = k_here + RING * TILE;
             // ---- transfers.  UNIFORM: the keys of one lie in one page, its place a number of the wave -----------------------------------------
             // (The places of 32 tiles wait in a lane each.  One transfer's keys are among 16 of a tile; where rows are no power of two they are all in one page.)
             constexpr bool HALVES = 64 % CPR == 0;
@@ -253,12 +253,13 @@ void paged_tiles_kernel(AttendArgs a, int grain)
             int64_t place = 0;
             int place_base = 0;
             int lane_off[2][OFFS];
+            const int lane_here = apart(lane);
             if constexpr (UNIFORM) {
 #pragma unroll
                 for (int v = 0; v < 2; ++v)
 #pragma unroll
                     for (int j = 0; j < OFFS; ++j) {
-                        const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
+                        const int x = (wave_here + NW * j) * 64 + lane_here, key = x / CPR;
                         const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
                         lane_off[v][j] = (HALVES ? key & 15 : key) * rb + (SHORT == 0 || ch < rb ? ch : 0);
                     }
@@ -266,22 +267,22 @@ void paged_tiles_kernel(AttendArgs a, int grain)
             auto look_up = [&](int t) __attribute__((always_inline)) {   // for the requests from tile t on, 15 tiles at least
                 if constexpr (UNIFORM) {
                     place_base = 2 * t;
-                    place = places[((wa * 32 - k0) >> 4) + min(2 * t + lane, 2 * n_tiles - 1)];
+                    place = places[((wa * 32 - k0) >> 4) + min(2 * t + lane_here, 2 * n_tiles - 1)];
                 }
             };
             auto transfer = [&](int t, int j, int i) __attribute__((always_inline)) {   // i: which of the four tiles of a pair's requests
-                if (XFERS % NW != 0 && wave + NW * j >= XFERS) return;
+                if (XFERS % NW != 0 && wave_here + NW * j >= XFERS) return;
                 const bool v = i >= 2;
                 const int ahead = t + (i < 2 ? 4 + i : i - 1), tile = min(ahead, n_tiles - 1);
-                const uint32_t to = uniform((int)((v ? v_at : k_at) + (ahead & (RING - 1)) * TILE + (wave + NW * j) * 1024));
+                const uint32_t to = uniform((int)((v ? v_here : k_here) + (ahead & (RING - 1)) * TILE + (wave_here + NW * j) * 1024));
                 const char* const where = v ? a.cache.V : a.cache.K;
                 if constexpr (UNIFORM) {
-                    const int half = HALVES ? ((wave + NW * j) * 64 / CPR) >> 4 : 0, from = 2 * tile + half - place_base;
+                    const int half = HALVES ? ((wave_here + NW * j) * 64 / CPR) >> 4 : 0, from = 2 * tile + half - place_base;
                     const int64_t off = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)place, from) |
                                         (int64_t)__builtin_amdgcn_readlane((int)(place >> 32), from) << 32;
                     dma16_untracked(where + off, (uint32_t)lane_off[v][j % OFFS], to);
                 } else {
-                    const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
+                    const int x = (wave_here + NW * j) * 64 + lane_here, key = x / CPR;
                     const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
                     const int slot = (wa + tile) * 32 + key - k0;
                     const char* src = where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 || ch < rb ? ch : 0);   // (behind a row's end: paged_rows.h)
@@ -516,21 +517,22 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 wait_vmem();
                 __syncthreads();
                 // a transfer of tile t, by lanes: any pages; slots past the end are read as the last
-                auto transfer = [&](const char* from_where, uint32_t to, int t, int j, bool v) __attribute__((always_inline)) {
-                    if (XFERS % NW != 0 && wave + NW * j >= XFERS) return;
-                    const int x = (wave + NW * j) * 64 + lane, key = x / CPR;
+                auto transfer = [&](const char* from_where, uint32_t to, int t, int j, bool v, int lane_here, int wave_here) __attribute__((always_inline)) {
+                    if (XFERS % NW != 0 && wave_here + NW * j >= XFERS) return;
+                    const int x = (wave_here + NW * j) * 64 + lane_here, key = x / CPR;
                     const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
                     const int slot = min(t * KT + key, k1 - 1) - k0;
                     const char* src = from_where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 || ch < rb ? ch : 0);   // (behind a row's end: paged_rows.h)
-                    dma16_untracked(src, to + (wave + NW * j) * 1024);
+                    dma16_untracked(src, to + (wave_here + NW * j) * 1024);
                 };
                 // tiles ta .. tb - 1 one after the other
                 auto run_alone = [&](int ta, int tb) __attribute__((always_inline)) {
+                    const int lane_here = apart(lane), wave_here = apart_uniform(wave), k_here = apart_uniform((int)k_at), v_here = k_here + RING * TILE;
                     auto issue = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
                         for (int j = 0; j < XW; ++j) {
-                            transfer(a.cache.K, uniform((int)(k_at + (i & (RING - 1)) * TILE)), ta + i, j, false);
-                            transfer(a.cache.V, uniform((int)(v_at + (i & (RING - 1)) * TILE)), ta + i, j, true);
+                            transfer(a.cache.K, uniform((int)(k_here + (i & (RING - 1)) * TILE)), ta + i, j, false, lane_here, wave_here);
+                            transfer(a.cache.V, uniform((int)(v_here + (i & (RING - 1)) * TILE)), ta + i, j, true, lane_here, wave_here);
                         }
                     };
                     const int n = tb - ta;
@@ -548,10 +550,10 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                                 uint32_t bad = 0;
 #pragma unroll
                                 for (int j = 0; j < XW; ++j)
-                                    if (XFERS % NW == 0 || wave + NW * j < XFERS)
-                                        bad |= any_lost<T>(*reinterpret_cast<const u32x4*>(v_lds + buf * TILE + (wave + NW * j) * 1024 + lane * 16));
+                                    if (XFERS % NW == 0 || wave_here + NW * j < XFERS)
+                                        bad |= any_lost<T>(*reinterpret_cast<const u32x4*>(v_lds + buf * TILE + (wave_here + NW * j) * 1024 + lane_here * 16));
                                 const uint32_t some = __builtin_amdgcn_ballot_w64(bad != 0) != 0 ? 1u : 0u;
-                                if (lane == 0) lost_in[buf * 8 + wave] = some;
+                                if (lane_here == 0) lost_in[buf * 8 + wave_here] = some;
                             }
                             __syncthreads();      // two tiles are there, and nobody reads the two before them any more
                             if (i + 2 < n) issue(i + 2);
@@ -588,21 +590,22 @@ void paged_tiles_kernel(AttendArgs a, int grain)
         const bool complete = seg.slot < 0;
         float* const out = a.partial + max(seg.slot, 0) * (int64_t)(C::ROWS * (C::COLS + 2));
         if (active) {
+            const int lane_here = apart(lane), row_of_lane = lane_here & 15, quarter_of_lane = lane_here >> 4 & 3;
 #pragma unroll
             for (int x = 0; x < NX; ++x) {
                 const float l = quarter_wave_sum(l_run[x]);
-                const int r = wave * 16 * NX + 16 * x + l16;
+                const int r = wave * 16 * NX + 16 * x + row_of_lane;
                 if (r >= rows) continue;
                 if (complete) {
                     const int row = row0 + r, token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
                     const int64_t o = (int64_t)(seq.first + token) * a.heads + head;
 #pragma unroll
-                    for (int i = 0; i < CB; ++i) store_output<T>(a.O, o, rb, 16 * i + 4 * quarter, oacc[i][x], l);
-                    if (quarter == 0 && a.lse) a.lse[o] = log_sum(m_run[x], l);
+                    for (int i = 0; i < CB; ++i) store_output<T>(a.O, o, rb, 16 * i + 4 * quarter_of_lane, oacc[i][x], l);
+                    if (quarter_of_lane == 0 && a.lse) a.lse[o] = log_sum(m_run[x], l);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < CB; ++i) *reinterpret_cast<f32x4*>(out + r * C::COLS + 16 * i + 4 * quarter) = oacc[i][x];
-                    if (quarter == 0) {
+                    for (int i = 0; i < CB; ++i) *reinterpret_cast<f32x4*>(out + r * C::COLS + 16 * i + 4 * quarter_of_lane) = oacc[i][x];
+                    if (quarter_of_lane == 0) {
                         out[C::ROWS * C::COLS + 2 * r] = m_run[x];
                         out[C::ROWS * C::COLS + 2 * r + 1] = l;
                     }

@@ -112,6 +112,25 @@ __device__ __forceinline__ u32x2 lds_read_tr16(const char* p)
 }
 __device__ __forceinline__ u32x4 u32x4_of(u32x2 lo, u32x2 hi) { return u32x4{lo[0], lo[1], hi[0], hi[1]}; }
 
+// x as a value of its own: what is computed from it stays where it is needed instead of waiting in registers across a whole kernel.
+__device__ __forceinline__ int apart(int x)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+v"(x));
+#endif
+    return x;
+}
+
+// (of a number that all lanes have)
+__device__ __forceinline__ int apart_uniform(int x)
+{
+    x = __builtin_amdgcn_readfirstlane(x);
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+s"(x));
+#endif
+    return x;
+}
+
 template <int I> struct IC { static constexpr int value = I; };
 
 // f(IC<0>{}), f(IC<1>{}), ... f(IC<N-1>{})
