@@ -329,8 +329,8 @@ int64_t attnw_paged_workspace(const attnw_cache *cache, int64_t tokens, int64_t 
  * Attention of the new tokens over the cache, their own slots among them (append first):
  *   O[t][h] = sum_j w_j V_j,  w = softmax of x over the slots that token t sees,
  *   lse[t][h] = log sum_j exp(x_j)   (lse may be NULL).
- * A row that sees nothing gives 0 and -infinity.  Rows of tokens that no sequence owns are
- * not written.
+ * A row that sees nothing gives 0 and -infinity (and so may one all of whose x lie below -10^29).  Rows of
+ * tokens that no sequence owns are not written.
  *
  * Q : rows of heads * d, q_stride apart (a multiple of 16 bytes).   O : [tokens][heads][d], dense.
  * workspace: at least attnw_paged_workspace bytes, 16-byte aligned, of any content; calls that

@@ -315,7 +315,7 @@ int attnw_paged_sums(const attnw_cache* cache, const attnw_rule* rule, const voi
     // (no tokens: the sums from before, still)
     if (!sums || !starts || (tokens > 0 && heads > 0 && (!Q || !lse))) return ATTNW_ERR_NULL;
     if ((e = check_call_support(cache, rule, tokens, heads, q_stride)) != ATTNW_OK) return e;
-    if (heads == 0 || elems > (int64_t)1 << 38) return ATTNW_ERR_UNSUPPORTED;   // (places of 64 slots: fewer than 2^31)
+    if (heads == 0 || elems > (int64_t)1 << 36) return ATTNW_ERR_UNSUPPORTED;   // (blocks of 16 slots or more: fewer than 2^31)
     if (!aligned(cache->K, 16) || !aligned(cache->table, 4) || !aligned(cache->lengths, 4) || !aligned(Q, 16) || !aligned(lse, 4) || !aligned(before, 4) ||
         !aligned(sums, 4) || !aligned(starts, 4) || !aligned(rule->slopes, 4) || !aligned(rule->prefix, 4))
         return ATTNW_ERR_ALIGN;

@@ -85,8 +85,9 @@ template <int ROWS> struct Walk {
         };
         own = Sequence{0, 0, 0};
         own_prefix = 0;
-        int32_t mine = 0, upto = 0;
+        int32_t upto = 0;
         if (held) {
+            int32_t mine = 0;
             if (lane < a.cache.batch) {
                 own = sequence_at(a.cache, a.starts, a.tokens, lane);
                 own_prefix = prefix_at(lane, own);
@@ -104,8 +105,9 @@ template <int ROWS> struct Walk {
         at = deal.first(w);
         end = deal.first(w + 1);
         if (held) {
-            b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < a.cache.batch && upto > at));
-            before = __builtin_amdgcn_readlane(upto - mine, b);
+            const uint64_t past = __builtin_amdgcn_ballot_w64(lane < a.cache.batch && upto > at);
+            b = past ? __builtin_ctzll(past) : a.cache.batch;
+            before = past && b > 0 ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
         } else {
             plan_find(a.cache.batch, lane, at, of, b, before);
         }
@@ -258,7 +260,8 @@ inline int64_t partial_bytes(int workgroups, int rows, int cols) { return (int64
 
 template <typename T> hipError_t launch_join(const AttendArgs& a, int rows, int cols, hipStream_t stream)
 {
-    // few blocks are in many parts each: then more workgroups to a block
+    // Few blocks are in many parts each: then more workgroups to a block.  4 rows a workgroup / 16, us of attention and join: a token over 16384 slots, one
+    // kv head of 128 18.6 / 21.3, 8 kv heads and 4097 slots 12.6 / 12.5; 512 tokens over 14336 slots, 8 kv heads 159 / 146.
     const int64_t blocks = ((int64_t)a.tokens * a.group.d / rows + a.cache.batch) * a.cache.kv_heads;
     if (blocks * 8 <= a.workgroups) paged_join_kernel<T, 4><<<dim3(a.workgroups, rows / 4), 256, 0, stream>>>(a, rows, cols);
     else paged_join_kernel<T, 16><<<dim3(a.workgroups, rows / 16), 256, 0, stream>>>(a, rows, cols);

@@ -45,7 +45,7 @@ __device__ __forceinline__ Sequence sequence_at(const CacheView& c, const int32_
     Sequence s;
     s.length = max(0, min(c.lengths[b], c.slots));
     s.first = max(0, min(starts[b], all));
-    s.tokens = max(0, min(starts[b + 1], all) - s.first);
+    s.tokens = max(0, max(0, min(starts[b + 1], all)) - s.first);   // (the least int would wrap)
     return s;
 }
 
@@ -136,12 +136,16 @@ struct Sight {
 // A value that all lanes of a wave have, as one that the compiler knows they have.
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// Numbers of places are counted up to 2^31 - 1 and no further: more there are only where starts are in no order, and then what comes out is any of the rows, but of
+// the caller's arrays.
+__device__ __forceinline__ int32_t plus(int32_t x, int32_t y) { return __builtin_elementwise_add_sat(x, y); }
+
 // (of the first n lanes)
 __device__ __forceinline__ int32_t wave_inclusive_sum(int32_t v, int lane, int n = 64)
 {
     for (int off = 1; off < n; off <<= 1) {
         const int32_t o = __shfl_up(v, off, 64);
-        if (lane >= off) v += o;
+        if (lane >= off) v = plus(v, o);
     }
     return v;
 }
@@ -150,9 +154,9 @@ __device__ __forceinline__ int32_t wave_inclusive_sum(int32_t v, int lane, int n
 template <typename Count> __device__ __forceinline__ int32_t plan_total(int batch, int lane, Count&& count)
 {
     int32_t sum = 0;
-    for (int b = lane; b < batch; b += 64) sum += count(b);
+    for (int b = lane; b < batch; b += 64) sum = plus(sum, count(b));
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    for (int off = 32; off > 0; off >>= 1) sum = plus(sum, __shfl_xor(sum, off, 64));
     return uniform(sum);
 }
 // The sequence that holds place `at` of the total, and the places before it.
@@ -160,13 +164,12 @@ template <typename Count> __device__ __forceinline__ void plan_find(int batch, i
 {
     int32_t base = 0;
     for (int b0 = 0; b0 < batch; b0 += 64) {
-        const int32_t mine = b0 + lane < batch ? count(b0 + lane) : 0;
-        const int32_t end = base + wave_inclusive_sum(mine, lane);
+        const int32_t end = plus(base, wave_inclusive_sum(b0 + lane < batch ? count(b0 + lane) : 0, lane));
         const uint64_t past = __builtin_amdgcn_ballot_w64(end > at);
         if (past) {
             const int first = __builtin_ctzll(past);
             found = b0 + first;
-            before = __builtin_amdgcn_readlane(end - mine, first);
+            before = first > 0 ? __builtin_amdgcn_readlane(end, first - 1) : base;
             return;
         }
         base = __builtin_amdgcn_readlane(end, 63);

@@ -169,6 +169,17 @@ def test_contents_out_of_range_stay_in_range():
     assert bool((O[1:3] == 0).all())
 
 
+@pytest.mark.parametrize("batch", [3, 100])
+def test_starts_in_no_order(batch):
+    """Sequences that claim each other's tokens, and tokens that there are not: any of the rows, but nothing outside the arrays."""
+    p = Problem("bf16", [(2, 50 + b % 7) for b in range(batch)], 4, 2, 64, 16, garbage=False)
+    p.starts = torch.tensor([(-3, 0, p.T, (1 << 31) - 1, 2, -(1 << 31), 7)[b % 7] for b in range(batch + 1)], dtype=torch.int32)
+    O, lse = p.on_gpu().run_attention()
+    sums = torch.zeros((batch, 2, p.max_pages * 16), device="cuda")
+    p.run_sums(torch.nan_to_num(lse, neginf=0.0), None, sums)
+    assert O.shape[0] == p.T and bool(torch.isfinite(O).all()) and bool(torch.isfinite(sums).all())
+
+
 def test_offsets_beyond_32_bits():
     """The last pages of a cache of more than 4 GiB of keys."""
     p = Problem("bf16", [(1, 70)], 2, 1, 256, 16)

@@ -31,7 +31,7 @@ def attend(c=None, rule=None, q=Q, o=O, lse=LSE, starts=STARTS, tokens=3, heads=
 CACHES = [(dict(dtype=7), E_DTYPE), (dict(dtype=7, K=None), E_DTYPE), (dict(pages=-1), E_SHAPE), (dict(d=-64, K=None), E_SHAPE),
           (dict(pages=1 << 40, page_size=1 << 40), E_SHAPE), (dict(K=None), E_NULL), (dict(V=None), E_NULL), (dict(table=None), E_NULL),
           (dict(lengths=None), E_NULL), (dict(d=24), E_UNSUP), (dict(d=272), E_UNSUP), (dict(d=0), E_UNSUP), (dict(d=6, dtype=F32), E_UNSUP),
-          (dict(page_size=0), E_UNSUP), (dict(pages=0), E_UNSUP), (dict(max_pages=1 << 27), E_UNSUP), (dict(K=K + 8), E_ALIGN), (dict(V=V + 2), E_ALIGN),
+          (dict(page_size=0), E_UNSUP), (dict(pages=0), E_UNSUP), (dict(max_pages=1 << 27), E_UNSUP), (dict(page_size=1 << 24), E_UNSUP), (dict(K=K + 8), E_ALIGN), (dict(V=V + 2), E_ALIGN),
           (dict(table=TABLE + 2), E_ALIGN), (dict(lengths=LENGTHS + 1), E_ALIGN)]
 
 
@@ -43,11 +43,9 @@ def test_caches(more, want):
     assert status("attnw_cache_append", c, Q, Q + 0x1000, Q + 0x2000, O, WORK, None, STARTS, 3, 4, 0, 0, 4 * d, 2 * d, 0) == want
     if "V" not in more:                           # (sums do not look at V)
         assert status("attnw_paged_sums", c, binding.AttnwRule(0.125), Q, LSE, None, O, STARTS, 3, 4, 4 * d) == want
-    good = cache(**{k: v for k, v in more.items() if k in ("d", "dtype")})
     if want != E_DTYPE:
         assert status("attnw_cache_evict", c, cache(K=Q, V=O, table=STARTS, lengths=WORK, **{k: v for k, v in more.items() if k in ("d", "dtype")}),
                       LSE, LSE + 0x100000, LSE + 0x200000, 8, 2) == want
-    del good
 
 
 def test_attention():
