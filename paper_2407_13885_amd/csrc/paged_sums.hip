@@ -6,8 +6,9 @@
 //
 // A workgroup owns the slots that it sums over: no atomics, K read once, sums in an order that the sizes alone decide.  Chunks: the waves of a workgroup keep
 // the same keys in registers and take the rows in turn, 16 at a time, straight from the caches, the next ones on their way; their sums are joined in the end (what
-// bounds it are the exponentials, as many as scores: three transcendental instructions each with a cap).  Single tokens: the waves hold the rows and have
-// keys of their own, some tiles of which are always on their way into LDS (what bounds it is the read of K).
+// bounds it are the exponentials, as many as scores: three transcendental instructions each with a cap; two chunks of 1024 tokens over 9216 slots at most, 16 heads of 64 with a
+// cap and a window 91 us).  Single tokens and short chunks: the waves hold the rows and have keys of their own, some tiles of which are always on their way into LDS
+// (what bounds it is the read of K; one token each over 64 sequences of 16384 slots, 8 kv heads of 128 422 us, 5.1 TB/s).
 #include "qk_common.h"
 #include "attention_common.h"
 #include "paged_common.h"
@@ -352,7 +353,9 @@ template <typename T, int UB, int MODE> hipError_t launch(const SumsArgs& p, hip
     a.cache = p.cache;
     a.rule = p.rule;
     // (workgroups of unequal work in several rounds: those that end early make room)
-    const bool turns = p.tokens * (int64_t)a.group.d > 32 * (int64_t)p.cache.batch;
+    // Rows of a sequence, on average.  Held / in turns, us: bf16, 8 sequences of 4096 slots, 4 kv heads of 128: 128 rows 27 / 40, 256 42 / 45, 384 57 / 52, 1024
+    // 136 / 90; 64 of them 164 / 239, 283 / 298, 451 / 351, 1236 / 636.  fp32, 4 of them: 128 rows 65 / 54, 256 117 / 73; d = 64, a cap: 96 rows 41 / 54, 192 73 / 66.
+    const bool turns = p.tokens * (int64_t)a.group.d > (sizeof(T) == 2 ? 256 : 96) * (int64_t)p.cache.batch;
     const uint32_t grid = (uint32_t)((compute_units() * (turns ? 16 : StepCfg<T, UB>::PER_CU) + 7) & ~7);
     const int grain = key_grain(a.cache);
     if (turns) paged_sums_kernel<T, UB, MODE><<<grid, 256, 0, stream>>>(a, grain);

@@ -31,8 +31,7 @@ struct Units {
 // A unit: V columns and their V partners (halves), V neighbouring columns (interleaved), or V columns behind the turned ones, which are copied.
 // CACHE: with keys and values; heads 0 .. heads - 1 are queries, then kv_heads of keys, then kv_heads of values (which have the units of a
 // head that does not turn).
-// A thread loads all it needs for some units before it stores any (16 KiB of rows a workgroup in flight instead of 4: chunks of 9923 tokens, 48 heads of
-// 128 80 -> 60 us).
+// With caches a thread loads all it needs for some units before it stores any (chunks of 9923 tokens, 48 heads of 128 80 -> 64 us).
 template <typename T, int V, bool INTERLEAVED, bool CACHE>
 __global__ __launch_bounds__(256)
 void rotary_kernel(const T* Q, const T* K, const T* Vn, T* R, T* Kc, T* Vc, const float* __restrict__ angles, const int32_t* __restrict__ positions,

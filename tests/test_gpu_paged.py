@@ -284,6 +284,47 @@ def test_sums_of_rows_that_see_nothing():
     assert bool((sums[:, :, :2] == 0).all()) and bool((sums[:, :, 2:] == 5).all())
 
 
+# (long enough that waves take rows in turns, in either type)
+LONG = [
+    ("one chunk", [(600, 777)], 2, 2, 64, 16),
+    ("beside others and none", [(700, 900), (0, 40), (3, 65), (0, 0), (513, 513)], 8, 4, 128, 20),
+    ("groups that blocks cut", [(95, 190), (61, 61)], 21, 3, 32, 7),
+    ("pages of one slot", [(300, 1101)], 2, 1, 16, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name,sequences,heads,kv_heads,d,page", LONG, ids=[s[0] for s in LONG])
+def test_sums_of_long_chunks(dtype, name, sequences, heads, kv_heads, d, page):
+    test_sums(dtype, name, sequences, heads, kv_heads, d, page)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name,more", RULES, ids=[r[0] for r in RULES])
+def test_sums_of_rules_and_long_chunks(dtype, name, more):
+    p = Problem(dtype, [(1, 410), (40, 333), (400, 620)], 8, 4, 64, 32, seed=3, **more).on_gpu()
+    _, lse, _, _ = p.attention()
+    want, bound = p.collected(lse.float(), None)
+    within(p.run_sums(lse.float().cuda(), None, torch.zeros(want.shape, device="cuda")), want, bound, "sums")
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", d) for d in (16, 80, 144, 256)] + [("f32", d) for d in (4, 36, 100, 252)])
+def test_sums_of_head_sizes_and_long_chunks(dtype, d):
+    p = Problem(dtype, [(1, 190), (290, 375)], 4, 2, d, 16, seed=d).on_gpu()
+    _, lse, _, _ = p.attention()
+    want, bound = p.collected(lse.float(), None)
+    within(p.run_sums(lse.float().cuda(), None, torch.zeros(want.shape, device="cuda")), want, bound, "sums")
+
+
+def test_sums_of_long_chunks_that_see_nothing():
+    p = Problem("bf16", [(400, 460)], 4, 2, 64, 16, more_pages=1)
+    p.lengths[0] = 2
+    p.on_gpu()
+    lse = torch.full((400, 4), -math.inf, device="cuda")
+    sums = p.run_sums(lse, None, torch.full((1, 2, p.max_pages * 16), 5.0, device="cuda"))
+    assert bool((sums[:, :, :2] == 0).all()) and bool((sums[:, :, 2:] == 5).all())
+
+
 # ---- eviction -----------------------------------------------------------------------------------------------------------------------------
 
 def check_eviction(dtype, lengths, kv_heads, d, page, keep, recent, sums, into_page=None, more_pages=0):
