@@ -90,6 +90,8 @@ class PagedLayer:
         positions = torch.tensor(self.next_position, dtype=torch.int32, device="cuda") - 1
         projected = torch.empty((self.batch, self.w_in.shape[1]), dtype=torch.bfloat16, device="cuda")
         buffers = self.buffers(self.batch)
+        # (a recording holds addresses, not tensors: all that it reads and writes has to live as long as it does)
+        buffers.update(starts=starts, positions=positions)
         graph = torch.cuda.CUDAGraph()
         torch.cuda.synchronize()
         with torch.cuda.graph(graph, stream=torch.cuda.Stream()):

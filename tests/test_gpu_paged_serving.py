@@ -100,3 +100,26 @@ def test_the_example_runs(example, capsys):
     example.main()
     text = capsys.readouterr().out
     assert "slots after eviction down to 512: [512, 333, 64, 512]" in text and "slots after 32 tokens" in text
+
+
+def test_a_recording_keeps_what_it_reads(example):
+    """Small tensors made between the replays take no memory that the recording reads or writes: their contents stay, and the outputs are right."""
+    torch.manual_seed(4)
+    model, cap = 256, 20.0
+    layer = example.PagedLayer(model, heads=4, kv_heads=2, d=64, batch=3, pages=60, max_pages=10, page_size=16, rot=32, positions=512, cap=cap)
+    dense = [Dense(layer, cap) for _ in range(3)]
+    x = [torch.randn((n, model), device="cuda").to(torch.bfloat16) for n in (40, 33, 5)]
+    for d, c, out in zip(dense, x, layer.prefill(x)):
+        near(out, d.forward(c))
+    step = layer.recorded_step()
+    others = []
+    for i in range(6):
+        for n in (1, 3, 4, 32, 128):              # up to 512 bytes: the sizes that starts and positions have
+            others += [torch.full((n,), 400 + i, dtype=torch.int32, device="cuda") for _ in range(8)]
+        token = torch.randn((3, model), device="cuda").to(torch.bfloat16)
+        out = step(token)
+        torch.cuda.synchronize()
+        for b in range(3):
+            near(out[b:b + 1], dense[b].forward(token[b:b + 1]))
+    for k, other in enumerate(others):
+        assert bool((other == 400 + k // 40).all()), f"tensor {k}, of {other.numel()} numbers, was written to"
