@@ -87,7 +87,7 @@ class PagedLayer:
         """One token of every sequence: a function from x [batch][model] to the layer's output.  What lies between the projections is recorded once and
         replayed.  (Not the projections: a library's product may clear memory on its way in a form that a replay does not repeat.)"""
         starts = torch.arange(self.batch + 1, dtype=torch.int32, device="cuda")
-        positions = torch.tensor(self.next_position, dtype=torch.int32, device="cuda") - 1
+        positions = torch.zeros(self.batch, dtype=torch.int32, device="cuda")
         projected = torch.empty((self.batch, self.w_in.shape[1]), dtype=torch.bfloat16, device="cuda")
         buffers = self.buffers(self.batch)
         # (a recording holds addresses, not tensors: all that it reads and writes has to live as long as it does)
@@ -96,12 +96,12 @@ class PagedLayer:
         torch.cuda.synchronize()
         with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
             self.lengths.add_(1)
-            positions.add_(1)
             self.attend(projected, starts, positions, buffers)
 
         def step(x):
             self.reserve([1] * self.batch)
             self.in_use = [m + 1 for m in self.in_use]
+            positions.copy_(torch.tensor(self.next_position, dtype=torch.int32))
             self.next_position = [p + 1 for p in self.next_position]
             projected.copy_(x @ self.w_in)
             graph.replay()

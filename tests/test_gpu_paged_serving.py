@@ -123,3 +123,27 @@ def test_a_recording_keeps_what_it_reads(example):
             near(out[b:b + 1], dense[b].forward(token[b:b + 1]))
     for k, other in enumerate(others):
         assert bool((other == 400 + k // 40).all()), f"tensor {k}, of {other.numel()} numbers, was written to"
+
+
+def test_prompts_between_recorded_steps(example):
+    """More of a prompt goes in between two replays: the next token's position follows it."""
+    torch.manual_seed(5)
+    model, cap = 256, 20.0
+    layer = example.PagedLayer(model, heads=4, kv_heads=2, d=64, batch=2, pages=60, max_pages=10, page_size=16, rot=64, positions=512, cap=cap)
+    dense = [Dense(layer, cap) for _ in range(2)]
+
+    def prompt(*sizes):
+        x = [torch.randn((n, model), device="cuda").to(torch.bfloat16) for n in sizes]
+        for d, c, out in zip(dense, x, layer.prefill(x)):
+            if c.shape[0]:
+                near(out, d.forward(c))
+    prompt(20, 7)
+    step = layer.recorded_step()
+    for sizes in ((0, 30), (17, 1)):
+        for _ in range(2):
+            token = torch.randn((2, model), device="cuda").to(torch.bfloat16)
+            out = step(token)
+            torch.cuda.synchronize()
+            for b in range(2):
+                near(out[b:b + 1], dense[b].forward(token[b:b + 1]))
+        prompt(*sizes)
