@@ -199,9 +199,10 @@ def _entry_point(pointers: int, sizes: int, scales: int, dtypes: int):
     return lambda function: _in_front(function, _points, (pointers, sizes, scales, dtypes))
 
 
-def _word_entry_point(kinds: str):
-    """The same for arguments of the given kinds (s: a structure, p: an address, i: a whole number, n: one of 32 bits) and a stream."""
-    return lambda function: _in_front(function, _word_points, (kinds,))
+def _word_entry_point(kinds: str, *structures):
+    """The same for arguments of the given kinds (s: a structure, of the next of the types, p: an address, i: a whole number, n: one of 32 bits)
+    and a stream."""
+    return lambda function: _in_front(function, _word_points, (kinds, structures))
 
 
 def _attach() -> None:
@@ -219,7 +220,7 @@ def _attach() -> None:
         scope["direct"] = _direct[function.__name__] = _entry.Entry(function, _check, *kinds)
     try:
         entries = [_entry.Words(function, _check, *kinds) for function, kinds, _ in _word_points]
-    except (AttributeError, ValueError):          # (built from sources older than this file: ctypes alone for these until the next build)
+    except (AttributeError, TypeError, ValueError):   # (built from sources older than this file: ctypes alone for these until the next build)
         return
     for (function, _, scope), entry in zip(_word_points, entries):
         scope["direct"] = _word_direct[function.__name__] = entry
@@ -310,7 +311,7 @@ def attnw_rotary(X, Y, table, positions, tokens: int, heads: int, d: int, rot: i
                                        int(layout), int(inverse), int(dtype), _stream(stream)))
 
 
-@_word_entry_point("spppppppiiiiiin")
+@_word_entry_point("spppppppiiiiiin", AttnwCache)
 def attnw_cache_append(cache, Q, K, V, R, table, positions, starts, tokens: int, heads: int, rot: int, rows: int, q_stride: int,
                        kv_stride: int, layout: int, stream=None) -> None:
     """Queries turned, keys turned and values into the cache; see ``attnw_cache_append`` in include/attnw.h."""
@@ -325,7 +326,7 @@ def attnw_paged_workspace(cache, tokens: int, heads: int) -> int:
     return size
 
 
-@_word_entry_point("ssppppiiipi")
+@_word_entry_point("ssppppiiipi", AttnwCache, AttnwRule)
 def attnw_paged_attention(cache, rule, Q, O, lse, starts, tokens: int, heads: int, q_stride: int, workspace, workspace_bytes: int,
                           stream=None) -> None:
     """Attention of new tokens over a paged cache; see ``attnw_paged_attention`` in include/attnw.h."""
@@ -333,14 +334,14 @@ def attnw_paged_attention(cache, rule, Q, O, lse, starts, tokens: int, heads: in
                                                 _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
-@_word_entry_point("sspppppiii")
+@_word_entry_point("sspppppiii", AttnwCache, AttnwRule)
 def attnw_paged_sums(cache, rule, Q, lse, before, sums, starts, tokens: int, heads: int, q_stride: int, stream=None) -> None:
     """The weight that slots collect from new tokens; see ``attnw_paged_sums`` in include/attnw.h."""
     _check(load_library().attnw_paged_sums(_cache(cache), _rule(rule), _ptr(Q), _ptr(lse), _ptr(before), _ptr(sums), _ptr(starts), tokens, heads,
                                            q_stride, _stream(stream)))
 
 
-@_word_entry_point("sspppii")
+@_word_entry_point("sspppii", AttnwCache, AttnwCache)
 def attnw_cache_evict(cache, into, sums, into_sums, kept, keep: int, recent: int, stream=None) -> None:
     """The slots that collected the most weight into other pages; see ``attnw_cache_evict`` in include/attnw.h."""
     _check(load_library().attnw_cache_evict(_cache(cache), _cache(into), _ptr(sums), _ptr(into_sums), _ptr(kept), keep, recent, _stream(stream)))

@@ -175,6 +175,7 @@ struct Words {
     PyObject_HEAD
     vectorcallfunc call;
     PyObject *any, *check;
+    PyObject* structures;                         // a tuple: the types of the 's' among the arguments, in order
     void* fn;
     int count;
     char kinds[kMostWords];                       // 's' a structure of the binding, 'p' an address, 'i' a whole number of 64 bits, 'n' one of 32; the stream is not among them
@@ -198,11 +199,12 @@ PyObject* words_call(PyObject* self, PyObject* const* args, size_t nargsf, PyObj
     const Py_ssize_t given = PyVectorcall_NARGS(nargsf);
     if (e->fn && (!names || PyTuple_GET_SIZE(names) == 0) && (given == e->count || given == e->count + 1)) {
         i64 w[kMostWords];
-        int ok = 1;
+        int ok = 1, structure = 0;
         for (int i = 0; ok > 0 && i < e->count; ++i) {
             if (e->kinds[i] == 's') {             // (an address of anything else would be read as one: the Python function refuses it)
                 void* p = nullptr;
-                ok = PyLong_CheckExact(args[i]) ? 0 : address(args[i], s_address, false, &p);
+                PyObject* const type = PyTuple_GET_ITEM(e->structures, structure++);
+                ok = args[i] == Py_None ? 1 : PyObject_TypeCheck(args[i], reinterpret_cast<PyTypeObject*>(type)) ? address(args[i], s_address, false, &p) : 0;
                 w[i] = static_cast<i64>(reinterpret_cast<uintptr_t>(p));
             } else if (e->kinds[i] == 'p') {
                 void* p = nullptr;
@@ -233,20 +235,25 @@ PyObject* words_call(PyObject* self, PyObject* const* args, size_t nargsf, PyObj
     return PyObject_Vectorcall(e->any, args, nargsf, names);
 }
 
-// Words(function, check, kinds)
+// Words(function, check, kinds, types of the structures)
 int words_init(PyObject* self, PyObject* args, PyObject*)
 {
     Words* const e = reinterpret_cast<Words*>(self);
-    PyObject *any, *check;
+    PyObject *any, *check, *types;
     const char* kinds;
-    if (!PyArg_ParseTuple(args, "OOs", &any, &check, &kinds)) return -1;
+    if (!PyArg_ParseTuple(args, "OOsO!", &any, &check, &kinds, &PyTuple_Type, &types)) return -1;
     const size_t count = strlen(kinds);
-    if (count < 1 || count >= kMostWords || strspn(kinds, "spin") != count) {
+    Py_ssize_t structures = 0;
+    for (const char* k = kinds; *k; ++k) structures += *k == 's';
+    bool known = count >= 1 && count < kMostWords && strspn(kinds, "spin") == count && PyTuple_GET_SIZE(types) == structures;
+    for (Py_ssize_t i = 0; known && i < structures; ++i) known = PyType_Check(PyTuple_GET_ITEM(types, i));
+    if (!known) {
         PyErr_SetString(PyExc_ValueError, "no such entry point");
         return -1;
     }
     Py_XSETREF(e->any, Py_NewRef(any));
     Py_XSETREF(e->check, Py_NewRef(check));
+    Py_XSETREF(e->structures, Py_NewRef(types));
     e->fn = nullptr;
     e->count = static_cast<int>(count);
     memcpy(e->kinds, kinds, count);
@@ -267,6 +274,7 @@ int words_traverse(PyObject* self, visitproc visit, void* arg)
     Words* const e = reinterpret_cast<Words*>(self);
     Py_VISIT(e->any);
     Py_VISIT(e->check);
+    Py_VISIT(e->structures);
     return 0;
 }
 
@@ -275,6 +283,7 @@ int words_clear(PyObject* self)
     Words* const e = reinterpret_cast<Words*>(self);
     Py_CLEAR(e->any);
     Py_CLEAR(e->check);
+    Py_CLEAR(e->structures);
     return 0;
 }
 

@@ -184,3 +184,24 @@ def test_the_callable_in_front_is_the_same_as_the_function(name):
         assert _outcome(f, bad, {"stream": stream}) == _outcome(plain, bad, {"stream": stream})
     for wrong in (bad[:-1], bad + [None, None]):
         assert _outcome(f, wrong, {}) == _outcome(plain, wrong, {})
+
+
+class Lookalike:
+    _address = Q
+
+
+def test_structures_are_told_apart():
+    """One structure in the other's place, or anything else that has an address, is refused by both ways in: the host would read past its end."""
+    binding.load_library()
+    rule, c = binding.AttnwRule(0.125), cache()
+    rest = dict(attnw_cache_append=[Q, Q + 0x1000, Q + 0x2000, O, WORK, None, STARTS, 3, 4, 64, 10, 256, 128, 0],
+                attnw_paged_attention=[Q, O, LSE, STARTS, 3, 4, 256, WORK, 1 << 30], attnw_paged_sums=[Q, LSE, None, O, STARTS, 3, 4, 256],
+                attnw_cache_evict=[LSE, LSE + 0x100000, LSE + 0x200000, 8, 2])
+    for name, first in (("attnw_cache_append", [c]), ("attnw_paged_attention", [c, rule]), ("attnw_paged_sums", [c, rule]), ("attnw_cache_evict", [c, c])):
+        f = getattr(binding, name)
+        for i, right in enumerate(first):
+            for wrong in (rule if right is c else c, Lookalike(), Lookalike, 7, "x"):
+                args = first[:i] + [wrong] + first[i + 1:] + rest[name]
+                for call in (f, f.__wrapped__):
+                    with pytest.raises(TypeError, match="expected, not"):
+                        call(*args)
