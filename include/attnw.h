@@ -266,7 +266,9 @@ typedef struct attnw_cache {
  *   x = scale * q . k;   x = cap * tanh(x / cap) where cap > 0;   x = x - slopes[h] * |i - j| where slopes are given,
  * for the slots it sees: j <= i, of those the last `window` (itself among them) where
  * window > 0; and every slot below prefix[b] in any case.  Other slots have no part in
- * the result, whatever K and V hold there (NaN included).  Distances are counted in slots.
+ * the result, whatever K and V hold there (NaN included).  What is infinite or NaN in slots that are seen has the part that
+ * IEEE arithmetic gives it: an infinite value makes its column infinite, or NaN where both signs meet or its weight
+ * is 0 in fp32; a score of -infinity is a weight of 0.  Distances are counted in slots.
  */
 typedef struct attnw_rule {
     float scale, cap;

@@ -157,6 +157,21 @@ template <int ROWS> struct Walk {
     }
 };
 
+// Values that are not finite must not reach the rows that do not see them, by way of a weight of 0: where some are, they count as 0 in the product, and this is
+// what they add to the rows that do see them.  v: a fragment of V; some, none: the weights that are seen, as 1 where they are not 0, and where they are (0
+// times infinity is NaN); multiply(sum, v, weights).
+template <typename T, typename Multiply> __device__ __forceinline__ f32x4 lost_part(const u32x4& v, const u32x4& some, const u32x4& none, Multiply&& multiply)
+{
+    f32x4 up = {0.0f, 0.0f, 0.0f, 0.0f}, down = up, r;
+    multiply(up, lost_as_one<T, kUp>(v), some);
+    multiply(down, lost_as_one<T, kDown>(v), some);
+    multiply(up, lost_as_one<T, kAny>(v), none);
+    multiply(down, lost_as_one<T, kAny>(v), none);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (up[i] > 0.0f ? __builtin_inff() : 0.0f) - (down[i] > 0.0f ? __builtin_inff() : 0.0f);
+    return r;
+}
+
 // A row of partial results, or a whole one: 4 columns of the output of token, head (numbered o), l the sum of its weights.
 template <typename T> __device__ __forceinline__ void store_output(char* O, int64_t o, int rb, int c, f32x4 y, float l)
 {

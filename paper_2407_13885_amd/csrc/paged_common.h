@@ -94,8 +94,8 @@ template <bool CAPPED, bool EXACT> struct ScoreMap {
     }
 };
 
-// Of 16 bytes of elements T: whether one is infinite or NaN; those as 1 and the others as 0; those as 0.  (An exponent of ones carries into the sign's
-// place when one is added at its end.)
+// Of 16 bytes of elements T: whether one is infinite or NaN; those of a kind as 1 and the others as 0; all of them as 0.  (An exponent of ones carries into
+// the sign's place when one is added at its end.)
 template <typename T> __device__ __forceinline__ uint32_t lost_signs(uint32_t w)
 {
     if constexpr (sizeof(T) == 4) return ((w & 0x7f800000u) + 0x00800000u) & 0x80000000u;
@@ -105,11 +105,16 @@ template <typename T> __device__ __forceinline__ uint32_t any_lost(const u32x4& 
 {
     return lost_signs<T>(v[0]) | lost_signs<T>(v[1]) | lost_signs<T>(v[2]) | lost_signs<T>(v[3]);
 }
-template <typename T> __device__ __forceinline__ u32x4 lost_as_one(const u32x4& v)
+enum { kAny, kUp, kDown };                        // of those that are lost: all; +infinity and NaN; -infinity and NaN
+template <typename T, int KIND> __device__ __forceinline__ u32x4 lost_as_one(const u32x4& v)
 {
     u32x4 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = (lost_signs<T>(v[i]) >> 1) - (lost_signs<T>(v[i]) >> 8);   // 0x40.. - 0x00800..
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = v[i], nan = sizeof(T) == 4 ? (w & 0x7fffffffu) + 0x007fffffu : (w & 0x7fff7fffu) + 0x007f007fu;   // (in the signs' places)
+        const uint32_t t = lost_signs<T>(w) & (KIND == kAny ? ~0u : KIND == kUp ? ~w | nan : w | nan);
+        r[i] = (t >> 1) - (t >> 8);               // 0x40.. - 0x00800..
+    }
     return r;
 }
 template <typename T> __device__ __forceinline__ u32x4 without_lost(const u32x4& v)

@@ -207,25 +207,25 @@ void paged_rows_kernel(AttendArgs a, int grain)
                     };
                     const u32x4 pw = operand(p);
                     if (!whole) {
-                        // A value that is no number must not reach the rows that do not see it, by way of a weight of 0: such values
-                        // count as 0, and make the columns of the rows that do see them NaN.
                         uint32_t bad = 0;
 #pragma unroll
                         for (int c = 0; c < CB; ++c) bad |= any_lost<T>(v_frag(c));
-                        if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
-                            float saw[NK * 4];
+                        if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {                      // (lost_part)
+                            const Sight sight(query, a.rule, prefix, k1);
+                            float some[NK * 4], none[NK * 4];
 #pragma unroll
-                            for (int i = 0; i < NK * 4; ++i) saw[i] = x[i] == -__builtin_inff() ? 0.0f : 1.0f;
-                            const u32x4 sw = operand(saw);
+                            for (int i = 0; i < NK * 4; ++i) {
+                                const bool hidden = sight.hidden(key + 16 * (i / 4) + i % 4) < 0;
+                                const uint32_t weight = F32 ? pw[i % 4] : i % 2 ? pw[i / 2 % 4] >> 16 : pw[i / 2 % 4] & 0xffffu;   // (as it is multiplied)
+                                some[i] = hidden || weight == 0 ? 0.0f : 1.0f;
+                                none[i] = hidden || weight != 0 ? 0.0f : 1.0f;
+                            }
+                            const u32x4 so = operand(some), no = operand(none);
 #pragma unroll
                             for (int c = 0; c < CB; ++c) {
-                                const u32x4 v = v_frag(c), lost = lost_as_one<T>(v);
-                                f32x4 hits = {0.0f, 0.0f, 0.0f, 0.0f};
-                                multiply(hits, lost, sw);
+                                const u32x4 v = v_frag(c);
                                 multiply(oacc[c], without_lost<T>(v), pw);
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (hits[r] > 0.0f) oacc[c][r] = __builtin_nanf("");
+                                oacc[c] += lost_part<T>(v, so, no, multiply);
                             }
                             return;
                         }

@@ -206,29 +206,31 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 pw[x] = operand(p[x]);
             }
             if (!whole) {
-                // (a value that is no number must not reach the rows that do not see it: paged_rows.h)
                 u32x4 bad = *reinterpret_cast<const u32x4*>(lost_in + buf * 8);
                 if constexpr (NW == 8) bad |= *reinterpret_cast<const u32x4*>(lost_in + buf * 8 + 4);
-                if (__builtin_amdgcn_readfirstlane(bad[0] | bad[1] | bad[2] | bad[3]) != 0) {
-                    u32x4 sw[NX];
+                if (__builtin_amdgcn_readfirstlane(bad[0] | bad[1] | bad[2] | bad[3]) != 0) {   // (lost_part)
+                    u32x4 so[NX], no[NX];
 #pragma unroll
                     for (int x = 0; x < NX; ++x) {
-                        float saw[4 * NK];
+                        const Sight sight(query[x], a.rule, prefix, past);
+                        float some[4 * NK], none[4 * NK];
 #pragma unroll
-                        for (int i = 0; i < 4 * NK; ++i) saw[i] = y[x][i] == -__builtin_inff() ? 0.0f : 1.0f;
-                        sw[x] = operand(saw);
+                        for (int i = 0; i < 4 * NK; ++i) {
+                            const bool hidden = sight.hidden(key + 16 * (i / 4) + i % 4) < 0;
+                            const uint32_t weight = F32 ? pw[x][i % 4] : i % 2 ? pw[x][i / 2 % 4] >> 16 : pw[x][i / 2 % 4] & 0xffffu;   // (as it is multiplied)
+                            some[i] = hidden || weight == 0 ? 0.0f : 1.0f;
+                            none[i] = hidden || weight != 0 ? 0.0f : 1.0f;
+                        }
+                        so[x] = operand(some);
+                        no[x] = operand(none);
                     }
 #pragma unroll
                     for (int i = 0; i < CB; ++i) {
-                        const u32x4 v = v_frag(buf, i), lost = lost_as_one<T>(v), rest_of = without_lost<T>(v);
+                        const u32x4 v = v_frag(buf, i), rest_of = without_lost<T>(v);
 #pragma unroll
                         for (int x = 0; x < NX; ++x) {
-                            f32x4 hits = {0.0f, 0.0f, 0.0f, 0.0f};
-                            multiply(hits, lost, sw[x]);
                             multiply(oacc[i][x], rest_of, pw[x]);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (hits[r] > 0.0f) oacc[i][x][r] = __builtin_nanf("");
+                            oacc[i][x] += lost_part<T>(v, so[x], no[x], multiply);
                         }
                     }
                     return;

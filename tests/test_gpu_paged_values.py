@@ -1,0 +1,96 @@
+"""Attention over a paged cache and the slots' sums where values or keys are infinite or no numbers: what a row sees has the part that IEEE arithmetic gives
+it, wherever it lies in a tile; what it does not see has none."""
+import math
+
+import pytest
+import torch
+
+from gpu_util import require_gpu
+from paged_util import Problem, within
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    require_gpu()
+
+
+@pytest.fixture(params=[("bf16", "rows"), ("bf16", "tiles"), ("f32", "rows"), ("f32", "tiles")], ids=lambda p: "-".join(p))
+def dtype(request, monkeypatch):
+    monkeypatch.setenv("ATTNW_PAGED_KERNEL", request.param[1])
+    return request.param[0]
+
+
+VALUES = [(99, 0, 4, math.inf), (80, 2, 6, -math.inf), (62, 8, 10, math.nan), (62, 5, 6, math.inf), (71, 9, 12, math.inf), (30, 12, 14, -math.inf),
+          (99, 13, 16, -math.inf)]
+
+
+def expected(p, want, values):
+    """The output with values that are not finite: [tokens][heads][d], 0 where only finite ones are seen, else the infinity or NaN."""
+    extra = torch.zeros_like(want)
+    seen = p.seen(0)
+    for slot, c0, c1, kind in values:
+        at = torch.zeros(want.shape[2], dtype=torch.float64)
+        at[c0:c1] = kind
+        extra += torch.where(seen[:, slot, None, None], at, 0.0)
+    return extra
+
+
+def compare(O, want, off, extra, what):
+    O = O.double().cpu()
+    finite = extra == 0
+    assert bool(finite.any()) and not bool(finite.all())
+    within(torch.where(finite, O, 0.0), torch.where(finite, want, 0.0), torch.where(finite, off, 0.0), what)
+    same = (O == extra) | (torch.isnan(O) & torch.isnan(extra)) | finite
+    assert bool(same.all()), f"{what}: {int((~same).sum())} values are neither the infinity nor the NaN that the definition has"
+
+
+@pytest.mark.parametrize("rule", [dict(), dict(window=30), dict(window=12, prefix=[35]), dict(cap=8.0, slopes=True)], ids=["all", "window", "prefix", "cap"])
+@pytest.mark.parametrize("d,page", [(64, 16), (80, 20)])
+def test_infinite_values(dtype, d, page, rule):
+    p = Problem(dtype, [(40, 100)], 4, 2, d, page, **rule)
+    want, want_lse, off, lse_off = p.attention()
+    for slot, c0, c1, kind in VALUES:
+        p.V[int(p.table[0, slot // page]), :, slot % page, c0:c1] = kind
+    O, lse = p.on_gpu().run_attention()
+    # (columns that two of them meet in: the sum of both)
+    merged = {}
+    for slot, c0, c1, kind in VALUES:
+        for c in range(c0, c1):
+            merged[slot, c] = kind
+    extra = expected(p, want, [(slot, c, c + 1, kind) for (slot, c), kind in merged.items()])
+    # (the plain definition had the values that were there before; those slots' columns are judged by `extra` alone where seen)
+    seen = p.seen(0)
+    for (slot, c) in merged:
+        assert bool((extra[seen[:, slot], :, c] != 0).all())
+    compare(O, want, off, extra, "O")
+    within(lse.cpu(), want_lse, lse_off, "lse")
+
+
+class Some(Problem):
+    """Scores of -infinity are exact."""
+
+    def scores(self, b, h):
+        x, off = super().scores(b, h)
+        return x, torch.where(torch.isinf(x), 0.0, off)
+
+
+def test_a_value_with_a_weight_of_nothing(dtype):
+    """A slot that a row sees with a score of -infinity has a weight of 0: finite values there add nothing, NaN and infinities are NaN."""
+    p = Some(dtype, [(40, 100)], 4, 2, 64, 16)
+    p.Q[:, 0::64] = p.Q[:, 0::64].abs() + 0.25
+    for slot, kind in ((70, math.nan), (85, math.inf)):
+        page = int(p.table[0, slot // 16])
+        p.K[page, :, slot % 16] = 0
+        p.K[page, :, slot % 16, 0] = -math.inf
+        p.V[page, :, slot % 16, 7] = kind
+    O, lse = p.on_gpu().run_attention()
+    want, want_lse, off, lse_off = p.attention()
+    within(lse.cpu(), want_lse, lse_off, "lse")
+    rows = torch.arange(60, 100)
+    assert bool(torch.isnan(O.cpu()[rows >= 70][:, :, 7]).all()), "0 times NaN, 0 times infinity"
+    keep = torch.ones(64, dtype=torch.bool)
+    keep[7] = False
+    within(O.cpu()[:, :, keep], want[:, :, keep], off[:, :, keep], "O")
+    within(O.cpu()[rows < 70], want[rows < 70], off[rows < 70], "O")
