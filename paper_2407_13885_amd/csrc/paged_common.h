@@ -128,6 +128,30 @@ template <typename T> __device__ __forceinline__ u32x4 without_lost(const u32x4&
     return r;
 }
 
+// Rows that are shorter than their place on chip.  Zeros of Q behind their end would make NaN of a product with infinity, so that nothing is multiplied by 0: a key
+// has its first chunks of 16 bytes there once more (d = 4 in fp32: its only one, three times), and the query shares their columns out between the two places (the
+// four), which adds up to the same.
+// Where the chunk at byte `at` of a place comes from, rows being rb bytes, which are half a place at least but for that one:
+__device__ __forceinline__ int chunk_in_row(int at, int rb) { return at < rb ? at : min(at - rb, rb - 16); }
+// Numbers times 2^-halvings: exact, as those below 2^-118, where it might not be, are whole in their first place and 0 in the others.  Infinities and NaN as they are.
+template <typename T> __device__ __forceinline__ uint32_t shared_out(uint32_t w, int halvings, bool first)
+{
+    // (flags in the signs' places: an exponent field of 9 or more)
+    const uint32_t can = sizeof(T) == 4 ? ((w & 0x7f800000u) + 0x7b800000u) & 0x80000000u : ((w & 0x7f807f80u) + 0x7b807b80u) & 0x80008000u;
+    const uint32_t less = w - ((can & ~lost_signs<T>(w)) >> 8) * halvings;
+    return first ? less : less & (sizeof(T) == 4 ? (uint32_t)((int32_t)can >> 31) : (can << 1) - (can >> 15));
+}
+// The chunk of a query that meets chunk `ch` of a key's place of `all` chunks.
+template <typename T> __device__ __forceinline__ u32x4 query_chunk(const char* q, int ch, int all, int rb)
+{
+    const int from = chunk_in_row(ch * 16, rb);
+    const int halvings = rb == 16 ? all / 2 : from + rb < all * 16 ? 1 : 0;   // (rb = 16: all = 4)
+    u32x4 v = *reinterpret_cast<const u32x4*>(q + from);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = shared_out<T>(v[i], halvings, ch * 16 < rb);
+    return v;
+}
+
 // Below 0 where a token at slot `query` does not see slot j, `past` the first that nobody sees: in numbers, as conditions the compiler makes a branch of each.
 struct Sight {
     int32_t low, high, prefix;

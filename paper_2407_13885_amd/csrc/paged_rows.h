@@ -77,8 +77,7 @@ void paged_rows_kernel(AttendArgs a, int grain)
 #pragma unroll
             for (int g = 0; g < UB; ++g) {
                 const int ch = 4 * g + quarter;
-                qf[g] = *reinterpret_cast<const u32x4*>(q + (EXACT || ch * 16 < rb ? ch * 16 : 0));
-                if (!EXACT && ch * 16 >= rb) qf[g] = u32x4{0u, 0u, 0u, 0u};
+                qf[g] = EXACT ? *reinterpret_cast<const u32x4*>(q + ch * 16) : query_chunk<T>(q, ch, CPR, rb);
             }
         }
         f32x4 oacc[CB];
@@ -118,8 +117,8 @@ void paged_rows_kernel(AttendArgs a, int grain)
                             const int ch = v == 0 ? c ^ L::k_chunk(key)
                                          : F32 ? c ^ ((UB % 4 == 0 ? (key >> 2) & 3 : UB % 4 == 2 ? (key >> 2) & 1 : 0) * 4)
                                                : c ^ (L::v16_block(key) * 2);
-                            // (behind a row's end on chip: its first chunk, which meets zeros of Q and columns that nobody stores)
-                            dma16_untracked((v ? a.cache.V : a.cache.K) + row[j] + (EXACT || ch * 16 < rb ? ch * 16 : 0), stage_at + (2 * s + v) * TILE + j * 1024);
+                            // (behind a row's end on chip: its first chunks, which query_chunk expects and which make columns of V that nobody stores)
+                            dma16_untracked((v ? a.cache.V : a.cache.K) + row[j] + (EXACT ? ch * 16 : chunk_in_row(ch * 16, rb)), stage_at + (2 * s + v) * TILE + j * 1024);
                         }
                 };
                 auto compute = [&](int key0, int s, bool more) __attribute__((always_inline)) {

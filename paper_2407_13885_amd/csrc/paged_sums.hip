@@ -31,6 +31,7 @@ struct SumsKernelArgs {
 // NK: blocks of 16 keys of a wave.
 template <typename T, int UB> struct SumsCfg {
     static constexpr int NW = 4, NK = UB <= 2 ? 4 : UB <= 4 ? (sizeof(T) == 2 ? 4 : 2) : UB <= 8 ? 2 : 1, KEYS = 16 * NK;
+    static constexpr int FULL = UB / 2;           // of the groups of 64 bytes, those that rows fill (launch_paged_sums)
 };
 // Single tokens: KT keys of a wave's tile, RING tiles on chip.
 template <typename T, int UB> struct StepCfg {
@@ -63,7 +64,8 @@ template <int UB> struct Rows {
     float lse, slope;
     int query;
 };
-template <int UB, int MODE>
+// TWICE: against keys that have their first chunks once more behind their end (chunk_in_row); else zeros there.
+template <typename T, int UB, int MODE, bool TWICE>
 __device__ __forceinline__ Rows<UB> fetch_rows(const SumsKernelArgs& a, const Sequence& seq, int kv_head, int rb, int r, int last, int lane)
 {
     Rows<UB> x;
@@ -73,8 +75,12 @@ __device__ __forceinline__ Rows<UB> fetch_rows(const SumsKernelArgs& a, const Se
 #pragma unroll
     for (int g = 0; g < UB; ++g) {
         const int ch = 4 * g + (lane >> 4);
-        x.q[g] = *reinterpret_cast<const u32x4*>(q + (ch * 16 < rb ? ch * 16 : 0));
-        if (ch * 16 >= rb) x.q[g] = u32x4{0u, 0u, 0u, 0u};
+        if constexpr (TWICE) {
+            x.q[g] = query_chunk<T>(q, ch, 4 * UB, rb);
+        } else {
+            x.q[g] = *reinterpret_cast<const u32x4*>(q + (ch * 16 < rb ? ch * 16 : 0));
+            if (ch * 16 >= rb) x.q[g] = u32x4{0u, 0u, 0u, 0u};
+        }
     }
     x.lse = a.lse[at_row * a.heads + head];
     x.slope = MODE & kBias ? a.rule.slopes[head] * kLog2e : 0.0f;
@@ -218,8 +224,9 @@ void paged_sums_kernel(SumsKernelArgs a, int grain)
                 const char* src = a.cache.K + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb;
 #pragma unroll
                 for (int g = 0; g < UB; ++g) {
-                    const int ch = 4 * g + quarter;    // (behind a row's end: its first chunk, which meets zeros of Q)
+                    const int ch = 4 * g + quarter;    // (behind a row's end: zeros, as the rows have them)
                     kf[k][g] = *reinterpret_cast<const u32x4*>(src + (ch * 16 < rb ? ch * 16 : 0));
+                    if (g >= C::FULL && ch * 16 >= rb) kf[k][g] = u32x4{0u, 0u, 0u, 0u};
                 }
             }
             int t0, t1;
@@ -233,9 +240,9 @@ void paged_sums_kernel(SumsKernelArgs a, int grain)
             };
             int r = t0 * group + wave * 16;
             if (r < r1) {
-                Rows<UB> x = fetch_rows<UB, MODE>(a, run.seq, run.kv_head, rb, r, r1 - 1, lane);
+                Rows<UB> x = fetch_rows<T, UB, MODE, false>(a, run.seq, run.kv_head, rb, r, r1 - 1, lane);
                 for (; r + 16 * NW < r1; r += 16 * NW) {
-                    const Rows<UB> y = fetch_rows<UB, MODE>(a, run.seq, run.kv_head, rb, r + 16 * NW, r1 - 1, lane);
+                    const Rows<UB> y = fetch_rows<T, UB, MODE, false>(a, run.seq, run.kv_head, rb, r + 16 * NW, r1 - 1, lane);
                     work(r, x);
                     x = y;
                 }
@@ -263,7 +270,8 @@ void paged_sums_kernel(SumsKernelArgs a, int grain)
     }
 }
 
-template <typename T, int UB, int MODE, int THREADS = 64 * StepCfg<T, UB>::NW>
+// EXACT: rows fill their place on chip.
+template <typename T, int UB, int MODE, bool EXACT, int THREADS = 64 * StepCfg<T, UB>::NW>
 __global__ __launch_bounds__(THREADS, 2)
 void paged_sums_step_kernel(SumsKernelArgs a, int grain)
 {
@@ -275,7 +283,7 @@ void paged_sums_step_kernel(SumsKernelArgs a, int grain)
     int64_t* const places = reinterpret_cast<int64_t*>(lds + C::TILES);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
-    const int rb = a.cache.row_bytes, group = a.group.d;
+    const int rb = EXACT ? DB : a.cache.row_bytes, group = a.group.d;
     char* const tiles = lds + wave * RING * PLACE;      // K of a tile, what its slots had
     const uint32_t tiles_at = lds_offset_of(tiles);
     const ScoreMap<(MODE & kCap) != 0, sizeof(T) == 4> map(a.rule);
@@ -284,7 +292,7 @@ void paged_sums_step_kernel(SumsKernelArgs a, int grain)
     while (walk.next(run, places)) {
         const int all = run.seq.tokens * group;
         Rows<UB> held;
-        if (all > 0) held = fetch_rows<UB, MODE>(a, run.seq, run.kv_head, rb, 0, all - 1, lane);
+        if (all > 0) held = fetch_rows<T, UB, MODE, !EXACT>(a, run.seq, run.kv_head, rb, 0, all - 1, lane);
         wait_vmem();
         const float* const had = (a.before ? a.before : a.sums) + run.row;
         // Tile i of the wave (behind the last it is transferred again, unused: as many transfers are under way at any time.)
@@ -294,7 +302,7 @@ void paged_sums_step_kernel(SumsKernelArgs a, int grain)
 #pragma unroll
             for (int j = 0; j < XFERS; ++j) {
                 const int x = j * 64 + lane, key = x / CPR, ch = ((x - key * CPR) ^ L::k_chunk(key)) * 16, slot = min(first + key, run.k1 - 1) - run.k0;
-                dma16_untracked(a.cache.K + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (ch < rb ? ch : 0), to + j * 1024);
+                dma16_untracked(a.cache.K + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (EXACT ? ch : chunk_in_row(ch, rb)), to + j * 1024);
             }
             dma4_untracked(reinterpret_cast<const char*>(had + min(first + lane, run.k1 - 1)), to + TILE);
         };
@@ -309,17 +317,19 @@ void paged_sums_step_kernel(SumsKernelArgs a, int grain)
             f32x4 sum[NK];
 #pragma unroll
             for (int k = 0; k < NK; ++k) sum[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            const auto work = [&](int r, int r1, const Rows<UB>& x) __attribute__((always_inline)) {
+            const auto work = [&](int r, int r1, const Rows<UB>& x, bool twice) __attribute__((always_inline)) {
                 add_weights<T, UB, MODE>(sum, a, run.seq, run.prefix, mine, r, r1, x, lane, [&](int k, int g) __attribute__((always_inline)) {
-                    return *reinterpret_cast<const u32x4*>(kt + (16 * k + l16) * DB + ((4 * g + quarter) ^ L::k_chunk(l16)) * 16);
+                    const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + (16 * k + l16) * DB + ((4 * g + quarter) ^ L::k_chunk(l16)) * 16);
+                    const uint32_t keep = EXACT || twice || g < SumsCfg<T, UB>::FULL || (4 * g + quarter) * 16 < rb ? ~0u : 0u;
+                    return u32x4{kf[0] & keep, kf[1] & keep, kf[2] & keep, kf[3] & keep};
                 }, map);
             };
-            if (all > 16) {                       // (a sequence of more tokens than a step's)
+            if (all > 16) {                       // (a sequence of more tokens than a step's: rows as they are, zeros of keys)
                 int t0, t1;
                 walk.viewers(run, mine, KT, t0, t1);
-                for (int r = t0 * group; r < t1 * group; r += 16) work(r, t1 * group, fetch_rows<UB, MODE>(a, run.seq, run.kv_head, rb, r, t1 * group - 1, lane));
+                for (int r = t0 * group; r < t1 * group; r += 16) work(r, t1 * group, fetch_rows<T, UB, MODE, false>(a, run.seq, run.kv_head, rb, r, t1 * group - 1, lane), false);
             } else if (all > 0 && mine < run.k1) {
-                work(0, all, held);
+                work(0, all, held, true);
             }
             float before[NK];
 #pragma unroll
@@ -358,8 +368,10 @@ template <typename T, int UB, int MODE> hipError_t launch(const SumsArgs& p, hip
     const bool turns = p.tokens * (int64_t)a.group.d > (sizeof(T) == 2 ? 256 : 96) * (int64_t)p.cache.batch;
     const uint32_t grid = (uint32_t)((compute_units() * (turns ? 16 : StepCfg<T, UB>::PER_CU) + 7) & ~7);
     const int grain = key_grain(a.cache);
+    constexpr bool OWN = UB > 1;                  // rows that fill their place: kernels of their own
     if (turns) paged_sums_kernel<T, UB, MODE><<<grid, 256, 0, stream>>>(a, grain);
-    else paged_sums_step_kernel<T, UB, MODE><<<grid, 64 * StepCfg<T, UB>::NW, 0, stream>>>(a, grain);
+    else if (OWN && p.cache.row_bytes == UB * 64) paged_sums_step_kernel<T, UB, MODE, OWN><<<grid, 64 * StepCfg<T, UB>::NW, 0, stream>>>(a, grain);
+    else paged_sums_step_kernel<T, UB, MODE, false><<<grid, 64 * StepCfg<T, UB>::NW, 0, stream>>>(a, grain);
     return hipGetLastError();
 }
 

@@ -123,7 +123,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const int ch = 4 * g + chunk_of_lane;
-                qf[x][g] = ch * 16 < rb ? *reinterpret_cast<const u32x4*>(q + ch * 16) ^ sign_flip : u32x4{0u, 0u, 0u, 0u};
+                qf[x][g] = (SHORT == 0 ? *reinterpret_cast<const u32x4*>(q + ch * 16) : query_chunk<T>(q, ch, CPR, rb)) ^ sign_flip;
             }
         }
         f32x4 oacc[CB][NX];                        // columns 16 i + 4 quarter .. + 3 of rows l16, 16 + l16
@@ -264,7 +264,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     for (int j = 0; j < OFFS; ++j) {
                         const int x = (wave_here + NW * j) * 64 + lane_here, key = x / CPR;
                         const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
-                        lane_off[v][j] = (HALVES ? key & 15 : key) * rb + (SHORT == 0 || ch < rb ? ch : 0);
+                        lane_off[v][j] = (HALVES ? key & 15 : key) * rb + (SHORT == 0 ? ch : chunk_in_row(ch, rb));
                     }
             }
             auto look_up = [&](int t) __attribute__((always_inline)) {   // for the requests from tile t on, 15 tiles at least
@@ -288,7 +288,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     const int x = (wave_here + NW * j) * 64 + lane_here, key = x / CPR;
                     const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
                     const int slot = (wa + tile) * 32 + key - k0;
-                    const char* src = where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 || ch < rb ? ch : 0);   // (behind a row's end: paged_rows.h)
+                    const char* src = where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 ? ch : chunk_in_row(ch, rb));   // (behind a row's end: paged_rows.h)
                     dma16_untracked(src, to);
                 }
             };
@@ -525,7 +525,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     const int x = (wave_here + NW * j) * 64 + lane_here, key = x / CPR;
                     const int ch = (v ? v_chunk(key, x - key * CPR) : (x - key * CPR) ^ L::k_chunk(key)) * 16;
                     const int slot = min(t * KT + key, k1 - 1) - k0;
-                    const char* src = from_where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 || ch < rb ? ch : 0);   // (behind a row's end: paged_rows.h)
+                    const char* src = from_where + places[slot >> grain] + (slot & ((1 << grain) - 1)) * rb + (SHORT == 0 ? ch : chunk_in_row(ch, rb));   // (behind a row's end: paged_rows.h)
                     dma16_untracked(src, to + (wave_here + NW * j) * 1024);
                 };
                 // tiles ta .. tb - 1 one after the other

@@ -94,3 +94,64 @@ def test_a_value_with_a_weight_of_nothing(dtype):
     keep[7] = False
     within(O.cpu()[:, :, keep], want[:, :, keep], off[:, :, keep], "O")
     within(O.cpu()[rows < 70], want[rows < 70], off[rows < 70], "O")
+
+
+def with_infinite_keys(p, slots=(70, 85, 3)):
+    """Keys of some slots are -infinity in their first column, where all queries are positive: scores of -infinity, weights of 0."""
+    for first in range(0, p.Q.shape[1], p.d):
+        p.Q[:, first] = p.Q[:, first].abs() + 0.25
+    for slot in slots:
+        p.K[int(p.table[0, slot // p.page]), :, slot % p.page, 0] = -math.inf
+    return p
+
+
+WIDTHS = {"bf16": (16, 48, 64, 80, 112, 144, 176, 208, 240), "f32": (4, 12, 20, 36, 64, 68, 84, 100, 132, 196, 252)}
+
+
+def test_infinite_keys(dtype):
+    """Whatever the head size, also where a row leaves part of its place on chip empty."""
+    for d in WIDTHS[dtype]:
+        p = with_infinite_keys(Some(dtype, [(40, 100)], 4, 2, d, 16, seed=d))
+        O, lse = p.on_gpu().run_attention()
+        want, want_lse, off, lse_off = p.attention()
+        within(lse.cpu(), want_lse, lse_off, f"lse, d = {d}")
+        within(O.cpu(), want, off, f"O, d = {d}")
+
+
+def test_infinite_keys_in_long_runs(monkeypatch):
+    """(Tiles that all rows see whole: test_gpu_paged_segments.)"""
+    monkeypatch.setenv("ATTNW_PAGED_KERNEL", "tiles")
+    for d in (16, 48, 80, 112, 144):
+        p = with_infinite_keys(Some("bf16", [(300, 4000)], 192, 96, d, 32, seed=d, garbage=False), (70, 1500, 3901))
+        O, lse = p.on_gpu().run_attention()
+        want, want_lse, off, lse_off = p.attention()
+        within(lse.cpu(), want_lse, lse_off, f"lse, d = {d}")
+        within(O.cpu(), want, off, f"O, d = {d}")
+
+
+@pytest.mark.parametrize("new", [1, 300])
+@pytest.mark.parametrize("of", ["bf16", "f32"])
+def test_infinite_keys_of_sums(of, new):
+    """(300 tokens: rows in turns, else held.)"""
+    for d in WIDTHS[of]:
+        p = with_infinite_keys(Some(of, [(new, 400)], 4, 2, d, 16, seed=d)).on_gpu()
+        _, lse, _, _ = p.attention()
+        want, bound = p.collected(lse.float(), None)
+        within(p.run_sums(lse.float().cuda(), None, torch.zeros(want.shape, device="cuda")), want, bound, f"sums, d = {d}")
+
+
+def test_small_queries(dtype):
+    """Queries of all sizes down to the least normal number: what is shared out between two places on chip adds up."""
+    for d in WIDTHS[dtype]:
+        p = Problem(dtype, [(40, 100)], 4, 2, d, 16, seed=d)
+        g = torch.Generator().manual_seed(d)
+        p.Q = p.Q.sign() * torch.exp2(torch.randint(-126, -108, p.Q.shape, generator=g).float()).to(p.Q.dtype) * (1.0 + 0.5 * torch.rand(p.Q.shape, generator=g)).to(p.Q.dtype)
+        p.K = torch.where(torch.isfinite(p.K), p.K * 2.0 ** 110, p.K)
+        p.scale = 2.0 ** -4
+        O, lse = p.on_gpu().run_attention()
+        want, want_lse, off, lse_off = p.attention()
+        assert float((want_lse[:, 0] - want_lse[:, 1]).abs().max()) > 1e-4
+        within(lse.cpu(), want_lse, lse_off, f"lse, d = {d}")
+        within(O.cpu(), want, off, f"O, d = {d}")
+        want, bound = p.collected(lse.cpu(), None)
+        within(p.run_sums(lse, None, torch.zeros(want.shape, device="cuda")), want, bound, f"sums, d = {d}")
