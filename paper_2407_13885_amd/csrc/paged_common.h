@@ -4,7 +4,7 @@
 // read it, so that nothing outside the caller's arrays is touched whatever it holds.
 #pragma once
 
-#include "device_utils.h"
+#include "qk_common.h"
 #include "launchers.h"
 
 namespace attnw {
@@ -78,19 +78,47 @@ constexpr int32_t kNoWindow = 1 << 30;            // (as many slots as a sequenc
 enum : int { kPlain = 0, kCap = 1, kBias = 2 };
 inline int rule_mode(const RuleView& r) { return (r.cap > 0.0f ? kCap : kPlain) | (r.slopes ? kBias : kPlain); }
 
-// A score as exponent of 2: scale (or cap) and log2(e) in it.  EXACT: tanh to fp32's last bits instead of by way of 2^x (off by 2^-23).
+// Scores as exponents of 2, of some dot products at once: scale (or cap) and log2(e) in them.
+// The cap: c tanh(t), t = scale dot / cap, in fp32 (EXACT) by tanhf, else c - 2 c / (2^(2 log2(e) t) + 1), off by 2^-22 c: two transcendental instructions and three
+// others.  That is 2^-15 of an exponent at most up to a cap of 128; where caps are larger, t below a quarter goes by its series (the next term is 2^-27 of the first),
+// and the error is 2^-20 of the score.  (Not for all: a chunk of 2048 tokens over 14336 slots 640 us, with the series 1122.)  In fp32 the series is for caps where
+// scale / cap might no longer be a normal number.
 template <bool CAPPED, bool EXACT> struct ScoreMap {
-    float c, inner;                               // dot -> c dot, or c tanh(inner dot)
+    float c, inner, plain, ratio;                 // plain: scale; ratio: dot -> t; inner: as large() takes it
+    bool series;
     __device__ __forceinline__ explicit ScoreMap(const RuleView& r)
     {
-        c = (CAPPED ? r.cap : r.scale) * kLog2e;
-        inner = !CAPPED ? 0.0f : EXACT ? r.scale / r.cap : r.scale / r.cap * (2.0f * kLog2e);
+        const auto finite = [](float x) __attribute__((always_inline)) { return fmaxf(-3.4e38f, fminf(x, 3.4e38f)); };
+        plain = r.scale * kLog2e;
+        c = CAPPED ? finite(r.cap * kLog2e) : plain;
+        ratio = CAPPED ? finite(r.scale / r.cap) : 0.0f;
+        inner = EXACT ? ratio : finite(ratio * (2.0f * kLog2e));
+        series = r.cap > (EXACT ? 0x1p100f : 128.0f);
     }
-    __device__ __forceinline__ float operator()(float dot) const
+    __device__ __forceinline__ float large(float dot) const
     {
         if constexpr (!CAPPED) return dot * c;
         else if constexpr (EXACT) return c * tanhf(dot * inner);
         else return __builtin_fmaf(-2.0f * c, __builtin_amdgcn_rcpf(fast_exp2(dot * inner) + 1.0f), c);
+    }
+    __device__ __forceinline__ float any(float dot) const
+    {
+        const float t = dot * ratio, u = t * t;
+        const float p = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f);
+        const float x = dot * plain;
+        return fabsf(t) < 0.25f ? __builtin_fmaf(x * u, p, x) : large(dot);
+    }
+    template <int N> __device__ __forceinline__ void operator()(float (&x)[N]) const
+    {
+        if constexpr (CAPPED) {
+            if (apart_uniform(series) != 0) {     // (where it stands: not two of every loop around it)
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = any(x[i]);
+                return;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = large(x[i]);
     }
 };
 

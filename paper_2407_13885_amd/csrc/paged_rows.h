@@ -144,8 +144,7 @@ void paged_rows_kernel(AttendArgs a, int grain)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) x[4 * k + r] = acc[r];
                     }
-#pragma unroll
-                    for (int i = 0; i < NK * 4; ++i) x[i] = map(x[i]);
+                    map(x);
                     const int key = key0 + 4 * quarter;        // + 16 k + r
                     if constexpr ((MODE & kBias) != 0) {
 #pragma unroll

@@ -115,14 +115,15 @@ __device__ __forceinline__ void add_weights(f32x4 (&sum)[NK], const SumsKernelAr
     // (tokens of the rows: first .. last)
     const int first = __builtin_amdgcn_readlane(x.query, 0), last = __builtin_amdgcn_readlane(x.query, 15);
     const bool whole = mine + 16 * NK <= seq.length && ((mine + 16 * NK - 1 <= first && mine > last - a.rule.window) || mine + 16 * NK <= prefix);
+    float y[4 * NK];
 #pragma unroll
-    for (int k = 0; k < NK; ++k)
+    for (int i = 0; i < 4 * NK; ++i) y[i] = acc[i / 4][i % 4];
+    map(y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float y = map(acc[k][e]);
-            if constexpr ((MODE & kBias) != 0) y -= x.slope * (float)abs(x.query - (mine + 16 * k + 4 * quarter + e));
-            acc[k][e] = fast_exp2(y - lse);
-        }
+    for (int i = 0; i < 4 * NK; ++i) {
+        if constexpr ((MODE & kBias) != 0) y[i] -= x.slope * (float)abs(x.query - (mine + 16 * (i / 4) + 4 * quarter + i % 4));
+        acc[i / 4][i % 4] = fast_exp2(y[i] - lse);
+    }
     if (!whole) {
         const Sight sight(x.query, a.rule, prefix, seq.length);
 #pragma unroll

@@ -169,13 +169,14 @@ void paged_tiles_kernel(AttendArgs a, int grain)
             }
             const int key = key0 + 4 * quarter;
 #pragma unroll
-            for (int x = 0; x < NX; ++x)
+            for (int x = 0; x < NX; ++x) {
+                if constexpr (MODE != kPlain) map(y[x]);
 #pragma unroll
                 for (int i = 0; i < 4 * NK; ++i) {
-                    if constexpr (MODE != kPlain) y[x][i] = map(y[x][i]);
-                    else y[x][i] *= c;
+                    if constexpr (MODE == kPlain) y[x][i] *= c;
                     if constexpr ((MODE & kBias) != 0) y[x][i] -= slope[x] * (float)abs(query[x] - (key + 16 * (i / 4) + i % 4));
                 }
+            }
             const bool whole = key0 + KT <= past && ((key0 + KT - 1 <= first && key0 > last - a.rule.window) || key0 + KT <= prefix);
             if (!whole) {
 #pragma unroll
@@ -336,7 +337,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     for (int x = 0; x < 2; ++x)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            float y = map(r.s[i / 4][x][i % 4]);
+                            float y = map.large(r.s[i / 4][x][i % 4]);
                             if constexpr ((MODE & kBias) != 0) y -= slope[x] * (float)abs(query[x] - (key + 16 * (i / 4) + i % 4));
                             r.s[i / 4][x][i % 4] = y;
                         }
@@ -565,12 +566,13 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                         if (active) tile_alone(i & (RING - 1), (ta + i) * KT, k1);
                     }
                 };
-                // Tiles that all rows of the block see whole go through run_piped, those before and behind them, with masks, one by one.
+                // Tiles that all rows of the block see whole go through run_piped, those before and behind them, with masks, one by one.  (So do all of a call whose cap is so
+                // large that scores go by a series: it would take the registers that run_piped has none of to spare.)
                 int f0 = k0 / KT, f1 = (k1 + KT - 1) / KT, w0 = f1, w1 = f1;
                 if constexpr (C::PIPE) {
                     if (near) w0 = max(f0, (max(0, last - a.rule.window + 1) + 31) / 32), w1 = min(k1, max(0, first + 1)) / 32;
                     else w0 = f0, w1 = min(k1, prefix) / 32;
-                    if (w1 - w0 < 6) w0 = w1 = f1;
+                    if (w1 - w0 < 6 || map.series) w0 = w1 = f1;
                 }
 #pragma clang loop unroll(disable)
                 for (int side = 0; side < 2; ++side) {

@@ -155,3 +155,47 @@ def test_small_queries(dtype):
         within(O.cpu(), want, off, f"O, d = {d}")
         want, bound = p.collected(lse.cpu(), None)
         within(p.run_sums(lse, None, torch.zeros(want.shape, device="cuda")), want, bound, f"sums, d = {d}")
+
+
+# ---- caps ---------------------------------------------------------------------------------------------------------------------------------
+
+class Capped(Problem):
+    """The same, with what fp32 may be off by in terms of the score, not of the cap."""
+
+    def scores(self, b, h):
+        cap, self.cap = self.cap, 0.0
+        x, off = super().scores(b, h)
+        self.cap = cap
+        seen = self.seen(b)
+        y = cap * torch.tanh(torch.where(seen, x, 0.0) / cap)
+        # 1 - 2 / (2^z + 1) is off by 2^-22 (a unit in the last place each of exponential and reciprocal, half of one of the sum and of z): 2^-20 of tanh from a quarter
+        # on, and with the roundings of what it is multiplied by 2^-19; below a quarter, and by tanhf, less.  Caps up to 128 may be made so everywhere.
+        own = 2.0 ** -19 * y.abs() if cap > 128.0 else torch.full_like(y, cap * 2.0 ** -22)
+        return y.masked_fill(~seen, -math.inf), off + own + 8 * 2.0 ** -24 * y.abs()
+
+
+@pytest.mark.parametrize("cap", [1e-40, 1e-3, 30.0, 128.0, 129.0, 1000.0, 1e5, 1e30, 3e38])
+@pytest.mark.parametrize("sharp", [1.0, 40.0])
+def test_caps(dtype, cap, sharp):
+    """However large the cap: scores are as exact as their own size lets them be."""
+    p = Capped(dtype, [(40, 300)], 4, 2, 64, 16, cap=cap, sharp=sharp)
+    O, lse = p.on_gpu().run_attention()
+    want, want_lse, off, lse_off = p.attention()
+    within(lse.cpu(), want_lse, lse_off, "lse")
+    within(O.cpu(), want, off, "O")
+    for new in (40, 150):                         # (held rows, rows in turn)
+        p = Capped(dtype, [(new, 300)], 4, 2, 64, 16, cap=cap, sharp=sharp).on_gpu()
+        _, lse, _, _ = p.attention()
+        want, bound = p.collected(lse.float(), None)
+        within(p.run_sums(lse.float().cuda(), None, torch.zeros(want.shape, device="cuda")), want, bound, f"sums of {new}")
+
+
+@pytest.mark.parametrize("cap", [128.0, 200.0])
+def test_caps_in_long_runs(monkeypatch, cap):
+    """(Workgroups with two places of 128 keys and more: the order in which tiles that all rows see go up to a cap of 128.)"""
+    monkeypatch.setenv("ATTNW_PAGED_KERNEL", "tiles")
+    p = Capped("bf16", [(300, 2500)], 24, 24, 128, 32, cap=cap, sharp=20.0)
+    O, lse = p.on_gpu().run_attention()
+    want, want_lse, off, lse_off = p.attention()
+    within(lse.cpu(), want_lse, lse_off, "lse")
+    within(O.cpu(), want, off, "O")
