@@ -35,7 +35,7 @@ struct Units {
 template <typename T, int V, bool INTERLEAVED, bool CACHE>
 __global__ __launch_bounds__(256)
 void rotary_kernel(const T* Q, const T* K, const T* Vn, T* R, T* Kc, T* Vc, const float* __restrict__ angles, const int32_t* __restrict__ positions,
-                   const int32_t* __restrict__ starts, int32_t tokens, int32_t d, int32_t rot, int32_t rows, int64_t q_stride, int64_t kv_stride,
+                   const int32_t* __restrict__ starts, int32_t tokens, int32_t d, int32_t rot, int64_t rows, int64_t q_stride, int64_t kv_stride,
                    int64_t r_stride, float sign, CacheView cache, Units u)
 {
     typedef Chunk<T, V> C;
@@ -160,7 +160,7 @@ hipError_t launch(const RotaryArgs& a, hipStream_t stream)
     auto go = [&](auto kernel) {
         kernel<<<dim3(blocks, across), 256, 0, stream>>>(static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), static_cast<T*>(a.R),
                                                        static_cast<T*>(a.Kc), static_cast<T*>(a.Vc), a.angles, a.positions, a.starts, (int32_t)a.tokens,
-                                                       (int32_t)a.d, (int32_t)a.rot, (int32_t)a.rows, a.q_stride, a.kv_stride, a.r_stride, sign, a.cache, u);
+                                                       (int32_t)a.d, (int32_t)a.rot, a.rows, a.q_stride, a.kv_stride, a.r_stride, sign, a.cache, u);
         return hipGetLastError();
     };
     if (with_cache) return go(rotary_kernel<T, V, INTERLEAVED, true>);

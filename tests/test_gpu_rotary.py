@@ -191,3 +191,31 @@ def test_append_of_what_has_no_place():
     torch.cuda.synchronize()
     before[int(p.table[1, 0]), 0, 0] = x[4, 64:96]   # the second sequence's one slot
     assert torch.equal(p.dev["K"], before) and torch.equal(R.view(5, 64), x[:, :64])
+
+
+def test_a_table_of_2_to_the_31_rows():
+    """More rows than 31 bits count: positions of any size find theirs."""
+    rows, heads, d = (1 << 31) + 5, 2, 16
+    table = torch.empty((rows, 2), device="cuda")              # (16 GiB, of which a few rows are looked at)
+    at = torch.tensor([0, 1, 12345, (1 << 30) + 7, (1 << 31) - 1], dtype=torch.int64, device="cuda")
+    angle = torch.tensor([0.0, 0.5, 1.0, 2.0, 3.0], dtype=torch.float64)
+    table[at] = torch.stack([angle.cos(), angle.sin()], 1).float().cuda()
+    positions = at.to(torch.int32)
+    x = torch.randn((5, heads, d), device="cuda")
+    y = torch.empty_like(x)
+    attnw.attnw_rotary(x, y, table, positions, 5, heads, d, 2, rows, heads * d, heads * d, attnw.ATTNW_HALVES, 0, attnw.ATTNW_F32)
+    X = x.double().cpu()
+    c, s = angle.cos()[:, None], angle.sin()[:, None]
+    want = X.clone()
+    want[..., 0], want[..., 1] = X[..., 0] * c - X[..., 1] * s, X[..., 1] * c + X[..., 0] * s
+    # (cos and sin to half a unit in the last place, two products and a sum)
+    bound = 4 * 2.0 ** -24 * (X[..., :2].abs().sum(-1, keepdim=True) + X.abs())
+    within(y, want, bound, "y")
+    starts = torch.tensor([0, 5], dtype=torch.int32, device="cuda")
+    K, V = (torch.zeros((1, heads, 16, d), device="cuda") for _ in range(2))
+    pages, lengths = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.tensor([5], dtype=torch.int32, device="cuda")
+    cache = attnw.AttnwCache(K, V, pages, lengths, 1, 1, 1, 16, heads, d, attnw.ATTNW_F32)
+    R = torch.empty_like(x)
+    attnw.attnw_cache_append(cache, x, x, x, R, table, positions, starts, 5, heads, 2, rows, heads * d, heads * d, attnw.ATTNW_HALVES)
+    within(R, want, bound, "R")
+    within(K[0, :, :5].transpose(0, 1), want, bound, "K")
