@@ -195,12 +195,11 @@ int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, c
         !aligned(positions, 4) || !aligned(starts, 4))
         return ATTNW_ERR_ALIGN;
     const int64_t kv_bytes = extent(tokens, kv_stride, kv_wide, size), all = cache_bytes(cache);
-    const void* const inputs[] = {K, V, table, positions, starts};
-    const int64_t lengths[] = {kv_bytes, kv_bytes, rows * rot * 4, tokens * 4, (cache->batch + 1) * 4};
-    for (int i = 0; i < 5; ++i) {
-        if (!inputs[i]) continue;
-        if (overlaps(cache->K, all, inputs[i], lengths[i]) || overlaps(cache->V, all, inputs[i], lengths[i])) return ATTNW_ERR_ALIAS;
-    }
+    struct Range { const void* at; int64_t bytes; };
+    const Range read[] = {{K, kv_bytes}, {V, kv_bytes}, {table, rows * rot * 4}, {positions, tokens * 4}, {starts, (cache->batch + 1) * 4},
+                          {cache->table, cache->batch * cache->max_pages * 4}, {cache->lengths, cache->batch * 4}};
+    for (const Range& r : read)
+        if (r.at && (overlaps(cache->K, all, r.at, r.bytes) || overlaps(cache->V, all, r.at, r.bytes))) return ATTNW_ERR_ALIAS;
     if (overlaps(cache->K, all, cache->V, all)) return ATTNW_ERR_ALIAS;
     if (heads > 0) {
         const int64_t q_bytes = extent(tokens, q_stride, wide, size), r_bytes = tokens * wide * size;
@@ -208,8 +207,8 @@ int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, c
         if (overlaps(cache->K, all, Q, q_bytes) || overlaps(cache->V, all, Q, q_bytes) || overlaps(cache->K, all, R, r_bytes) ||
             overlaps(cache->V, all, R, r_bytes))
             return ATTNW_ERR_ALIAS;
-        for (int i = 0; i < 5; ++i)
-            if (inputs[i] && overlaps(R, r_bytes, inputs[i], lengths[i])) return ATTNW_ERR_ALIAS;
+        for (const Range& r : read)
+            if (r.at && overlaps(R, r_bytes, r.at, r.bytes)) return ATTNW_ERR_ALIAS;
     }
     attnw::RotaryArgs a{};
     a.dt = static_cast<DType>(cache->dtype);
@@ -321,6 +320,7 @@ int attnw_paged_sums(const attnw_cache* cache, const attnw_rule* rule, const voi
         return ATTNW_ERR_ALIGN;
     struct Range { const void* at; int64_t bytes; };
     const Range read[] = {{tokens > 0 ? Q : nullptr, extent(tokens, q_stride, heads * cache->d, size_of(cache->dtype))}, {cache->K, cache_bytes(cache)},
+                          {cache->V, cache_bytes(cache)},          // (not read here, but the cache's)
                           {cache->table, cache->batch * cache->max_pages * 4}, {cache->lengths, cache->batch * 4}, {starts, (cache->batch + 1) * 4},
                           {rule->slopes, heads * 4}, {rule->prefix, cache->batch * 4}, {tokens > 0 ? lse : nullptr, tokens * heads * 4},
                           {before == sums ? nullptr : before, elems}};

@@ -205,3 +205,16 @@ def test_structures_are_told_apart():
                 for call in (f, f.__wrapped__):
                     with pytest.raises(TypeError, match="expected, not"):
                         call(*args)
+
+
+def test_nothing_is_written_over_what_is_read():
+    """Appending over the cache's own table and lengths, sums over its values."""
+    def append(c=None, r=O):
+        return status("attnw_cache_append", c or cache(), Q, Q + 0x1000, Q + 0x2000, r, WORK, None, STARTS, 3, 4, 64, 10, 256, 128, 0)
+
+    def sums(out, **more):
+        return status("attnw_paged_sums", cache(**more), binding.AttnwRule(0.125), Q, LSE, None, out, STARTS, 3, 4, 256)
+    assert append(r=TABLE) == E_ALIAS and append(r=LENGTHS) == E_ALIAS
+    for more in (dict(K=TABLE), dict(K=LENGTHS), dict(V=TABLE), dict(V=LENGTHS), dict(table=V + 64), dict(lengths=K + 1024)):
+        assert append(cache(**more)) == E_ALIAS, more
+    assert sums(V) == E_ALIAS and sums(V + 4096) == E_ALIAS
