@@ -131,6 +131,13 @@ __device__ __forceinline__ void add_weights(f32x4 (&sum)[NK], const SumsKernelAr
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[k][e] = sight.hidden(mine + 16 * k + 4 * quarter + e) < 0 ? 0.0f : acc[k][e];
     }
+    const bool nothing = x.lse == -__builtin_inff();
+    if (__builtin_amdgcn_ballot_w64(nothing) != 0) {           // (whatever its scores are: NaN is not 0 by now)
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[k][e] = nothing ? 0.0f : acc[k][e];
+    }
 #pragma unroll
     for (int k = 0; k < NK; ++k) sum[k] += acc[k];
 }

@@ -199,3 +199,20 @@ def test_caps_in_long_runs(monkeypatch, cap):
     want, want_lse, off, lse_off = p.attention()
     within(lse.cpu(), want_lse, lse_off, "lse")
     within(O.cpu(), want, off, "O")
+
+
+@pytest.mark.parametrize("of", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [3, 20, 300])
+def test_sums_of_rows_that_do_not_count(of, new):
+    """Rows whose lse is -infinity add nothing, whatever their queries are: padding may hold anything."""
+    for d in (64, 80):
+        p = Problem(of, [(new, 400)], 4, 2, d, 16, seed=d)
+        _, lse, _, _ = p.attention()
+        lse = lse.float()
+        for t, h, kind in ((0, 0, math.nan), (new - 1, 3, math.inf), (new // 2, 1, -math.inf), (new - 1, 2, math.nan)):
+            p.Q[t, h * d:(h + 1) * d] = kind
+            lse[t, h] = -math.inf
+        clean = Problem(of, [(new, 400)], 4, 2, d, 16, seed=d)
+        want, bound = clean.collected(lse, None)
+        p.on_gpu()
+        within(p.run_sums(lse.cuda(), None, torch.zeros(want.shape, device="cuda")), want, bound, f"sums, d = {d}")
