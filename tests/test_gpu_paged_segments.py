@@ -201,3 +201,22 @@ def test_sums_of_many_blocks(dtype, d, page, more, new):
     within(p.run_sums(lse.float().cuda(), None, sums), want, bound, "sums")
     O, got_lse = p.run_attention()
     assert TORCH_DT[dtype] == O.dtype
+
+
+# ---- which kernel -------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,tokens,heads,kv_heads,d,want", [
+    ("bf16", 64, 32, 8, 256, "tiles"),            # measured at 4096 and 16384 slots, us, small blocks / large ones: 96 / 64, 334 / 108
+    ("bf16", 128, 4, 1, 256, "rows"),             # 37 / 55, 98 / 94
+    ("bf16", 64, 64, 16, 64, "rows"),             # 22 / 56, 63 / 70
+    ("bf16", 256, 32, 8, 64, "tiles"),            # 39 / 39, 118 / 66
+    ("f32", 32, 64, 16, 64, "rows"),              # 36 / 54, 112 / 126
+    ("f32", 64, 16, 4, 256, "tiles"),             # 135 / 86, 478 / 244
+    ("bf16", 1, 32, 8, 128, "rows"),
+])
+def test_the_kernel_that_sizes_lead_to(dtype, tokens, heads, kv_heads, d, want):
+    p = Problem(dtype, [(tokens, 4096)], heads, kv_heads, d, 64, garbage=False).on_gpu()
+    work = torch.empty(attnw.attnw_paged_workspace(p.cache, tokens, heads), dtype=torch.uint8, device="cuda")
+    O, dev = torch.empty((tokens, heads, d), dtype=TORCH_DT[dtype], device="cuda"), p.dev
+    ran = kernels(lambda s: attnw.attnw_paged_attention(p.cache, p.rule, dev["Q"], O, None, dev["starts"], tokens, heads, p.q_stride, work, work.numel(), s))
+    assert f"paged_{want}_kernel" in ran[0]
