@@ -220,3 +220,41 @@ def test_the_kernel_that_sizes_lead_to(dtype, tokens, heads, kv_heads, d, want):
     O, dev = torch.empty((tokens, heads, d), dtype=TORCH_DT[dtype], device="cuda"), p.dev
     ran = kernels(lambda s: attnw.attnw_paged_attention(p.cache, p.rule, dev["Q"], O, None, dev["starts"], tokens, heads, p.q_stride, work, work.numel(), s))
     assert f"paged_{want}_kernel" in ran[0]
+
+
+# ---- scales, and batches of more sequences than a wave has lanes ------------------------------------------------------------------------------
+
+class Scaled(OnDevice):
+    """A scale of either sign: what fp32 may be off by goes with its size."""
+
+    def scores(self, b, h):
+        scale, self.scale = self.scale, abs(self.scale)
+        off = super().scores(b, h)[1]
+        self.scale = scale
+        x, own = super().scores(b, h)
+        return x, torch.maximum(off, own.abs())
+
+
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+@pytest.mark.parametrize("scale", [0.0, -0.125, 1e-30, 2.0])
+def test_scales(kernel, scale, cap):
+    p = Scaled("bf16", [(300, 2500), (3, 70)], 24, 24, 64, 32, seed=4, cap=cap)
+    p.scale = scale
+    O, lse = check_attention(p)
+    before = torch.rand((2, 24, p.max_pages * 32))
+    want, bound = p.collected(lse, before.cuda())
+    sums = p.run_sums(lse, before.cuda(), torch.zeros(want.shape, device="cuda"))
+    for b, (_, m) in enumerate(p.sequences):
+        within(sums[b, :, :m], want[b, :, :m], bound[b, :, :m], "sums")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,most", [(1, 2000), (3, 500), (90, 700)])
+def test_many_sequences_of_either_kernel(kernel, dtype, new, most):
+    sequences = [((i * 7) % (new + 1), max((i * 7) % (new + 1), (i * 37) % most + 2)) for i in range(150)]
+    p = OnDevice(dtype, sequences, 4, 2, 32, 16, seed=new)
+    O, lse = check_attention(p)
+    want, bound = p.collected(lse, None)
+    sums = p.run_sums(lse, None, torch.zeros(want.shape, device="cuda"))
+    for b, (_, m) in enumerate(p.sequences):
+        within(sums[b, :, :m], want[b, :, :m], bound[b, :, :m], "sums")
