@@ -371,9 +371,10 @@ template <typename T, int UB, int MODE> hipError_t launch(const SumsArgs& p, hip
     a.cache = p.cache;
     a.rule = p.rule;
     // (workgroups of unequal work in several rounds: those that end early make room)
-    // Rows of a sequence, on average.  Held / in turns, us: bf16, 8 sequences of 4096 slots, 4 kv heads of 128: 128 rows 27 / 40, 256 42 / 45, 384 57 / 52, 1024
-    // 136 / 90; 64 of them 164 / 239, 283 / 298, 451 / 351, 1236 / 636.  fp32, 4 of them: 128 rows 65 / 54, 256 117 / 73; d = 64, a cap: 96 rows 41 / 54, 192 73 / 66.
-    const bool turns = p.tokens * (int64_t)a.group.d > (sizeof(T) == 2 ? 256 : 96) * (int64_t)p.cache.batch;
+    // Rows of a sequence, on average.  Held / in turns, us: bf16, 8 sequences of 4096 slots, 4 kv heads of 128: 128 rows 30 / 40, 256 47 / 44, 384 63 / 51, 1024
+    // 151 / 88; 64 of them 183 / 238, 333 / 294, 530 / 350, 1433 / 630; d = 64 256 rows 22 / 26, 384 29 / 30.  fp32, 4 of them: 96 rows 38 / 51, 128 47 / 52, 256 84 / 70; d = 64, a
+    // cap: 128 rows 25 / 30, 192 33 / 34; d = 100 128 rows 44 / 43.
+    const bool turns = p.tokens * (int64_t)a.group.d > (sizeof(T) == 2 ? 256 : 128) * (int64_t)p.cache.batch;
     const uint32_t grid = (uint32_t)((compute_units() * (turns ? 16 : StepCfg<T, UB>::PER_CU) + 7) & ~7);
     const int grain = key_grain(a.cache);
     constexpr bool OWN = UB > 1;                  // rows that fill their place: kernels of their own
