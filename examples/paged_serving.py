@@ -1,5 +1,6 @@
 """An attention layer that serves from a paged cache: prompts of uneven length go in by chunks, tokens follow one by one (recorded once, replayed),
-and sequences that outgrow their budget give up the slots that collected the least weight.
+and sequences that outgrow their budget give up the slots that collected the least weight.  (Windows and slopes count slots: after that they are no
+longer distances of positions, which the rotation keeps.)
 
     python examples/paged_serving.py
 

@@ -268,7 +268,9 @@ typedef struct attnw_cache {
  * window > 0; and every slot below prefix[b] in any case.  Other slots have no part in
  * the result, whatever K and V hold there (NaN included).  What is infinite or NaN in slots that are seen has the part that
  * IEEE arithmetic gives it: an infinite value makes its column infinite, or NaN where both signs meet or its weight
- * is 0 in fp32; a score of -infinity is a weight of 0.  Distances are counted in slots.
+ * is 0 in fp32; a score of -infinity is a weight of 0.  A bf16 cap is exact to cap 2^-22 up to a cap of 128, beyond and in fp32 to 2^-20
+ * of the score.  Distances (window and slopes) are counted in slots: once slots have been given up, and other ones by each kv
+ * head, they are no longer distances of positions.
  */
 typedef struct attnw_rule {
     float scale, cap;
@@ -338,7 +340,7 @@ int64_t attnw_paged_workspace(const attnw_cache *cache, int64_t tokens, int64_t 
  * workspace: at least attnw_paged_workspace bytes, 16-byte aligned, of any content; calls that
  * may run at the same time need one each.  Two launches at most.
  * (ATTNW_PAGED_KERNEL=rows / =tiles in the environment, read at every call of this function and of the one
- * before it, puts all bf16 calls on the kernel for few / for many rows; unset, the sizes decide.)
+ * before it, puts all calls on the kernel for few / for many rows; unset, the sizes decide.)
  */
 int attnw_paged_attention(const attnw_cache *cache, const attnw_rule *rule, const void *Q,
                           void *O, float *lse, const int32_t *starts, int64_t tokens,

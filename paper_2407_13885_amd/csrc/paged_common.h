@@ -161,7 +161,8 @@ template <typename T> __device__ __forceinline__ u32x4 without_lost(const u32x4&
 // four), which adds up to the same.
 // Where the chunk at byte `at` of a place comes from, rows being rb bytes, which are half a place at least but for that one:
 __device__ __forceinline__ int chunk_in_row(int at, int rb) { return at < rb ? at : min(at - rb, rb - 16); }
-// Numbers times 2^-halvings: exact, as those below 2^-118, where it might not be, are whole in their first place and 0 in the others.  Infinities and NaN as they are.
+// Numbers times 2^-halvings: exact, as those below 2^-118, where it might not be, are whole in their first place and 0 in the others (an infinite key makes NaN
+// of those).  Infinities and NaN as they are.
 template <typename T> __device__ __forceinline__ uint32_t shared_out(uint32_t w, int halvings, bool first)
 {
     // (flags in the signs' places: an exponent field of 9 or more)
