@@ -258,11 +258,11 @@ def _handles(state):
                                         int(state["fresh"]))
     if state["call"] == "axes":
         return
-    state["cache"] = attnw.AttnwCache8(state["K"], state["V"], state["K_scales"], state["V_scales"], state["table"], state["lengths"], state["batch"],
+    state["cache"] = attnw.AttnwByteCache(state["K"], state["V"], state["K_scales"], state["V_scales"], state["table"], state["lengths"], state["batch"],
                                        state["pages"], state["most"], state["page"], state["block"], state["kv_heads"], state["d"], state["code"])
     if state["call"] == "attention":
         state["rule"] = attnw.AttnwRule(state["d"] ** -0.5, state["cap"], state["slope"], state["first"], state["window"])
-        state["bytes"] = attnw.attnw_paged8_workspace(state["cache"], state["T"], state["heads"])
+        state["bytes"] = attnw.attnw_byte_paged_workspace(state["cache"], state["T"], state["heads"])
         state["workspace"] = torch.empty(max(1, state["bytes"]), dtype=torch.uint8, device="cuda")
 
 
@@ -289,10 +289,10 @@ def _own(s):
                                 s["heads"] * s["d"], layout, int(s["inverse"]), s["code"], stream)
     elif s["call"] == "append":
         x, wide = s["projected"], s["heads"] * s["d"]
-        attnw.attnw_cache8_append(s["cache"], x, x[:, wide:], x[:, wide + s["kv_heads"] * s["d"]:], s["R"], s["angles"], s["positions"], s.get("axes"),
+        attnw.attnw_byte_cache_append(s["cache"], x, x[:, wide:], x[:, wide + s["kv_heads"] * s["d"]:], s["R"], s["angles"], s["positions"], s.get("axes"),
                                   s["starts"], s["T"], s["heads"], s["rot"], _TABLE_ROWS, _row(s), _row(s), layout, stream)
     else:
-        attnw.attnw_paged8_attention(s["cache"], s["rule"], s["Q"], s["O"], s["lse"], s["starts"], s["T"], s["heads"], s["heads"] * s["d"],
+        attnw.attnw_byte_paged_attention(s["cache"], s["rule"], s["Q"], s["O"], s["lse"], s["starts"], s["T"], s["heads"], s["heads"] * s["d"],
                                      s["workspace"], s["bytes"], stream)
     return _outputs(s)
 
