@@ -375,6 +375,79 @@ int attnw_cache_evict(const attnw_cache *cache, const attnw_cache *into,
                       const float *sums, float *into_sums, int32_t *kept, int64_t keep,
                       int64_t recent, void *stream);
 
+/*
+ * Rotary positions with several axes: tokens of images and video stand at a time, a height and a width, say, and each
+ * pair of columns turns by the position that its token has on one of up to 4 axes.  Of the rot / 2 pairs axis a has
+ * pairs[a], one at least: all that follow those of the axis before (ATTNW_SECTIONS), or the axes take one each in turns, those that have all
+ * of theirs passed over (ATTNW_TURNS: t h w t h w .. t t).  The description is read during the call and not kept.
+ */
+typedef enum {
+    ATTNW_SECTIONS = 0,
+    ATTNW_TURNS = 1
+} attnw_order;
+typedef struct attnw_axes {
+    int32_t count;              /* 1 .. 4 */
+    int32_t order;              /* attnw_order */
+    int32_t fresh;              /* attnw_rotary_axes_table: frequencies begin again with each axis */
+    int32_t pairs[4];           /* of each axis; together rot / 2 */
+} attnw_axes;
+
+/*
+ * The table of such a rotation, [positions][rot] as attnw_rotary_table makes it, all axes sharing its rows.  fresh == 0: the same table (pair j turns by
+ * base^(-2 j / rot) whatever its axis); else the i-th pair of an axis of n turns by base^(-i / n).
+ */
+int attnw_rotary_axes_table(float *table, const attnw_axes *axes, int64_t positions, int64_t rot, double base,
+                            double factor, double low, double high, double original,
+                            double gain, void *stream);
+
+/*
+ * attnw_rotary with several axes: pair j of token t turns by the angle at column j of row positions[axis of j][t] of the table; positions:
+ * [axes][tokens].  Everything else as there (in place, part of a head, inverse: the gradient); where the table does not have the row, that axis'
+ * columns come out as NaN.  (Keys and values turned so go into a cache by attnw_cache_append with rot = 0.)
+ */
+int attnw_rotary_axes(const void *X, void *Y, const float *table, const int32_t *positions,
+                      const attnw_axes *axes, int64_t tokens, int64_t heads, int64_t d,
+                      int64_t rot, int64_t rows, int64_t x_stride, int64_t y_stride,
+                      int layout, int inverse, int dtype, void *stream);
+
+/*
+ * A paged cache in 8 bits: K and V of `cache` hold a byte an element, an e4m3 number (4 bits of exponent, 3 of mantissa, up to
+ * 448, no infinities), which stands for itself times 2^(s - 127), s the byte that `block` slots of a page share for a kv head: slot
+ * row r of a page has K_scales[page][kv_head][r / block] (254 at most counts).  block divides page_size.
+ * d: a multiple of 16.  `dtype` is the type of queries, new tokens and outputs.
+ */
+typedef struct attnw_byte_cache {
+    attnw_cache cache;          /* K, V: [pages][kv_heads][page_size][d] of bytes */
+    uint8_t *K_scales, *V_scales;   /* [pages][kv_heads][page_size / block] */
+    int64_t block;
+} attnw_byte_cache;
+
+/*
+ * attnw_cache_append to a cache in 8 bits.  axes NULL: one position a token, as there (positions NULL: its slot); else positions are [axes][tokens].
+ * Keys are turned in fp32 (three roundings: x c, y s and their difference), and with the values rounded once, to the nearest
+ * number that the cache holds.  A block's scale is the least 2^e, e from -117 to 119, with |x| <= 448 2^e for all its new rows, and not less than the one it
+ * had where it had rows before the new ones; where that grows, those are rounded again in place (times a power of 2: what stays above 2^-6 of the scale keeps
+ * its value).  NaN and infinities become NaN and do not count for the scale; beyond 448 2^119 numbers become that.
+ */
+int attnw_byte_cache_append(const attnw_byte_cache *cache, const void *Q, const void *K,
+                        const void *V, void *R, const float *table,
+                        const int32_t *positions, const attnw_axes *axes,
+                        const int32_t *starts, int64_t tokens, int64_t heads, int64_t rot,
+                        int64_t rows, int64_t q_stride, int64_t kv_stride, int layout,
+                        void *stream);
+
+/* attnw_paged_workspace of a cache in 8 bits. */
+int64_t attnw_byte_paged_workspace(const attnw_byte_cache *cache, int64_t tokens, int64_t heads);
+
+/*
+ * attnw_paged_attention over a cache in 8 bits, by the same rule, with the values that its elements stand for (bf16 holds them exactly: nothing of the cache is rounded
+ * again).  bf16: as there.  fp32: queries and weights in three bf16 parts, which hold 24 bits (those above 2^-126), fp32 sums.
+ */
+int attnw_byte_paged_attention(const attnw_byte_cache *cache, const attnw_rule *rule, const void *Q,
+                           void *O, float *lse, const int32_t *starts, int64_t tokens,
+                           int64_t heads, int64_t q_stride, void *workspace,
+                           int64_t workspace_bytes, void *stream);
+
 /* Human-readable name of a status code; never NULL. */
 const char *attnw_status_string(int status);
 

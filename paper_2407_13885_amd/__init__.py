@@ -10,18 +10,27 @@ from .binding import (  # noqa: F401
     ATTNW_F32,
     ATTNW_HALVES,
     ATTNW_PAIRS,
+    ATTNW_SECTIONS,
+    ATTNW_TURNS,
+    AttnwAxes,
     AttnwCache,
+    AttnwByteCache,
     AttnwError,
     AttnwRule,
     attnw_attention,
+    attnw_byte_cache_append,
     attnw_cache_append,
     attnw_cache_evict,
     attnw_fused,
     attnw_gemm_scores,
+    attnw_byte_paged_attention,
+    attnw_byte_paged_workspace,
     attnw_paged_attention,
     attnw_paged_sums,
     attnw_paged_workspace,
     attnw_rotary,
+    attnw_rotary_axes,
+    attnw_rotary_axes_table,
     attnw_rotary_table,
     attnw_scale,
     attnw_softmax,

@@ -28,6 +28,8 @@ ATTNW_F32 = 0
 ATTNW_BF16 = 1
 ATTNW_HALVES = 0
 ATTNW_PAIRS = 1
+ATTNW_SECTIONS = 0
+ATTNW_TURNS = 1
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
@@ -37,7 +39,8 @@ _ENTRY = os.path.join(_PKG, "_entry.so")
 
 EXPORTS = ("attnw_fused", "attnw_softmax", "attnw_softmax_cast", "attnw_gemm_scores", "attnw_scale", "attnw_attention",
            "attnw_rotary_table", "attnw_rotary", "attnw_cache_append", "attnw_paged_workspace", "attnw_paged_attention",
-           "attnw_paged_sums", "attnw_cache_evict", "attnw_status_string", "attnw_version")
+           "attnw_paged_sums", "attnw_cache_evict", "attnw_rotary_axes_table", "attnw_rotary_axes", "attnw_byte_cache_append", "attnw_byte_paged_workspace",
+           "attnw_byte_paged_attention", "attnw_status_string", "attnw_version")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -132,9 +135,16 @@ def load_library():
         lib.attnw_paged_attention.argtypes = [vp] * 6 + [i64] * 3 + [vp, i64, vp]
         lib.attnw_paged_sums.argtypes = [vp] * 7 + [i64] * 3 + [vp]
         lib.attnw_cache_evict.argtypes = [vp] * 5 + [i64] * 2 + [vp]
-        for name in ("rotary_table", "rotary", "cache_append", "paged_attention", "paged_sums", "cache_evict"):
+        lib.attnw_rotary_axes_table.argtypes = [vp, vp, i64, i64, cd, cd, cd, cd, cd, cd, vp]
+        lib.attnw_rotary_axes.argtypes = [vp] * 5 + [i64] * 7 + [ci] * 3 + [vp]
+        lib.attnw_byte_cache_append.argtypes = [vp] * 9 + [i64] * 6 + [ci, vp]
+        lib.attnw_byte_paged_workspace.argtypes = [vp, i64, i64]
+        lib.attnw_byte_paged_attention.argtypes = [vp] * 6 + [i64] * 3 + [vp, i64, vp]
+        for name in ("rotary_table", "rotary", "cache_append", "paged_attention", "paged_sums", "cache_evict", "rotary_axes_table", "rotary_axes", "byte_cache_append",
+                     "byte_paged_attention"):
             getattr(lib, f"attnw_{name}").restype = ci
         lib.attnw_paged_workspace.restype = i64
+        lib.attnw_byte_paged_workspace.restype = i64
         lib.attnw_status_string.argtypes = [ci]
         lib.attnw_status_string.restype = ctypes.c_char_p
         lib.attnw_version.argtypes = []
@@ -289,12 +299,41 @@ class AttnwRule(ctypes.Structure):
         self._address = ctypes.addressof(self)
 
 
+class AttnwAxes(ctypes.Structure):
+    """Axes of rotary positions: how many pairs of columns each has; see ``attnw_axes`` in include/attnw.h."""
+    _fields_ = [("count", ctypes.c_int32), ("order", ctypes.c_int32), ("fresh", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4)]
+
+    def __init__(self, pairs, order: int = ATTNW_SECTIONS, fresh: int = 0):
+        pairs = tuple(pairs)
+        super().__init__(len(pairs), int(order), int(fresh), (ctypes.c_int32 * 4)(*pairs[:4]))
+        self._address = ctypes.addressof(self)
+
+
+class AttnwByteCache(ctypes.Structure):
+    """A paged cache in 8 bits; see ``attnw_byte_cache`` in include/attnw.h.  Addresses or tensors, which it keeps alive."""
+    _fields_ = [("cache", AttnwCache), ("K_scales", ctypes.c_void_p), ("V_scales", ctypes.c_void_p), ("block", ctypes.c_int64)]
+
+    def __init__(self, K, V, K_scales, V_scales, table, lengths, batch: int, pages: int, max_pages: int, page_size: int, block: int, kv_heads: int, d: int,
+                 dtype: int):
+        super().__init__(AttnwCache(K, V, table, lengths, batch, pages, max_pages, page_size, kv_heads, d, dtype), _ptr(K_scales), _ptr(V_scales), block)
+        self._kept = (K, V, K_scales, V_scales, table, lengths)
+        self._address = ctypes.addressof(self)
+
+
 def _cache(x) -> Optional[int]:
     return _struct(x, AttnwCache)
 
 
 def _rule(x) -> Optional[int]:
     return _struct(x, AttnwRule)
+
+
+def _axes(x) -> Optional[int]:
+    return _struct(x, AttnwAxes)
+
+
+def _byte_cache(x) -> Optional[int]:
+    return _struct(x, AttnwByteCache)
 
 
 def attnw_rotary_table(table, positions: int, rot: int, base: float = 10000.0, factor: float = 1.0, low: float = 0.0,
@@ -345,6 +384,42 @@ def attnw_paged_sums(cache, rule, Q, lse, before, sums, starts, tokens: int, hea
 def attnw_cache_evict(cache, into, sums, into_sums, kept, keep: int, recent: int, stream=None) -> None:
     """The slots that collected the most weight into other pages; see ``attnw_cache_evict`` in include/attnw.h."""
     _check(load_library().attnw_cache_evict(_cache(cache), _cache(into), _ptr(sums), _ptr(into_sums), _ptr(kept), keep, recent, _stream(stream)))
+
+
+def attnw_rotary_axes_table(table, axes, positions: int, rot: int, base: float = 10000.0, factor: float = 1.0, low: float = 0.0, high: float = 0.0,
+                            original: float = 0.0, gain: float = 1.0, stream=None) -> None:
+    """Cosines and sines of rotary positions with several axes; see ``attnw_rotary_axes_table`` in include/attnw.h."""
+    _check(load_library().attnw_rotary_axes_table(_ptr(table), _axes(axes), positions, rot, base, factor, low, high, original, gain, _stream(stream)))
+
+
+@_word_entry_point("ppppsiiiiiiinnn", AttnwAxes)
+def attnw_rotary_axes(X, Y, table, positions, axes, tokens: int, heads: int, d: int, rot: int, rows: int, x_stride: int, y_stride: int, layout: int,
+                      inverse: int, dtype: int, stream=None) -> None:
+    """Y = X with rotary positions on several axes, or the gradient of that; see ``attnw_rotary_axes`` in include/attnw.h."""
+    _check(load_library().attnw_rotary_axes(_ptr(X), _ptr(Y), _ptr(table), _ptr(positions), _axes(axes), tokens, heads, d, rot, rows, x_stride, y_stride,
+                                            int(layout), int(inverse), int(dtype), _stream(stream)))
+
+
+@_word_entry_point("sppppppspiiiiiin", AttnwByteCache, AttnwAxes)
+def attnw_byte_cache_append(cache, Q, K, V, R, table, positions, axes, starts, tokens: int, heads: int, rot: int, rows: int, q_stride: int, kv_stride: int,
+                        layout: int, stream=None) -> None:
+    """Queries turned, keys turned and values into a cache in 8 bits; see ``attnw_byte_cache_append`` in include/attnw.h."""
+    _check(load_library().attnw_byte_cache_append(_byte_cache(cache), _ptr(Q), _ptr(K), _ptr(V), _ptr(R), _ptr(table), _ptr(positions), _axes(axes), _ptr(starts),
+                                              tokens, heads, rot, rows, q_stride, kv_stride, int(layout), _stream(stream)))
+
+
+def attnw_byte_paged_workspace(cache, tokens: int, heads: int) -> int:
+    """Bytes of workspace that ``attnw_byte_paged_attention`` needs; see include/attnw.h."""
+    size = int(load_library().attnw_byte_paged_workspace(_byte_cache(cache), tokens, heads))
+    _check(min(size, 0))
+    return size
+
+
+@_word_entry_point("ssppppiiipi", AttnwByteCache, AttnwRule)
+def attnw_byte_paged_attention(cache, rule, Q, O, lse, starts, tokens: int, heads: int, q_stride: int, workspace, workspace_bytes: int, stream=None) -> None:
+    """Attention of new tokens over a paged cache in 8 bits; see ``attnw_byte_paged_attention`` in include/attnw.h."""
+    _check(load_library().attnw_byte_paged_attention(_byte_cache(cache), _rule(rule), _ptr(Q), _ptr(O), _ptr(lse), _ptr(starts), tokens, heads, q_stride,
+                                                 _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 _attach()

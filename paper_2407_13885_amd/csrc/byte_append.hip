@@ -1,0 +1,288 @@
+// New tokens on their way into a paged cache that holds a byte an element: queries turned, keys turned and rounded, values rounded.
+//
+// The slots of a block share a scale 2^e, e the least with max |x| <= 448 2^e over the block's rows; a block that had rows before keeps at least the e that it had, and
+// where that grows its old rows are rounded again.  So a block's rows, old and new, are the work of one group of lanes: they turn the new rows and keep them in registers, find
+// the largest element, and store.  No atomics, and nothing that depends on which block comes first.
+//
+// What bounds it: memory.  Rows of queries are turned as without a cache (rotary_common.h), by other workgroups of the same launch.
+#include "rotary_common.h"
+#include "byte_cache.h"
+
+namespace attnw {
+namespace {
+
+struct AppendArgs {
+    const void *Q, *K, *V;
+    void* R;
+    uint8_t *Kc, *Vc;
+    const float* angles;
+    const int32_t* starts;
+    AxesView axes;
+    CacheView cache;
+    ScalesView scales;
+    TurnUnits queries, keys;
+    FastDiv value_units;                          // units of a row of values
+    int64_t rows, q_stride, kv_stride;
+    int32_t tokens, heads, d, rot, most_blocks;   // most_blocks: of all sequences, at most
+    uint32_t kv_workgroups, q_blocks, q_parts;
+};
+
+// (each product rounded: the scale that a block gets is the one that the definition in fp32 gives it)
+__device__ __forceinline__ void turn_apart(float& x, float& y, float c, float s)
+{
+#pragma clang fp contract(off)
+    const float a = x * c - y * s, b = y * c + x * s;
+    x = a;
+    y = b;
+}
+
+// LANES: so many share a block of a head; HOLD: units of it that a lane keeps (the others are read again).
+template <typename T, int V> constexpr int kHold = V == 8 ? 4 : 8;
+
+template <typename T, int V, bool INTERLEAVED, int LANES>
+__global__ __launch_bounds__(256)
+void byte_append_kernel(AppendArgs a)
+{
+    typedef Chunk<T, V> C;
+    constexpr bool TWO = !INTERLEAVED || V == 1;
+    constexpr int P = TWO ? V : V / 2, HOLD = kHold<T, V>, HEADS = LANES < 64 ? 64 / LANES : 1;   // HEADS: that a wave works on at once
+    __shared__ uint32_t of[8];
+    __shared__ uint32_t tops[4];
+    if (threadIdx.x < 8) of[threadIdx.x] = a.axes.of[threadIdx.x];
+    __syncthreads();
+    const CacheView& cache = a.cache;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+
+    if (blockIdx.x >= a.kv_workgroups) {          // ---- queries ----------------------------------------------------------------------------
+        const auto position = [&](int64_t t, int axis) __attribute__((always_inline)) {
+            if (a.axes.positions) return (int64_t)a.axes.positions[axis * a.axes.tokens + t];
+            int low = 0, high = cache.batch;      // the first sequence that ends behind t
+            while (low < high) {
+                const int mid = (low + high) >> 1;
+                if (a.starts[mid + 1] > t) high = mid;
+                else low = mid + 1;
+            }
+            if (low >= cache.batch) return (int64_t)-1;
+            const Sequence s = sequence_at(cache, a.starts, a.tokens, low);
+            const int64_t slot = s.length - s.tokens + (t - s.first);
+            return t >= s.first ? slot : (int64_t)-1;
+        };
+        const uint32_t w = blockIdx.x - a.kv_workgroups, block = w % a.q_blocks;
+        turn_rows<T, V, INTERLEAVED>(static_cast<const T*>(a.Q), static_cast<T*>(a.R), a.angles, a.axes.count, of, position, a.tokens, a.d, a.rot, a.rows, a.q_stride,
+                                     (int64_t)a.heads * a.d, 1.0f, a.queries, block, a.q_blocks, w / a.q_blocks, a.q_parts);
+        return;
+    }
+
+    // ---- keys and values -------------------------------------------------------------------------------------------------------------------
+    const int32_t size = (int32_t)a.scales.block.d;
+    const auto blocks_of = [&](int b) __attribute__((always_inline)) {   // that new tokens of sequence b lie in
+        const Sequence s = sequence_at(cache, a.starts, a.tokens, b);
+        if (s.tokens == 0 || s.length == 0) return 0;
+        return (int32_t)(quotient(s.length - 1, a.scales.block) - quotient(max(0, s.length - s.tokens), a.scales.block)) + 1;
+    };
+    const int32_t total = plan_total(cache.batch, lane, blocks_of);
+    const int32_t groups = (cache.kv_heads + HEADS - 1) / HEADS, per_block = 2 * groups;
+    constexpr int AT_ONCE = LANES == 256 ? 1 : 4;              // items of a workgroup
+    const int l = LANES == 256 ? (int)threadIdx.x : lane % LANES;
+    for (int64_t item = (int64_t)blockIdx.x * AT_ONCE + (AT_ONCE > 1 ? wave : 0); item < (int64_t)total * per_block; item += (int64_t)a.kv_workgroups * AT_ONCE) {
+        const int32_t block = (int32_t)(item / per_block), of_block = (int32_t)(item - (int64_t)block * per_block);
+        const bool value = of_block >= groups;
+        const int32_t head = (value ? of_block - groups : of_block) * HEADS + (HEADS > 1 ? lane / LANES : 0);
+        int32_t b, before;
+        plan_find(cache.batch, lane, block, blocks_of, b, before);
+        if (b >= cache.batch) break;              // (starts in no order)
+        const Sequence s = sequence_at(cache, a.starts, a.tokens, b);
+        const int32_t base = max(0, s.length - s.tokens);
+        const int32_t slot0 = (int32_t)(quotient(base, a.scales.block) + (block - before)) * size;   // the block's first
+        const int32_t first = max(slot0, base), count = min(slot0 + size, s.length) - first;          // its new ones
+        const uint32_t page = quotient(slot0, cache.page);
+        const int32_t id = cache.table[(int64_t)b * cache.max_pages + page];
+        if ((uint32_t)id >= (uint32_t)cache.pages) continue;  // no such page: nothing is cached
+        const int32_t row0 = slot0 - (int32_t)(page * cache.page.d);
+        const bool active = head < cache.kv_heads;
+        const int64_t place = (int64_t)id * cache.kv_heads + (active ? head : 0);
+        uint8_t* const at = (value ? a.Vc : a.Kc) + (place * cache.page.d + row0) * a.d;              // of slot0
+        uint8_t* const scale = (value ? a.scales.V : a.scales.K) + place * a.scales.per_page + quotient(row0, a.scales.block);
+        const T* const src = static_cast<const T*>(value ? a.V : a.K) + (int64_t)(active ? head : 0) * a.d;
+        const int64_t t0 = (int64_t)s.first + s.tokens - (s.length - first);                           // the token of slot `first`
+        const FastDiv by_row = value ? a.value_units : a.keys.by_head;
+        const int32_t units = active ? count * (int32_t)by_row.d : 0;
+        const int32_t held = first > slot0 ? (int32_t)*scale : 0;   // (the block had rows before)
+
+        struct Unit { C a, b; };
+        float x[HOLD][TWO ? 2 : 1][V];
+        const auto columns = [&](int32_t row, int32_t u) __attribute__((always_inline)) {
+            const int32_t k = u - row * (int32_t)by_row.d;
+            return value ? UnitColumns{k * V, -1} : unit_columns<V, INTERLEAVED>(a.keys, k, a.rot);
+        };
+        const auto load = [&](int32_t u) __attribute__((always_inline)) {
+            const int32_t row = (int32_t)quotient(u, by_row);
+            const UnitColumns c = columns(row, u);
+            const T* const p = src + (t0 + row) * a.kv_stride;
+            Unit r;
+            r.a = *reinterpret_cast<const C*>(p + c.a);
+            r.b = r.a;
+            if constexpr (TWO)
+                if (c.b >= 0) r.b = *reinterpret_cast<const C*>(p + c.b);
+            return r;
+        };
+        const auto turn = [&](int32_t u, const Unit& r, float (&y)[TWO ? 2 : 1][V]) __attribute__((always_inline)) {
+            const int32_t row = (int32_t)quotient(u, by_row);
+            const UnitColumns c = columns(row, u);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                y[0][e] = wide(r.a.x[e]);
+                if constexpr (TWO) y[TWO ? 1 : 0][e] = c.b < 0 ? 0.0f : wide(r.b.x[e]);
+            }
+            if (c.b < 0) return;
+            Chunk<float, P> co, si;
+            load_angles<P>(a.angles, a.rot, a.rows, (u - row * (int32_t)by_row.d) * P, a.axes.count, of,
+                           [&](int axis) __attribute__((always_inline)) {
+                               return a.axes.positions ? (int64_t)a.axes.positions[axis * a.axes.tokens + t0 + row] : (int64_t)first + row;
+                           }, co, si);
+#pragma unroll
+            for (int e = 0; e < P; ++e) turn_apart(TWO ? y[0][e] : y[0][2 * e % V], TWO ? y[TWO ? 1 : 0][e] : y[0][(2 * e + 1) % V], co.x[e], si.x[e]);
+        };
+        const auto largest = [](const float (&y)[TWO ? 2 : 1][V]) __attribute__((always_inline)) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int n = 0; n < (TWO ? 2 : 1); ++n)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const uint32_t bits = __float_as_uint(y[n][e]) & 0x7fffffffu;
+                    top = max(top, bits < 0x7f800000u ? bits : 0u);   // (infinities and NaN come to be NaN and leave the others their scale)
+                }
+            return top;
+        };
+        const auto store = [&](int32_t u, const float (&y)[TWO ? 2 : 1][V], float up) __attribute__((always_inline)) {
+            const int32_t row = (int32_t)quotient(u, by_row);
+            const UnitColumns c = columns(row, u);
+            uint8_t* const to = at + (int64_t)(first - slot0 + row) * a.d;
+#pragma unroll
+            for (int n = 0; n < (TWO ? 2 : 1); ++n) {
+                if (n == 1 && c.b < 0) break;
+                uint8_t* const p = to + (n == 0 ? c.a : c.b);
+                if constexpr (V == 1) {
+                    *p = (uint8_t)pack_e4m3<false>(y[n][0] * up, 0.0f, 0);
+                } else {
+                    uint32_t w[V / 4 > 0 ? V / 4 : 1];
+#pragma unroll
+                    for (int q = 0; q < V / 4; ++q) w[q] = pack_e4m3(y[n][4 * q] * up, y[n][(4 * q + 1) % V] * up, y[n][(4 * q + 2) % V] * up, y[n][(4 * q + 3) % V] * up);
+                    if constexpr (V == 8) *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[V / 4 > 1 ? 1 : 0]};
+                    else *reinterpret_cast<uint32_t*>(p) = w[0];
+                }
+            }
+        };
+
+        uint32_t top = 0;
+        {
+            Unit raw[HOLD];
+#pragma unroll
+            for (int n = 0; n < HOLD; ++n)
+                if (l + n * LANES < units) raw[n] = load(l + n * LANES);
+#pragma unroll
+            for (int n = 0; n < HOLD; ++n)
+                if (l + n * LANES < units) {
+                    turn(l + n * LANES, raw[n], x[n]);
+                    top = max(top, largest(x[n]));
+                }
+        }
+        for (int32_t u = l + HOLD * LANES; u < units; u += LANES) {
+            float y[TWO ? 2 : 1][V];
+            turn(u, load(u), y);
+            top = max(top, largest(y));
+        }
+#pragma unroll
+        for (int off = (LANES < 64 ? LANES : 64) / 2; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
+        if constexpr (LANES == 256) {
+            if (lane == 0) tops[wave] = top;
+            __syncthreads();
+            top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+            __syncthreads();
+        }
+        if (!active) continue;
+        int e = exponent_for(top);
+        if (first > slot0) {
+            const int old = max(kLeastScale, min(held - 127, kMostScale));
+            if (e > old) {                        // older rows in units of the new scale
+                const float down = __uint_as_float((uint32_t)max(0, 127 + old - e) << 23);
+                uint32_t* const words = reinterpret_cast<uint32_t*>(at);
+                for (int32_t i = l; i < (first - slot0) * (a.d / 4); i += LANES) {
+                    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(words[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(words[i], true);
+                    words[i] = pack_e4m3(lo[0] * down, lo[1] * down, hi[0] * down, hi[1] * down);
+                }
+            } else {
+                e = old;
+            }
+        }
+        if (l == 0) *scale = (uint8_t)(e + 127);
+        const float up = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+        for (int n = 0; n < HOLD; ++n)
+            if (l + n * LANES < units) store(l + n * LANES, x[n], up);
+        for (int32_t u = l + HOLD * LANES; u < units; u += LANES) {
+            float y[TWO ? 2 : 1][V];
+            turn(u, load(u), y);
+            store(u, y, up);
+        }
+    }
+}
+
+template <typename T, int V, bool INTERLEAVED> hipError_t launch(AppendArgs a, hipStream_t stream)
+{
+    a.queries = turn_units<V, INTERLEAVED>(a.heads > 0 ? a.heads : 1, a.d, a.rot);
+    a.keys = turn_units<V, INTERLEAVED>(1, a.d, a.rot);
+    a.value_units = fast_div((uint32_t)(a.d / V));
+    const dim3 q = turn_grid(a.queries, a.tokens);
+    a.q_blocks = q.x;
+    a.q_parts = q.y;
+    const int64_t units = (int64_t)a.scales.block.d * (a.d / V);   // of a block, at most
+    auto go = [&](auto kernel, int lanes) {
+        const int64_t groups = lanes < 64 ? (a.cache.kv_heads + 64 / lanes - 1) / (64 / lanes) : a.cache.kv_heads;
+        const int64_t items = a.most_blocks * 2 * groups, all = lanes == 256 ? items : (items + 3) / 4;
+        a.kv_workgroups = (uint32_t)(all < 1 << 20 ? all : 1 << 20);
+        kernel<<<a.kv_workgroups + (a.heads > 0 ? a.q_blocks * a.q_parts : 0), 256, 0, stream>>>(a);
+        return hipGetLastError();
+    };
+    if (units <= 16 * kHold<T, V>) return go(byte_append_kernel<T, V, INTERLEAVED, 16>, 16);
+    if (units <= 64 * kHold<T, V>) return go(byte_append_kernel<T, V, INTERLEAVED, 64>, 64);
+    return go(byte_append_kernel<T, V, INTERLEAVED, 256>, 256);
+}
+
+template <typename T, int V> hipError_t launch_typed(const RotaryArgs& r, const AppendArgs& a, hipStream_t stream)
+{
+    const bool chunks = turns_by_chunks(V, a.d, a.rot, a.heads > 0 ? a.q_stride : V, a.kv_stride, r.interleaved);
+    if (r.interleaved) return chunks ? launch<T, V, true>(a, stream) : launch<T, 1, true>(a, stream);
+    return chunks ? launch<T, V, false>(a, stream) : launch<T, 1, false>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_byte_append(const RotaryArgs& r, const ScalesView& scales, const AxesMap* map, hipStream_t stream)
+{
+    AppendArgs a{};
+    a.Q = r.Q;
+    a.K = r.K;
+    a.V = r.V;
+    a.R = r.R;
+    a.Kc = static_cast<uint8_t*>(r.Kc);
+    a.Vc = static_cast<uint8_t*>(r.Vc);
+    a.angles = r.angles;
+    a.starts = r.starts;
+    if (map) a.axes = axes_view(*map, r.positions, r.tokens);
+    else a.axes = AxesView{r.positions, r.tokens, 1, {}};
+    a.cache = r.cache;
+    a.scales = scales;
+    a.rows = r.rows;
+    a.q_stride = r.q_stride;
+    a.kv_stride = r.kv_stride;
+    a.tokens = (int32_t)r.tokens;
+    a.heads = (int32_t)r.heads;
+    a.d = (int32_t)r.d;
+    a.rot = (int32_t)r.rot;
+    const int64_t blocks = r.tokens / scales.block.d + 2 * (int64_t)r.cache.batch;
+    a.most_blocks = (int32_t)(blocks < r.tokens ? blocks : r.tokens);
+    return r.dt == DType::F32 ? launch_typed<float, 4>(r, a, stream) : launch_typed<uint16_t, 8>(r, a, stream);
+}
+
+}  // namespace attnw

@@ -1,0 +1,417 @@
+// Attention of new tokens over a paged cache in 8 bits, blocks of 16 rows: single tokens and short chunks.
+//
+//     O = softmax(s) V,  s = scale q . k  -> cap tanh(s / cap) -> s - slope |i - j|,  over the slots j that the token at slot i sees
+//
+// As paged_rows.h: a row is one query head of one token, the heads of a kv head and their tokens share a block, each wave has keys of its own, tiles of 32, that go
+// from their pages into its part of LDS as they lie in memory, one tile under way while it computes another.  An element becomes bf16 (which holds it exactly) on its way
+// to the matrix instruction, two to an instruction: keys with their scale, values without, whose scale goes into the weights.  A lane's 16 bytes
+// of a key are 16 columns, the operands of two instructions; of values the transposing read of bytes gives a lane a column of the 8 keys that its weights are for.
+// fp32 queries and weights are three bf16 parts, three products where the fp32 instruction would take eight times as long.
+//
+// What bounds it: the read of K and V.
+#pragma once
+
+#include "paged_attention.h"
+#include "byte_cache.h"
+
+namespace attnw {
+namespace {
+
+constexpr int kRows = 16;                         // of a block
+
+// UB: 64-byte groups of a row on chip.
+template <int UB> struct ByteRowsCfg {
+    static constexpr int KT = 32;                 // keys of a tile
+    static constexpr int DB = UB * 64, CPR = UB * 4, TILE = KT * DB, XFERS = TILE / 1024;
+    static constexpr int COLS = DB, CB = COLS / 16;
+    static constexpr int NW = UB <= 2 ? 8 : 4;
+    static constexpr int UNIT = KT * NW;          // keys of a place
+    static constexpr int PITCH = COLS + 4;        // floats of a row of partial results
+    static constexpr int STAGES = NW * 4 * TILE;
+    static constexpr int LDS = STAGES + kPlaces * 8 + NW * kRows * 8;
+    static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;
+    static_assert(4 * TILE >= kRows * PITCH * 4, "partial results of a wave in its stages");
+    static_assert(STAGES <= kDirectLds);
+};
+
+// Transposing LDS read of bytes (ds_read_b64_tr_b8): each group of 16 lanes reads eight runs of 16 bytes, lanes 2j and 2j + 1 run j, and lane i of the group gets
+// byte i of the eight runs.
+__device__ __forceinline__ u32x2 lds_read_tr8(const char* p)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    typedef i32x2 __attribute__((address_space(3)))* tr_ptr;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((tr_ptr)(p)));
+#else
+    (void)p;
+    return u32x2{0u, 0u};
+#endif
+}
+// Four elements as bf16, times a power of 2; eight of them, the operand of a matrix instruction.
+__device__ __forceinline__ u32x2 bf16_of(uint32_t w, float scale)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
+#else
+    (void)w;
+    (void)scale;
+    return u32x2{0u, 0u};
+#endif
+}
+__device__ __forceinline__ u32x4 bf16_of(uint32_t a, uint32_t b, float scale) { return u32x4_of(bf16_of(a, scale), bf16_of(b, scale)); }
+
+// 8 numbers as bf16: as they are, or their three parts
+template <int PARTS> struct Parts { u32x4 of[PARTS]; };
+template <int PARTS> __device__ __forceinline__ Parts<PARTS> parts_of(const float (&y)[8])
+{
+    Parts<PARTS> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = y[2 * i], b = y[2 * i + 1];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const uint32_t w = pack_bf16x2(a, b);
+            r.of[p][i] = w;
+            a -= bf16_lo_to_f32(w);
+            b -= bf16_hi_to_f32(w);
+        }
+    }
+    return r;
+}
+// (the smallest part first)
+template <int PARTS> __device__ __forceinline__ void multiply_parts(f32x4& acc, const u32x4& x, const Parts<PARTS>& y)
+{
+#pragma unroll
+    for (int p = PARTS - 1; p >= 0; --p) mma16(acc, x, y.of[p]);
+}
+
+// Where the keys of a place of 2^grain lie, and the bytes of their scales in the upper 16 bits.
+__device__ __forceinline__ int64_t slot_place(const CacheView& c, const ScalesView& s, const int32_t* pages_of, int kv_head, int j)
+{
+    const uint32_t p = quotient((uint32_t)j, c.page);
+    const int32_t id = max(0, min(pages_of[p], c.pages - 1)), row = j - (int)(p * c.page.d);
+    const int64_t scale = ((int64_t)id * c.kv_heads + kv_head) * s.per_page + quotient(row, s.block);
+    const uint64_t at = (uint64_t)(uint32_t)id * c.page_bytes + (uint32_t)kv_head * c.head_bytes + (uint32_t)row * (uint32_t)c.row_bytes;
+    return (int64_t)(at | (uint64_t)s.K[scale] << 48 | (uint64_t)s.V[scale] << 56);
+}
+__device__ __forceinline__ int64_t place_offset(int64_t place) { return place & (((int64_t)1 << 48) - 1); }
+__device__ __forceinline__ float key_scale(uint32_t high) { return scale_of(high >> 16 & 255); }
+__device__ __forceinline__ float value_scale(uint32_t high) { return scale_of(high >> 24); }
+// 2^grain slots lie in one page and share their scales
+inline int key_grain(const CacheView& c, const ScalesView& s)
+{
+    CacheView of = c;
+    of.page = s.block;                            // (it divides the page)
+    return key_grain(of);
+}
+
+template <typename T, int UB, int MODE, bool EXACT, int THREADS = 64 * ByteRowsCfg<UB>::NW>
+__global__ __launch_bounds__(THREADS, 2)
+void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
+{
+    using C = ByteRowsCfg<UB>;
+    using L = RowLayout<UB>;
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+    constexpr bool F32 = PARTS == 3;
+    constexpr int NW = C::NW, KT = C::KT, DB = C::DB, CPR = C::CPR, TILE = C::TILE, XFERS = C::XFERS, CB = C::CB, NK = KT / 16, PITCH = C::PITCH;
+    __shared__ __align__(1024) char lds[C::LDS];
+    int64_t* const places = reinterpret_cast<int64_t*>(lds + C::STAGES);
+    float* const stats = reinterpret_cast<float*>(lds + C::STAGES + kPlaces * 8);   // [wave][row]{maximum, sum}
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
+    char* const stage = lds + wave * 4 * TILE;    // K, V of one tile, K, V of the next
+    const uint32_t stage_at = lds_offset_of(stage);
+    const int rb = EXACT ? DB : a.cache.row_bytes;
+
+    Walk<kRows> walk(a, lane);
+    if (walk.at >= walk.end) return;
+
+    const ScoreMap<(MODE & kCap) != 0, F32> map(a.rule);
+    // Chunks of 16 bytes of V trade places so that eight rows of the transposing read (keys 4 q .. + 3 and 16 more) lie in different eighths of 128 bytes.
+    const auto v_chunk = [](int key) __attribute__((always_inline)) {
+        return UB % 2 == 0 ? (key & 3) | (key >> 2 & 4) : (key >> 1 & 1) | (key >> 3 & 2);
+    };
+    Segment seg;
+    while (walk.next(seg)) {
+        const Sequence& seq = seg.seq;
+        const int prefix = seg.prefix, kv_head = seg.kv_head, row0 = seg.row0, rows = seg.rows;
+        // ---- the rows of the block ------------------------------------------------------------------------------------------------
+        const int group = a.group.d, base = seq.length - seq.tokens;              // slot of the first new token
+        const int first = base + (int)quotient(row0, a.group), last = base + (int)quotient(row0 + rows - 1, a.group);
+        const int row = row0 + min(l16, rows - 1);
+        const int token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
+        const int query = base + token;   // sees the slots query - window + 1 .. query
+        const float slope = MODE & kBias ? a.rule.slopes[head] * kLog2e : 0.0f;
+
+        Parts<PARTS> qf[2 * UB];                  // columns 64 g + 16 quarter .. + 7, and the 8 behind them (zeros behind the row's end)
+        {
+            const char* q = a.Q + (int64_t)(seq.first + token) * a.q_stride + (int64_t)head * rb * (int)sizeof(T);
+#pragma unroll
+            for (int g = 0; g < UB; ++g) {
+                const int at = (4 * g + quarter) * 16;
+                const bool inside = EXACT || at < rb;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const char* const p = q + (inside ? at + 8 * half : 0) * (int)sizeof(T);
+                    if constexpr (F32) {
+                        const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 16);
+                        float y[8];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = inside ? lo[i] : 0.0f, y[4 + i] = inside ? hi[i] : 0.0f;
+                        qf[2 * g + half] = parts_of<PARTS>(y);
+                    } else {
+                        qf[2 * g + half].of[0] = inside ? *reinterpret_cast<const u32x4*>(p) : u32x4{0, 0, 0, 0};
+                    }
+                }
+            }
+        }
+        f32x4 oacc[CB];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) oacc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        float m_run = -__builtin_inff(), l_run = 0.0f;
+
+        // ---- the keys of places v0 .. v1 - 1 -----------------------------------------------------------------------------------------
+        const Span span = visible_span(a.unit_log, first, last, seq.length, prefix, a.rule.window);
+        const int units = last < 0 && span.head == 0 ? 0 : span.count();
+        const int u0 = walk.share(seg, seg.v0, units), u1 = walk.share(seg, seg.v1, units);
+        const int seen = min(seq.length, max(prefix, last + 1));
+        const int32_t* const pages_of = a.cache.table + (int64_t)seg.b * a.cache.max_pages;
+
+        auto sweep = [&](int from, int to) __attribute__((always_inline)) {   // keys
+            const int most = kPlaces << grain;    // (a whole number of units: the waves' tiles stay where they are)
+            for (int k0 = from; k0 < to;) {
+                const int k1 = min(to, k0 + most);
+                __syncthreads();
+                for (int i = threadIdx.x; i < (k1 - k0 + (1 << grain) - 1) >> grain; i += 64 * NW)
+                    places[i] = slot_place(a.cache, scales, pages_of, kv_head, k0 + (i << grain));
+                wait_vmem();
+                __syncthreads();
+
+                auto issue = [&](int key0, int s) __attribute__((always_inline)) {
+                    int64_t row[XFERS];
+#pragma unroll
+                    for (int j = 0; j < XFERS; ++j) {          // (past the end the last slot)
+                        const int slot = min(key0 + (j * 64 + lane) / CPR, k1 - 1) - k0;
+                        row[j] = place_offset(places[slot >> grain]) + (slot & ((1 << grain) - 1)) * rb;
+                    }
+#pragma unroll
+                    for (int v = 0; v < 2; ++v)
+#pragma unroll
+                        for (int j = 0; j < XFERS; ++j) {
+                            const int x = j * 64 + lane, key = x / CPR, c = x - key * CPR;
+                            const int ch = v == 0 ? c ^ L::k_chunk(key) : c ^ v_chunk(key);
+                            // (behind a row's end on chip: its first chunks, which meet zeros of Q and make columns of V that nobody stores)
+                            dma16_untracked((v ? a.cache.V : a.cache.K) + row[j] + (EXACT ? ch * 16 : chunk_in_row(ch * 16, rb)), stage_at + (2 * s + v) * TILE + j * 1024);
+                        }
+                };
+                const auto high_of = [&](int key) __attribute__((always_inline)) {   // of a key's place the half with the scales
+                    return reinterpret_cast<const uint32_t*>(places)[2 * ((min(key, k1 - 1) - k0) >> grain) + 1];
+                };
+                auto compute = [&](int key0, int s, bool more) __attribute__((always_inline)) {
+                    const char* const kt = stage + 2 * s * TILE;
+                    const char* const vt = kt + TILE;
+                    if (more) arrived<3 * XFERS>();
+                    else arrived<XFERS>();
+                    float x[NK * 4];
+#pragma unroll
+                    for (int k = 0; k < NK; ++k) {
+                        const float ks = key_scale(high_of(key0 + 16 * k + l16));
+                        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int g = 0; g < UB; ++g) {
+                            const u32x4 w = *reinterpret_cast<const u32x4*>(kt + (16 * k + l16) * DB + ((4 * g + quarter) ^ L::k_chunk(l16)) * 16);
+                            multiply_parts(acc, bf16_of(w[0], w[1], ks), qf[2 * g]);
+                            multiply_parts(acc, bf16_of(w[2], w[3], ks), qf[2 * g + 1]);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[4 * k + r] = acc[r];
+                    }
+                    map(x);
+                    const int key = key0 + 4 * quarter;        // + 16 k + r
+                    if constexpr ((MODE & kBias) != 0) {
+#pragma unroll
+                        for (int i = 0; i < NK * 4; ++i) x[i] -= slope * (float)abs(query - (key + 16 * (i / 4) + i % 4));
+                    }
+                    const bool whole = key0 + KT <= k1 && ((key0 + KT - 1 <= first && key0 > last - a.rule.window) || key0 + KT <= prefix);
+                    if (!whole) {
+                        const Sight sight(query, a.rule, prefix, k1);
+#pragma unroll
+                        for (int i = 0; i < NK * 4; ++i) x[i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? -__builtin_inff() : x[i];
+                    }
+                    float top = x[0];
+#pragma unroll
+                    for (int i = 1; i < NK * 4; ++i) top = fmaxf(top, x[i]);
+                    top = quarter_wave_max(top);
+                    if (__builtin_amdgcn_ballot_w64(top > m_run) != 0) {
+                        const float m = fmaxf(m_run, top), alpha = m == -__builtin_inff() ? 1.0f : fast_exp2(m_run - m);
+                        l_run *= alpha;
+#pragma unroll
+                        for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
+                        m_run = m;
+                    }
+                    const float ref = m_run == -__builtin_inff() ? 0.0f : m_run;   // (nothing seen yet: all weights 0)
+                    float p[NK * 4];
+#pragma unroll
+                    for (int i = 0; i < NK * 4; ++i) {
+                        p[i] = fast_exp2(x[i] - ref);
+                        l_run += p[i];
+                    }
+                    // weights in units of the values' scales (powers of 2: no rounding)
+#pragma unroll
+                    for (int k = 0; k < NK; ++k) {
+                        if (grain >= 2) {
+                            const float vs = value_scale(high_of(key + 16 * k));
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) p[4 * k + r] *= vs;
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) p[4 * k + r] *= value_scale(high_of(key + 16 * k + r));
+                        }
+                    }
+                    if (more) arrived<2 * XFERS>();
+                    else arrived<0>();
+                    // fragments of V: 16 columns x the keys of this lane's weights
+                    const int vkey = 4 * quarter + (l16 >> 1 & 3) + (l16 >> 3) * 16;
+                    const auto v_frag = [&](int c) __attribute__((always_inline)) {
+                        const u32x2 w = lds_read_tr8(vt + vkey * DB + (c ^ v_chunk(vkey)) * 16 + (lane & 1) * 8);
+                        return bf16_of(w[0], w[1], 1.0f);
+                    };
+                    const Parts<PARTS> pw = parts_of<PARTS>(p);
+                    if (!whole) {
+                        uint32_t bad = 0;
+#pragma unroll
+                        for (int c = 0; c < CB; ++c) bad |= any_lost<uint16_t>(v_frag(c));
+                        if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
+                            // NaN among the values, which must not reach rows that do not see them by way of a weight of 0: 0 in the product, and NaN for those that do
+                            const Sight sight(query, a.rule, prefix, k1);
+                            float some[NK * 4];
+#pragma unroll
+                            for (int i = 0; i < NK * 4; ++i) some[i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? 0.0f : 1.0f;
+                            const u32x4 so = parts_of<1>(some).of[0];
+#pragma unroll
+                            for (int c = 0; c < CB; ++c) {
+                                const u32x4 v = v_frag(c);
+                                f32x4 lost = {0.0f, 0.0f, 0.0f, 0.0f};
+                                mma16(lost, lost_as_one<uint16_t, kAny>(v), so);
+                                multiply_parts(oacc[c], without_lost<uint16_t>(v), pw);
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) oacc[c][r] = lost[r] > 0.0f ? __builtin_nanf("") : oacc[c][r];
+                            }
+                            return;
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) multiply_parts(oacc[c], v_frag(c), pw);
+                };
+                int key = k0 + wave * KT, s = 0;
+                if (key < k1) issue(key, 0);
+                for (; key < k1; key += C::UNIT, s ^= 1) {
+                    const bool more = key + C::UNIT < k1;
+                    if (more) issue(key + C::UNIT, s ^ 1);
+                    compute(key, s, more);
+                    wait_lds();                   // (the fragments have left the stage that is filled next)
+                }
+                k0 = k1;
+            }
+        };
+#pragma clang loop unroll(disable)
+        for (int part = 0; part < 2; ++part) {    // of the prefix, of what is near
+            const int f = part == 0 ? u0 : max(u0, span.head), t = part == 0 ? min(u1, span.head) : u1;
+            if (f < t) sweep(span.unit(f) << a.unit_log, (int)min((int64_t)seen, (int64_t)(span.unit(t - 1) + 1) << a.unit_log));
+        }
+        l_run = quarter_wave_sum(l_run);
+
+        // ---- the waves' results into one -----------------------------------------------------------------------------------------------
+        __syncthreads();
+        if (quarter == 0) {
+            stats[(wave * kRows + l16) * 2] = m_run;
+            stats[(wave * kRows + l16) * 2 + 1] = l_run;
+        }
+        float* const mine = reinterpret_cast<float*>(stage);
+#pragma unroll
+        for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4*>(mine + l16 * PITCH + 16 * c + 4 * quarter) = oacc[c];
+        __syncthreads();
+        const bool complete = seg.slot < 0;
+        float* const out = a.partial + max(seg.slot, 0) * (int64_t)(kRows * (C::COLS + 2));
+        constexpr int QUADS = C::COLS / 4;
+        for (int i = threadIdx.x; i < rows * QUADS; i += 64 * NW) {
+            const int r = i / QUADS, c = (i - r * QUADS) * 4;
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int n = 0; n < NW; ++n) top = fmaxf(top, stats[(n * kRows + r) * 2]);
+            const float ref = top == -__builtin_inff() ? 0.0f : top;
+            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+            float l = 0.0f;
+#pragma unroll
+            for (int n = 0; n < NW; ++n) {
+                const float f = fast_exp2(stats[(n * kRows + r) * 2] - ref);
+                l += f * stats[(n * kRows + r) * 2 + 1];
+                sum += *reinterpret_cast<const f32x4*>(lds + n * 4 * TILE + (r * PITCH + c) * 4) * f;
+            }
+            if (complete) {
+                const int tk = (int)quotient(row0 + r, a.group), h = kv_head * group + row0 + r - tk * group;
+                const int64_t o = (int64_t)(seq.first + tk) * a.heads + h;
+                store_output<T>(a.O, o, rb * (int)sizeof(T), c, sum, l);
+                if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
+            } else {
+                *reinterpret_cast<f32x4*>(out + r * C::COLS + c) = sum;
+                if (c == 0) {
+                    out[kRows * C::COLS + 2 * r] = top;
+                    out[kRows * C::COLS + 2 * r + 1] = l;
+                }
+            }
+        }
+    }
+}
+
+template <int UB> int byte_workgroups() { return (compute_units() * ByteRowsCfg<UB>::PER_CU + 7) & ~7; }
+
+template <typename T, int UB, int MODE> hipError_t launch(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
+{
+    using C = ByteRowsCfg<UB>;
+    AttendArgs a = attend_args(p, byte_workgroups<UB>(), kRows, C::UNIT, sizeof(T));
+    const int grain = key_grain(a.cache, scales);
+    // (rows that fill their place: kernels of their own for the usual sizes)
+    constexpr bool OWN = UB != 3;
+    if (OWN && a.cache.row_bytes == C::DB) byte_rows_kernel<T, UB, MODE, OWN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
+    else byte_rows_kernel<T, UB, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.cache.row_bytes *= (int)sizeof(T);          // (of the output)
+    return launch_join<T>(a, kRows, C::COLS, stream);
+}
+
+template <typename F> auto by_row(int row_bytes, F&& f)
+{
+    const int ub = (row_bytes + 63) / 64;
+    if (ub <= 1) return f(IC<1>{});
+    if (ub <= 2) return f(IC<2>{});
+    if (ub <= 3) return f(IC<3>{});
+    return f(IC<4>{});
+}
+
+inline int64_t rows_workspace(const PagedArgs& p)
+{
+    return by_row(p.cache.row_bytes, [&](auto ub) {
+        constexpr int UB = decltype(ub)::value;
+        return partial_bytes(byte_workgroups<UB>(), kRows, ByteRowsCfg<UB>::COLS);
+    });
+}
+
+template <typename T> hipError_t launch_rows(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
+{
+    return by_row(p.cache.row_bytes, [&](auto ubc) {
+        constexpr int UB = decltype(ubc)::value;
+        switch (rule_mode(p.rule)) {
+        case kPlain: return launch<T, UB, kPlain>(p, scales, stream);
+        case kCap: return launch<T, UB, kCap>(p, scales, stream);
+        case kBias: return launch<T, UB, kBias>(p, scales, stream);
+        default: return launch<T, UB, kCap | kBias>(p, scales, stream);
+        }
+    });
+}
+
+}  // namespace
+}  // namespace attnw

@@ -291,6 +291,25 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
 
+// Positions on several axes: the axis of each pair of columns, and which of its axis' pairs it is.
+struct AxesMap {
+    int32_t count, pairs[4];
+    bool fresh;                                   // frequencies begin again with each axis
+    uint8_t axis[128], index[128];
+};
+hipError_t launch_rotary_axes_table(float* table, const AxesMap& map, int64_t positions, int64_t rot, double base, double factor, double low, double high, double original,
+                                    double gain, hipStream_t stream);
+hipError_t launch_rotary_axes(const RotaryArgs& a, const AxesMap& map, hipStream_t stream);
+
+// The scales of a cache that holds a byte an element: [pages][kv_heads][page_size / block] each, a byte s standing for 2^(s - 127).
+struct ScalesView {
+    uint8_t *K, *V;
+    FastDiv block;                                // slots that share one
+    int32_t per_page;                             // of a page and head
+};
+// (a.Kc and a.Vc: the cache's bytes.  map: null where tokens have one position)
+hipError_t launch_byte_append(const RotaryArgs& a, const ScalesView& scales, const AxesMap* map, hipStream_t stream);
+
 struct PagedArgs {
     DType dt;
     CacheView cache;
@@ -315,6 +334,10 @@ hipError_t launch_paged_tiles_f32(const PagedArgs& a, hipStream_t stream);
 hipError_t launch_paged_tiles_cap(const PagedArgs& a, hipStream_t stream);
 hipError_t launch_paged_tiles_bias(const PagedArgs& a, hipStream_t stream);
 hipError_t launch_paged_tiles_both(const PagedArgs& a, hipStream_t stream);
+// The same over a cache that holds a byte an element (a.cache in bytes, a.dt the type of Q and O).
+int64_t byte_workspace(const PagedArgs& a, const ScalesView& scales);
+hipError_t launch_byte_attention(const PagedArgs& a, const ScalesView& scales, hipStream_t stream);
+hipError_t launch_byte_rows_f32(const PagedArgs& a, const ScalesView& scales, hipStream_t stream);
 
 struct SumsArgs {
     DType dt;

@@ -7,19 +7,10 @@
 //
 // What bounds it: memory, 2 bytes moved for every byte of the rows; a row of the table serves all heads of a token from the caches.  One launch
 // turns the queries, turns the keys and lays keys and values into their pages.
-#include "paged_common.h"
+#include "rotary_common.h"
 
 namespace attnw {
 namespace {
-
-template <typename T, int V> struct alignas(sizeof(T) * V) Chunk { T x[V]; };
-
-template <typename T> __device__ __forceinline__ float wide(T x);
-template <> __device__ __forceinline__ float wide<float>(float x) { return x; }
-template <> __device__ __forceinline__ float wide<uint16_t>(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-template <typename T> __device__ __forceinline__ T narrow(float x);
-template <> __device__ __forceinline__ float narrow<float>(float x) { return x; }
-template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float x) { return (uint16_t)pack_bf16x2(x, 0.0f); }
 
 struct Units {
     int32_t per_head, pairs;                      // units of a head; those of them that turn
@@ -186,10 +177,7 @@ void rotary_table_kernel(float* table, int64_t positions, int32_t half, double s
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < positions * half; i += (int64_t)gridDim.x * 256) {
         const int64_t p = i / half;
         const int32_t j = (int32_t)(i - p * half);
-        const double f = exp2(-step * j);         // radians a token
-        const double turns = original * f * 0.15915494309189535;
-        const double keep = turns >= high ? 1.0 : turns <= low ? 0.0 : (turns - low) / (high - low);
-        const double half_turns = (double)p * (f * (keep + (1.0 - keep) / factor)) * 0.3183098861837907;
+        const double half_turns = rotary_half_turns(p, step * j, factor, low, high, original);
         double s, c;
         sincospi(half_turns, &s, &c);
         table[p * 2 * half + j] = (float)(gain * c);

@@ -1,0 +1,229 @@
+"""Appending to a paged cache in 8 bits, byte by byte against its definition on the host (byte_util)."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_13885_amd as attnw
+from byte_util import Problem8, appended, axis_map, same_bytes, turned32
+from gpu_util import DT, TORCH_DT, require_gpu
+from paged_util import within
+from test_gpu_rotary import bound_of, table_of
+
+pytestmark = pytest.mark.gpu
+
+SECTIONS, TURNS, HALVES, PAIRS = attnw.ATTNW_SECTIONS, attnw.ATTNW_TURNS, attnw.ATTNW_HALVES, attnw.ATTNW_PAIRS
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    require_gpu()
+
+
+def new_rows(p, seed=0, spread=3.0):
+    """Queries, keys and values of the new tokens beside each other, tokens of very different sizes."""
+    g = torch.Generator().manual_seed(seed + 11)
+    wide = (p.heads + 2 * p.kv_heads) * p.d
+    x = torch.randn((max(1, p.T), wide), generator=g) * torch.exp2(spread * torch.randn((max(1, p.T), 1), generator=g))
+    return x.to(TORCH_DT[p.dtype])
+
+
+def run(p, x, rot, layout=HALVES, pairs=None, order=SECTIONS, positions=None, rows=400, stream=None, heads=None):
+    """What the library makes of it (R, and the cache's arrays in p.dev), and what the definition does."""
+    heads = p.heads if heads is None else heads
+    d, wide, table = p.dev, p.heads * p.d, table_of(rows, rot) if rot else None
+    R = torch.full((max(1, p.T), max(1, heads), p.d), 7.0, dtype=x.dtype, device="cuda")
+    dev = x.cuda()
+    table_dev, pos_dev = (None if v is None else v.cuda() for v in (table, positions))
+    axes = None if pairs is None else attnw.AttnwAxes(pairs, order)
+    attnw.attnw_byte_cache_append(p.cache, dev if heads else None, dev[:, wide:], dev[:, wide + p.kv_heads * p.d:], R if heads else None, table_dev, pos_dev, axes,
+                                  d["starts"], p.T, heads, rot, rows, x.shape[1], x.shape[1], layout, stream)
+    torch.cuda.synchronize()
+    at = positions
+    if at is None:                                # a token's slot
+        at = torch.cat([torch.arange(m - n, m) for n, m in zip(*zip(*[(int(p.starts[b + 1] - p.starts[b]), int(p.lengths[b])) for b in range(p.batch)]))]) if p.T else torch.zeros(0)
+    at = at.view(-1, max(1, p.T)) if p.T else at.view(1, 0)
+    axis = axis_map(pairs, order)[0] if pairs else [0] * (rot // 2)
+    q, k, v = x[:p.T].split([wide, p.kv_heads * p.d, p.kv_heads * p.d], 1)
+    k32 = turned32(k.reshape(p.T, p.kv_heads, p.d), table, at, axis, rot, layout) if rot else k.reshape(p.T, p.kv_heads, p.d).float()
+    want = {}
+    for name, new in (("K", k32), ("V", v.reshape(p.T, p.kv_heads, p.d).float())):
+        want[name] = appended(getattr(p, name + "8"), getattr(p, name + "_scales"), p.block, p.table, p.lengths, p.starts, p.page, new)
+    q = q[:, :heads * p.d].reshape(p.T, heads, p.d)
+    return R[:p.T], q, (turned32(q.double().float(), table, at, axis, rot, layout) if rot else q.float()), want
+
+
+def check(p, want):
+    for name in ("K", "V"):
+        same_bytes(p.dev[name + "8"], want[name][0], name)
+        assert torch.equal(p.dev[name + "_scales"].cpu(), want[name][1]), name + "_scales"
+
+
+# sequences (new, in use), heads, kv heads, d, page, block
+SHAPES = [
+    ("one token alone", [(1, 1)], 1, 1, 64, 16, 16),
+    ("one token into a block that has some", [(1, 21)], 4, 2, 128, 16, 16),
+    ("a step of a batch", [(1, 33), (1, 1), (1, 64), (0, 20), (1, 17)], 8, 8, 128, 16, 8),
+    ("a scale for every slot", [(5, 19), (3, 3)], 4, 3, 48, 6, 1),
+    ("a scale for two slots", [(9, 90)], 2, 5, 32, 10, 2),
+    ("odd pages", [(37, 95), (60, 61), (0, 5)], 6, 3, 80, 48, 12),
+    ("odd blocks", [(50, 77)], 2, 1, 16, 21, 7),
+    ("whole pages", [(130, 300), (64, 64), (1, 257)], 8, 2, 128, 64, 64),
+    ("blocks of more rows than are held", [(150, 260), (129, 129)], 4, 2, 256, 128, 128),
+    ("many sequences", [(i % 3, i % 3 + 5 * i % 40) for i in range(150)], 2, 2, 32, 16, 4),
+    ("a long chunk", [(700, 1500)], 8, 4, 64, 32, 32),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [HALVES, PAIRS])
+@pytest.mark.parametrize("name,sequences,heads,kv_heads,d,page,block", SHAPES, ids=[s[0] for s in SHAPES])
+def test_append(dtype, layout, name, sequences, heads, kv_heads, d, page, block):
+    p = Problem8(dtype, sequences, heads, kv_heads, d, page, block, seed=len(name)).on_gpu()
+    x = new_rows(p, len(name))
+    positions = torch.randint(0, 400, (p.T,), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    R, q, R32, want = run(p, x, d, layout, positions=positions)
+    check(p, want)
+    within(R, R32.double(), 2 * bound_of(q, dtype), "R")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [HALVES, PAIRS])
+@pytest.mark.parametrize("rot", [0, 2, 6, 16, 32, 40, 64])
+def test_parts_of_a_head(dtype, layout, rot):
+    p = Problem8(dtype, [(33, 70), (1, 6)], 3, 2, 64, 16, 16, seed=rot).on_gpu()
+    R, q, R32, want = run(p, new_rows(p), rot, layout)         # (positions: the slots)
+    check(p, want)
+    within(R, R32.double(), 2 * bound_of(q, dtype), "R")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [HALVES, PAIRS])
+@pytest.mark.parametrize("order", [SECTIONS, TURNS])
+@pytest.mark.parametrize("pairs", [[8, 12, 12], [32], [5, 20], [1, 2, 3, 4], [16, 16]])
+def test_axes(dtype, layout, order, pairs):
+    p = Problem8(dtype, [(21, 60), (40, 40), (1, 9)], 4, 2, 64, 12, 4, seed=1).on_gpu()
+    positions = torch.randint(0, 400, (len(pairs), p.T), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    R, q, R32, want = run(p, new_rows(p), 2 * sum(pairs), layout, pairs, order, positions)
+    check(p, want)
+    within(R, R32.double(), 2 * bound_of(q, dtype), "R")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_is_no_number_and_what_is_extreme(dtype):
+    """NaN and infinities become NaN and leave their block's other rows alone; scales end at 2^-117 and 2^119; zeros; numbers between two of e4m3."""
+    p = Problem8(dtype, [(64, 64)], 2, 1, 32, 16, 8, seed=4).on_gpu()
+    x = new_rows(p, spread=0.0)
+    x[3, 70] = math.nan
+    x[4, 97] = math.inf
+    x[5, 64:128] = -math.inf                      # (a whole row)
+    x[8:16] = 0.0
+    x[16:24] *= 2.0 ** -120
+    x[24:32] *= 2.0 ** 124
+    x[32:40] = 3.3e38 * torch.sign(x[32:40].float()).to(x.dtype)
+    x[40:48, 64:] = torch.arange(8 * 64).view(8, 64).to(x.dtype) * 448 / 512   # (ties among them)
+    x[48, 64], x[48:56, 65:96] = 448.0, 0.0       # the largest number of a scale, and the next one
+    x[56, 64], x[56:64, 65:96] = 450.0, 0.0
+    _, _, _, want = run(p, x, 0)
+    check(p, want)
+    got = p.dev["K_scales"].cpu()[p.table[0].long(), 0].flatten()
+    assert got[1] == 127 - 117 and got[4] == 127 + 119 and got[6] == 127 and got[7] == 128
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_block_that_fills_token_by_token(dtype):
+    """Growing and shrinking rows one after the other into one cache: scales only grow within a block, and what was there moves with them."""
+    p = Problem8(dtype, [(1, 1), (1, 30)], 2, 2, 48, 16, 16, seed=6, more_pages=4).on_gpu()
+    g = torch.Generator().manual_seed(7)
+    for step in range(40):
+        x = new_rows(p, step)
+        x = (x.float() * 2.0 ** float(torch.randint(-6, 7, (1,), generator=g))).to(x.dtype)
+        _, _, _, want = run(p, x, 16)
+        check(p, want)
+        for name in ("K", "V"):
+            setattr(p, name + "8", want[name][0])
+            setattr(p, name + "_scales", want[name][1])
+        p.lengths += 1
+        p.dev["lengths"] += 1
+
+
+def test_what_is_not_cached():
+    """Tokens before a sequence's first slot, pages that are none, rows that no sequence owns, no queries; K and V elsewhere stay as they were."""
+    p = Problem8("bf16", [(6, 40), (30, 50), (2, 20)], 4, 2, 64, 16, 16, seed=8)
+    p.lengths[0] = 2                              # (four of its six new tokens have no slot)
+    p.table[1, 2] = -5
+    p.table[2, 1] = p.pages
+    p.starts = torch.tensor([3, 9, 39, 41], dtype=torch.int32)
+    p.T = 45                                      # (rows 0 .. 2 and 41 .. 44 are nobody's)
+    p.on_gpu()
+    x = new_rows(p)
+    positions = torch.zeros(p.T, dtype=torch.int32) + 5
+    _, _, _, want = run(p, x, 64, positions=positions, heads=0)
+    check(p, want)
+
+
+def test_counts_in_no_order():
+    """Starts and lengths that mean nothing make no access outside the arrays: what lies around them stays."""
+    p = Problem8("bf16", [(9, 40), (30, 50), (2, 20)], 4, 2, 64, 16, 4, seed=9)
+    for starts, lengths in (([41, 0, 2 ** 31 - 1, -2 ** 31], [-5, 2 ** 31 - 1, 7]), ([0, 41, 0, 41], [64, 64, 64]), ([-9, 100, -100, 50], [1, 1, 1])):
+        p.starts, p.lengths = torch.tensor(starts, dtype=torch.int32), torch.tensor(lengths, dtype=torch.int32)
+        p.table[:] = torch.arange(p.pages, dtype=torch.int32)[:p.table.numel()].view(p.table.shape)
+        guarded = {}
+        p.on_gpu()
+        for name in ("K8", "V8", "K_scales", "V_scales"):
+            whole = torch.full((p.dev[name].numel() + 8192,), 91, dtype=torch.uint8, device="cuda")
+            guarded[name] = whole
+            whole[4096:-4096] = p.dev[name].flatten()
+        p.cache = attnw.AttnwByteCache(*(guarded[n][4096:] for n in ("K8", "V8", "K_scales", "V_scales")), p.dev["table"], p.dev["lengths"], p.batch, p.pages, p.max_pages,
+                                       p.page, p.block, p.kv_heads, p.d, attnw.ATTNW_BF16)
+        x = new_rows(p).cuda()
+        R, wide = torch.empty((p.T, 4, 64), dtype=torch.bfloat16, device="cuda"), 256
+        table = table_of(100, 64).cuda()
+        attnw.attnw_byte_cache_append(p.cache, x, x[:, wide:], x[:, wide + 128:], R, table, None, None, p.dev["starts"], p.T, 4, 64, 100, 512, 512, HALVES)
+        torch.cuda.synchronize()
+        for whole in guarded.values():
+            assert bool((whole[:4096] == 91).all()) and bool((whole[-4096:] == 91).all())
+
+
+def test_far_pages():
+    """Offsets past 2^32 bytes: the last pages of a pool of five GiB."""
+    pages, page, d, heads = 327680, 64, 64, 4
+    pool = torch.zeros(pages * page * d * heads, dtype=torch.uint8, device="cuda").view(pages, heads, page, d)
+    other = torch.zeros_like(pool)
+    scales, more = (torch.zeros((pages, heads, 2), dtype=torch.uint8, device="cuda") for _ in range(2))
+    table = torch.tensor([[pages - 1, 3, pages - 2]], dtype=torch.int32)
+    lengths, starts = torch.tensor([150], dtype=torch.int32), torch.tensor([0, 150], dtype=torch.int32)
+    dev = [v.cuda() for v in (table, lengths, starts)]
+    cache = attnw.AttnwByteCache(pool, other, scales, more, dev[0], dev[1], 1, pages, 3, page, 32, heads, d, attnw.ATTNW_F32)
+    x = torch.randn((150, 2 * heads * d), generator=torch.Generator().manual_seed(3))
+    x_dev = x.cuda()
+    attnw.attnw_byte_cache_append(cache, None, x_dev, x_dev[:, heads * d:], None, None, None, None, dev[2], 150, 0, 0, 0, 0, 2 * heads * d, HALVES)
+    torch.cuda.synchronize()
+    few = torch.tensor([[2, 1, 0]], dtype=torch.int32)         # the same three pages, by themselves
+    for got, got_scales, rows in ((pool, scales, x[:, :heads * d]), (other, more, x[:, heads * d:])):
+        empty = torch.zeros((3, heads, page, d), dtype=torch.uint8), torch.zeros((3, heads, 2), dtype=torch.uint8)
+        b, s = appended(*empty, 32, few, lengths, starts, page, rows.view(150, heads, d))
+        at = torch.tensor([pages - 2, 3, pages - 1], device="cuda")
+        same_bytes(got[at], b, "bytes")
+        assert torch.equal(got_scales[at].cpu(), s)
+        assert int(got[:3].max()) == 0 and int(got[4:pages - 2].max()) == 0
+
+
+def test_in_place_and_on_another_stream():
+    p = Problem8("bf16", [(20, 50)], 4, 2, 64, 16, 16, seed=10).on_gpu()
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn((20, 4 * 64), generator=g).to(torch.bfloat16)
+    kv = torch.randn((20, 4 * 64), generator=g).to(torch.bfloat16)
+    q_dev, kv_dev, table = q.cuda(), kv.cuda(), table_of(100, 64).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    attnw.attnw_byte_cache_append(p.cache, q_dev, kv_dev, kv_dev[:, 128:], q_dev, table, None, None, p.dev["starts"], 20, 4, 64, 100, 256, 256, PAIRS, side)
+    side.synchronize()
+    at = torch.arange(30, 50)[None]
+    within(q_dev.view(20, 4, 64), turned32(q.view(20, 4, 64), table.cpu(), at, [0] * 32, 64, PAIRS).double(), 2 * bound_of(q.view(20, 4, 64), "bf16"), "R")
+    k = turned32(kv[:, :128].reshape(20, 2, 64), table.cpu(), at, [0] * 32, 64, PAIRS)
+    for name, rows in (("K", k), ("V", kv[:, 128:].reshape(20, 2, 64).float())):
+        b, s = appended(getattr(p, name + "8"), getattr(p, name + "_scales"), 16, p.table, p.lengths, p.starts, 16, rows)
+        same_bytes(p.dev[name + "8"], b, name)
+        assert torch.equal(p.dev[name + "_scales"].cpu(), s)
+    assert DT["bf16"] == attnw.ATTNW_BF16

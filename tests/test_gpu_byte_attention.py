@@ -1,0 +1,209 @@
+"""Attention over a paged cache in 8 bits, against its definition in 64 bits on the values that the cache stands for (byte_util, paged_util)."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_13885_amd as attnw
+from byte_util import Problem8
+from gpu_util import require_gpu
+from paged_util import within
+from test_gpu_paged import RULES
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    require_gpu()
+
+
+def check(p):
+    O, lse = p.on_gpu().run_attention()
+    want, want_lse, off, lse_off = p.attention()
+    within(O[:p.T], want, off, "O")
+    within(lse[:p.T], want_lse, lse_off, "lse")
+    return O, lse
+
+
+# sequences (new, in use), heads, kv heads, d, page, block
+SHAPES = [
+    ("one token alone", [(1, 1)], 1, 1, 64, 16, 16),
+    ("one token, odd length", [(1, 777)], 8, 2, 128, 16, 16),
+    ("one token, a long row", [(1, 5001)], 4, 1, 64, 64, 32),
+    ("tokens of several lengths, some empty", [(1, 1), (0, 40), (1, 33), (1, 640), (0, 0), (1, 129)], 8, 4, 128, 32, 32),
+    ("a chunk at the start", [(37, 37)], 4, 4, 64, 16, 4),
+    ("a chunk over others", [(65, 300), (3, 259), (128, 128)], 8, 2, 128, 20, 10),
+    ("groups that blocks cut", [(19, 90), (5, 5)], 21, 3, 32, 7, 7),
+    ("more heads than a block has rows", [(2, 70), (1, 513)], 48, 1, 64, 128, 64),
+    ("a scale for every slot", [(4, 101), (70, 333)], 2, 1, 16, 5, 1),
+    ("a scale for two slots, more places than are kept on chip", [(2, 2600)], 2, 1, 16, 6, 2),
+    ("more places than are kept on chip", [(2, 2600)], 2, 1, 16, 1, 1),
+    ("a long chunk", [(300, 812)], 2, 1, 128, 48, 16),
+    ("many sequences", [(i % 3, i % 3 + 7 * i % 60) for i in range(150)], 4, 2, 32, 16, 8),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name,sequences,heads,kv_heads,d,page,block", SHAPES, ids=[s[0] for s in SHAPES])
+def test_attention(dtype, name, sequences, heads, kv_heads, d, page, block):
+    check(Problem8(dtype, sequences, heads, kv_heads, d, page, block, seed=len(name)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", range(16, 257, 16))
+def test_head_sizes(dtype, d):
+    check(Problem8(dtype, [(1, 190), (18, 75)], 4, 2, d, 16, 16 if d % 32 else 8, seed=d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name,more", RULES, ids=[r[0] for r in RULES])
+def test_rules(dtype, name, more):
+    check(Problem8(dtype, [(1, 410), (40, 333), (150, 420)], 8, 4, 64, 32, 16, seed=3, **more))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_see_nothing(dtype):
+    """A sequence of more tokens than slots: those before its first slot see the prefix or nothing."""
+    p = Problem8(dtype, [(4, 60)], 4, 2, 64, 16, more_pages=1)
+    p.lengths[0] = 2
+    O, lse = p.on_gpu().run_attention()
+    assert bool((O[:2] == 0).all()) and bool(torch.isneginf(lse[:2]).all())
+    p.sequences, p.starts, p.T, p.Q, p.batch = [(2, 2)], torch.tensor([0, 2], dtype=torch.int32), 2, p.Q[2:], 1
+    want, want_lse, off, lse_off = p.attention()
+    within(O[2:], want, off, "O")
+    within(lse[2:], want_lse, lse_off, "lse")
+    O, lse = Problem8(dtype, [(3, 0)], 4, 2, 64, 16, more_pages=1).on_gpu().run_attention()      # no slot at all
+    assert bool((O == 0).all()) and bool(torch.isneginf(lse).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 80, 192])
+def test_what_is_hidden_has_no_part(dtype, d):
+    """Keys, values and scales that a row does not see may hold anything: later tokens of its chunk, what lies in front of its window."""
+    p = Problem8(dtype, [(30, 300)], 4, 2, d, 16, 8, seed=5, window=40)
+    clean = p.on_gpu().run_attention()
+    slots = torch.arange(0, 300 - 30 - 40 - 16)
+    ids, row = p.table[0, slots // 16].long(), slots % 16
+    for name in ("K8", "V8"):
+        getattr(p, name)[ids, :, row] = 0x7f
+    for name in ("K_scales", "V_scales"):
+        getattr(p, name)[ids[:208], :, row[:208] // 8] = 255
+    again = p.restate().on_gpu().run_attention()
+    assert torch.equal(clean[0], again[0]) and torch.equal(clean[1], again[1])
+    # NaN in the values of one of the chunk's tokens: the rows from it on have it, in that column
+    p = Problem8(dtype, [(30, 300)], 4, 2, d, 16, 8, seed=5)
+    clean = p.on_gpu().run_attention()
+    p.V8[p.table[0, 285 // 16].long(), 1, 285 % 16, 7] = 0xff
+    O, lse = p.on_gpu().run_attention()
+    want = clean[0].clone()
+    want[15:, 2:, 7] = math.nan
+    assert torch.equal(O.isnan(), want.isnan()) and torch.equal(lse, clean[1])
+    keep = ~want.isnan()
+    assert torch.equal(O[keep], want[keep])
+    # in a key: the rows that see it are NaN, the others as they were
+    p = Problem8(dtype, [(30, 300)], 4, 2, d, 16, 8, seed=5)
+    p.K8[p.table[0, 285 // 16].long(), 0, 285 % 16, d - 1] = 0x7f
+    O, lse = p.on_gpu().run_attention()
+    assert bool(O[15:, :2].isnan().all()) and bool(lse[15:, :2].isnan().all())
+    for got, was in ((O, clean[0]), (lse, clean[1])):
+        assert torch.equal(got[:15], was[:15]) and torch.equal(got[:, 2:], was[:, 2:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_at_their_ends(dtype):
+    """The least and greatest scales that appending makes, in blocks beside ordinary ones: values of either, keys of the least (a score of the others is then the only one)."""
+    p = Problem8(dtype, [(5, 120), (33, 64)], 4, 2, 64, 16, 4, seed=11)
+    p.V_scales[p.table[0, 2].long()] = 127 - 117
+    p.K_scales[p.table[0, 3].long()] = 127 - 117
+    check(p.restate())
+    p.V_scales[p.table[0, :4].long()] = 127 + 100
+    check(p.restate())
+
+
+@pytest.mark.parametrize("scale", [-0.125, 0.0, 3.0])
+def test_scales_of_either_sign(scale):
+    for dtype in ("bf16", "f32"):
+        p = Problem8(dtype, [(1, 90), (20, 333)], 4, 2, 64, 16, 16, seed=12)
+        p.scale = scale
+        O, lse = p.on_gpu().run_attention()
+        q = p.scale
+        p.scale = abs(q)
+        if q < 0:
+            p.Q = -p.Q
+        want, want_lse, off, lse_off = p.attention()
+        within(O[:p.T], want, off, "O")
+        within(lse[:p.T], want_lse, lse_off, "lse")
+
+
+def test_padded_rows_and_rows_of_nobody():
+    """Queries in wider rows; rows that no sequence owns are not written."""
+    p = Problem8("bf16", [(3, 50), (9, 70)], 4, 2, 64, 16, 16, seed=13, q_pad=72)
+    O, lse = check(p)
+    q = Problem8("bf16", [(3, 50), (9, 70)], 4, 2, 64, 16, 16, seed=13, q_pad=72).on_gpu()
+    q.T = 16
+    q.dev["starts"] = torch.tensor([2, 5, 14], dtype=torch.int32, device="cuda")
+    q.dev["Q"] = torch.cat([torch.full((2, q.q_stride), math.nan, dtype=torch.bfloat16), q.Q, torch.full((2, q.q_stride), math.nan, dtype=torch.bfloat16)]).cuda()
+    P, lse2 = q.run_attention()
+    assert torch.equal(P[2:14], O) and torch.equal(lse2[2:14], lse)
+    assert bool((P[:2] == 7).all()) and bool((P[14:] == 7).all()) and bool((lse2[:2] == 7).all()) and bool((lse2[14:] == 7).all())
+
+
+def test_counts_and_pages_in_no_order():
+    """Whatever lengths, starts and page ids hold, the call ends and what lies around its outputs stays."""
+    for starts, lengths in (([41, 0, 2 ** 31 - 1, -2 ** 31], [-5, 2 ** 31 - 1, 7]), ([0, 41, 0, 41], [64, 64, 64]), ([-9, 100, -100, 50], [1, 1, 1])):
+        p = Problem8("bf16", [(9, 40), (30, 50), (2, 20)], 4, 2, 64, 16, 4, seed=9)
+        p.starts, p.lengths = torch.tensor(starts, dtype=torch.int32), torch.tensor(lengths, dtype=torch.int32)
+        p.table[0] = torch.tensor([-1, 2 ** 31 - 1, p.pages, 5][:p.table.shape[1]], dtype=torch.int32)
+        p.on_gpu()
+        O, lse = torch.full((p.T + 64, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((p.T + 64, 4), 7.0, device="cuda")
+        size = attnw.attnw_byte_paged_workspace(p.cache, p.T, 4)
+        work = torch.full((size + 4096,), 91, dtype=torch.uint8, device="cuda")
+        attnw.attnw_byte_paged_attention(p.cache, p.rule, p.dev["Q"], O, lse, p.dev["starts"], p.T, 4, 256, work, size)
+        torch.cuda.synchronize()
+        assert bool((O[p.T:] == 7).all()) and bool((lse[p.T:] == 7).all()) and bool((work[size:] == 91).all())
+
+
+def test_far_pages():
+    """Offsets past 2^32 bytes: keys and values in the last pages of a pool of five GiB."""
+    p = Problem8("bf16", [(40, 150), (1, 64)], 8, 4, 64, 64, 32, seed=14, garbage=False)
+    near = p.on_gpu().run_attention()
+    pages = 327680
+    far = {n: torch.zeros((pages, 4, 64, 64), dtype=torch.uint8, device="cuda") for n in ("K8", "V8")}
+    far.update({n: torch.zeros((pages, 4, 2), dtype=torch.uint8, device="cuda") for n in ("K_scales", "V_scales")})
+    for n, x in far.items():
+        x[pages - p.pages:] = p.dev[n]
+    table = p.dev["table"] + (pages - p.pages)
+    p.cache = attnw.AttnwByteCache(far["K8"], far["V8"], far["K_scales"], far["V_scales"], table, p.dev["lengths"], p.batch, pages, p.max_pages, 64, 32, 4, 64, attnw.ATTNW_BF16)
+    again = p.run_attention()
+    assert torch.equal(near[0], again[0]) and torch.equal(near[1], again[1])
+
+
+def test_streams_and_workspaces():
+    """Two calls on two streams at once, a workspace each; results do not change from call to call."""
+    p = Problem8("bf16", [(1, 900), (33, 800), (1, 2000)], 8, 2, 128, 16, 16, seed=15).on_gpu()
+    first = p.run_attention()
+    d, size = p.dev, attnw.attnw_byte_paged_workspace(p.cache, p.T, p.heads)
+    out = []
+    torch.cuda.synchronize()
+    for _ in range(2):
+        s = torch.cuda.Stream()
+        O, lse, work = torch.empty_like(first[0]), torch.empty_like(first[1]), torch.empty(size, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        out.append((s, O, lse, work))
+    for _ in range(5):
+        for s, O, lse, work in out:
+            attnw.attnw_byte_paged_attention(p.cache, p.rule, d["Q"], O, lse, d["starts"], p.T, p.heads, p.q_stride, work, size, s)
+    torch.cuda.synchronize()
+    for _, O, lse, _ in out:
+        assert torch.equal(O, first[0]) and torch.equal(lse, first[1])
+
+
+def test_without_lse():
+    p = Problem8("f32", [(1, 90), (20, 333)], 4, 2, 64, 16, 16, seed=16).on_gpu()
+    O, _ = p.run_attention()
+    size = attnw.attnw_byte_paged_workspace(p.cache, p.T, 4)
+    P, work = torch.empty_like(O), torch.empty(size, dtype=torch.uint8, device="cuda")
+    attnw.attnw_byte_paged_attention(p.cache, p.rule, p.dev["Q"], P, None, p.dev["starts"], p.T, 4, p.q_stride, work, size)
+    torch.cuda.synchronize()
+    assert torch.equal(O, P)
