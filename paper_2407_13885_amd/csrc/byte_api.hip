@@ -220,7 +220,7 @@ int64_t attnw_byte_paged_workspace(const attnw_byte_cache* cache, int64_t tokens
     a.cache = view(&c, 1);
     a.tokens = tokens;
     a.heads = heads;
-    return attnw::byte_workspace(a, scales(cache));
+    return attnw::byte_workspace(a);
 }
 
 int attnw_byte_paged_attention(const attnw_byte_cache* cache, const attnw_rule* rule, const void* Q, void* O, float* lse, const int32_t* starts, int64_t tokens,
@@ -249,7 +249,7 @@ int attnw_byte_paged_attention(const attnw_byte_cache* cache, const attnw_rule* 
     a.heads = heads;
     a.q_stride = q_stride;
     const ScalesView s = scales(cache);
-    const int64_t need = attnw::byte_workspace(a, s);
+    const int64_t need = attnw::byte_workspace(a);
     if (need > 0 && !workspace) return ATTNW_ERR_NULL;
     if (workspace_bytes < need) return ATTNW_ERR_WORKSPACE;
     if (!cache_aligned(&c) || !aligned(Q, 16) || !aligned(O, 16) || !aligned(lse, 4) || !aligned(starts, 4) || !aligned(workspace, 16) || !aligned(rule->slopes, 4) ||

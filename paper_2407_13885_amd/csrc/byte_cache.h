@@ -32,5 +32,64 @@ template <bool HIGH> __device__ __forceinline__ uint32_t pack_e4m3(float lo, flo
 }
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) { return pack_e4m3<true>(c, d, pack_e4m3<false>(a, b, 0)); }
 
+// Four elements as bf16, times a power of 2; eight of them, the operand of a matrix instruction.
+__device__ __forceinline__ u32x2 bf16_of(uint32_t w, float scale)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
+#else
+    (void)w;
+    (void)scale;
+    return u32x2{0u, 0u};
+#endif
+}
+__device__ __forceinline__ u32x4 bf16_of(uint32_t a, uint32_t b, float scale) { return u32x4_of(bf16_of(a, scale), bf16_of(b, scale)); }
+
+// 8 numbers as bf16: as they are, or their three parts
+template <int PARTS> struct Parts { u32x4 of[PARTS]; };
+template <int PARTS> __device__ __forceinline__ Parts<PARTS> parts_of(const float (&y)[8])
+{
+    Parts<PARTS> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = y[2 * i], b = y[2 * i + 1];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const uint32_t w = pack_bf16x2(a, b);
+            r.of[p][i] = w;
+            a -= bf16_lo_to_f32(w);
+            b -= bf16_hi_to_f32(w);
+        }
+    }
+    return r;
+}
+// (the smallest part first)
+template <int PARTS> __device__ __forceinline__ void multiply_parts(f32x4& acc, const u32x4& x, const Parts<PARTS>& y)
+{
+#pragma unroll
+    for (int p = PARTS - 1; p >= 0; --p) mma16(acc, x, y.of[p]);
+}
+
+// Where the keys of a place of 2^grain lie, and the bytes of their scales in the upper 16 bits.
+__device__ __forceinline__ int64_t slot_place(const CacheView& c, const ScalesView& s, const int32_t* pages_of, int kv_head, int j)
+{
+    const uint32_t p = quotient((uint32_t)j, c.page);
+    const int32_t id = max(0, min(pages_of[p], c.pages - 1)), row = j - (int)(p * c.page.d);
+    const int64_t scale = ((int64_t)id * c.kv_heads + kv_head) * s.per_page + quotient(row, s.block);
+    const uint64_t at = (uint64_t)(uint32_t)id * c.page_bytes + (uint32_t)kv_head * c.head_bytes + (uint32_t)row * (uint32_t)c.row_bytes;
+    return (int64_t)(at | (uint64_t)s.K[scale] << 48 | (uint64_t)s.V[scale] << 56);
+}
+__device__ __forceinline__ int64_t place_offset(int64_t place) { return place & (((int64_t)1 << 48) - 1); }
+__device__ __forceinline__ float key_scale(uint32_t high) { return scale_of(high >> 16 & 255); }
+__device__ __forceinline__ float value_scale(uint32_t high) { return scale_of(high >> 24); }
+// 2^grain slots lie in one page and share their scales
+inline int key_grain(const CacheView& c, const ScalesView& s)
+{
+    CacheView of = c;
+    of.page = s.block;                            // (it divides the page)
+    return key_grain(of);
+}
+
 }  // namespace
 }  // namespace attnw

@@ -3,10 +3,11 @@
 
 namespace attnw {
 
-int64_t byte_workspace(const PagedArgs& p, const ScalesView&) { return rows_workspace(p); }
+int64_t byte_workspace(const PagedArgs& p) { return prefers_byte_tiles(p) ? byte_tiles_workspace(p) : rows_workspace(p); }
 
 hipError_t launch_byte_attention(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
 {
+    if (prefers_byte_tiles(p)) return launch_byte_tiles(p, scales, stream);
     return p.dt == DType::F32 ? launch_byte_rows_f32(p, scales, stream) : launch_rows<uint16_t>(p, scales, stream);
 }
 

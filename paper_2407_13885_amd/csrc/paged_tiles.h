@@ -8,56 +8,72 @@
 //
 // What bounds it: the matrix unit, beside a vector unit that makes an exponential for every 4 d operations.  Measured: 2048 tokens over 14336 slots, 32
 // heads on 8 of 128, causal, 482 to 514 us (1.07 to 1.0 PFLOP/s); fp32 ragged chunks of d = 80 with bias, window and prefix 48 us.
+//
+// BYTES: a cache in 8 bits (byte_cache.h).  Two tiles of keys, then two of values, come as they lie in memory; the wave that brought 16 bytes a lane makes bf16 of them, scales
+// included, where the other kernels have the rows themselves.  From there on everything is the same; fp32 queries and weights are three bf16 parts each.
 #pragma once
 
 #include "paged_attention.h"
+#include "byte_cache.h"
 
 namespace attnw {
 namespace {
 
-
-template <typename T, int UB> struct TilesCfg {
-    static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int NX = !F32 && UB <= 5 ? 2 : 1;         // blocks of 16 rows of a wave
+template <typename T, int UB, bool BYTES = false> struct TilesCfg {
+    static constexpr bool F32 = sizeof(T) == 4 && !BYTES;      // on chip
+    static constexpr int PARTS = sizeof(T) == 4 && BYTES ? 3 : 1;
+    static constexpr int NX = !F32 && PARTS == 1 && UB <= 5 ? 2 : 1;         // blocks of 16 rows of a wave
     static constexpr int NW = F32 || UB <= 5 ? 4 : 8;          // waves
     static constexpr int ROWS = 16 * NX * NW, UNIT = F32 ? 64 : 128, KT = F32 ? 16 : 32;   // keys of a tile
     static constexpr int DB = UB * 64, CPR = UB * 4, TILE = KT * DB, XFERS = TILE / 1024, XW = (XFERS + NW - 1) / NW;
-    static constexpr int COLS = DB / (int)sizeof(T), CB = COLS / 16;
+    static constexpr int COLS = DB / (F32 ? 4 : 2), CB = COLS / 16;
     static constexpr bool PIPE = NX == 2;         // registers for the scores of two tiles
     static constexpr int RING = 4;                // tiles of K, and of V, on chip
-    static constexpr int LDS = 2 * RING * TILE + kPlaces * 8 + RING * 32;
+    static constexpr int RAW = BYTES ? TILE : 0, XR = (2 * UB + NW - 1) / NW;   // two tiles in bytes, and their transfers for a wave
+    static constexpr int PLACES = BYTES ? kPlaces / 2 : kPlaces;
+    static constexpr int LDS = RAW + 2 * RING * TILE + PLACES * 8 + RING * 32;
     static constexpr int PER_CU = NW == 4 && LDS <= 80 * 1024 ? 2 : 1;
-    static_assert(2 * RING * TILE <= kDirectLds, "reach of direct transfers");
+    static_assert((BYTES ? RAW : 2 * RING * TILE) <= kDirectLds, "reach of direct transfers");
 };
 
-// SHORT: by how many bytes a row in memory is shorter than on chip (up to d = 160: 0 or 32; beyond, -1: known at run time).
-template <typename T, int UB, int SHORT, int MODE, bool UNIFORM, int THREADS = 64 * TilesCfg<T, UB>::NW, int BLOCKS = (UB > (TilesCfg<T, UB>::F32 ? 8 : 5)) ? 1 : 2>
+struct ByteAttendArgs : AttendArgs {
+    ScalesView scales;
+};
+template <bool BYTES> struct TilesArgs { using type = AttendArgs; };
+template <> struct TilesArgs<true> { using type = ByteAttendArgs; };
+
+// SHORT: by how many bytes a row in memory (of bytes: as bf16) is shorter than on chip (up to d = 160: 0 or 32; beyond, -1: known at run time).
+template <typename T, int UB, int SHORT, int MODE, bool UNIFORM, bool BYTES = false, int THREADS = 64 * TilesCfg<T, UB, BYTES>::NW,
+          int BLOCKS = (UB > (TilesCfg<T, UB, BYTES>::F32 ? 8 : 5)) ? 1 : 2>
 __global__ __launch_bounds__(THREADS, BLOCKS)
-void paged_tiles_kernel(AttendArgs a, int grain)
+void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
 {
-    using C = TilesCfg<T, UB>;
+    using C = TilesCfg<T, UB, BYTES>;
     using L = RowLayout<UB>;
     constexpr int NW = C::NW, DB = C::DB, CPR = C::CPR, TILE = C::TILE, XFERS = C::XFERS, XW = C::XW, CB = C::CB, RING = C::RING, G = UB, NX = C::NX, KT = C::KT, NK = KT / 16;
+    constexpr int PARTS = C::PARTS;
     constexpr bool F32 = C::F32;
+    typedef std::conditional_t<BYTES, uint16_t, T> E;          // an element on chip
     __shared__ __align__(1024) char lds[C::LDS];
-    char* const k_lds = lds;
-    char* const v_lds = lds + RING * TILE;
-    int64_t* const places = reinterpret_cast<int64_t*>(lds + 2 * RING * TILE);
-    uint32_t* const lost_in = reinterpret_cast<uint32_t*>(lds + 2 * RING * TILE + kPlaces * 8);   // [tile of V][wave]: what is no number there
+    char* const k_lds = lds + C::RAW;
+    char* const v_lds = k_lds + RING * TILE;
+    int64_t* const places = reinterpret_cast<int64_t*>(k_lds + 2 * RING * TILE);
+    uint32_t* const lost_in = reinterpret_cast<uint32_t*>(k_lds + 2 * RING * TILE + C::PLACES * 8);   // [tile of V][wave]: what is no number there
     if constexpr (UNIFORM) grain = 4;
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
     const uint32_t k_at = lds_offset_of(k_lds);
-    const int rb = SHORT >= 0 ? DB - SHORT : a.cache.row_bytes;
+    const int rb = SHORT >= 0 ? DB - SHORT : a.cache.row_bytes * (BYTES ? 2 : 1);
+    const int qb = PARTS == 3 ? 2 * rb : rb;      // of a row of Q and O
 
     Walk<C::ROWS> walk(a, lane);
     if (walk.at >= walk.end) return;
 
     // A score as exponent of 2: c times the product (a negative scale negates Q), or by the map.
     const float c = MODE != kPlain ? 1.0f : fabsf(a.rule.scale) * kLog2e;
-    const uint32_t sign_flip = MODE == kPlain && a.rule.scale < 0.0f ? Mma<T>::kSignMask : 0u;
-    const ScoreMap<(MODE & kCap) != 0, F32> map(a.rule);
+    const uint32_t sign_flip = MODE == kPlain && a.rule.scale < 0.0f ? Mma<E>::kSignMask : 0u;
+    const ScoreMap<(MODE & kCap) != 0, sizeof(T) == 4> map(a.rule);
 
     // ---- per-lane places of the operand fragments ------------------------------------------------------------------------
     const char* const krow = k_lds + l16 * DB;
@@ -88,8 +104,11 @@ void paged_tiles_kernel(AttendArgs a, int grain)
             return u32x4_of(lds_read_tr16(p), lds_read_tr16(p + 16 * DB));
         }
     };
-    auto multiply = [&](f32x4& acc, const u32x4& x, const u32x4& y) __attribute__((always_inline)) {
-        if constexpr (F32) {
+    typedef std::conditional_t<PARTS == 1, u32x4, Parts<PARTS>> Operand;
+    auto multiply = [&](f32x4& acc, const u32x4& x, const Operand& y) __attribute__((always_inline)) {
+        if constexpr (PARTS != 1) {
+            multiply_parts(acc, x, y);
+        } else if constexpr (F32) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[i]), __uint_as_float(y[i]), acc, 0, 0, 0);
         } else {
@@ -112,17 +131,27 @@ void paged_tiles_kernel(AttendArgs a, int grain)
         const int lane_of_rows = apart(lane), row_of_lane = lane_of_rows & 15, chunk_of_lane = lane_of_rows >> 4 & 3;
         int query[NX];
         float slope[NX];
-        u32x4 qf[NX][G];
+        Operand qf[NX][G];
 #pragma unroll
         for (int x = 0; x < NX; ++x) {
             const int row = row0 + min(wave * 16 * NX + 16 * x + row_of_lane, rows - 1);
             const int token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
             query[x] = base + token;
             slope[x] = MODE & kBias ? a.rule.slopes[head] * kLog2e : 0.0f;
-            const char* q = a.Q + (int64_t)(seq.first + token) * a.q_stride + (int64_t)head * rb;
+            const char* q = a.Q + (int64_t)(seq.first + token) * a.q_stride + (int64_t)head * qb;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const int ch = 4 * g + chunk_of_lane;
+                if constexpr (PARTS != 1) {       // (zeros behind a row's end: the key has its first chunks there once more, nothing infinite, and NaN where it is NaN anyway)
+                    const bool inside = ch * 16 < rb;
+                    const f32x4 lo = *reinterpret_cast<const f32x4*>(q + (inside ? ch * 32 : 0)), hi = *reinterpret_cast<const f32x4*>(q + (inside ? ch * 32 + 16 : 0));
+                    float y[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = inside ? lo[i] : 0.0f, y[4 + i] = inside ? hi[i] : 0.0f;
+                    qf[x][g] = parts_of<PARTS>(y);
+#pragma unroll
+                    for (int n = 0; n < PARTS; ++n) qf[x][g].of[n] ^= sign_flip;
+                } else
                 qf[x][g] = (SHORT == 0 ? *reinterpret_cast<const u32x4*>(q + ch * 16) : query_chunk<T>(q, ch, CPR, rb)) ^ sign_flip;
             }
         }
@@ -144,7 +173,8 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 
         // weights as the operand of the second product
         auto operand = [&](const float (&y)[4 * NK]) __attribute__((always_inline)) {
-            if constexpr (F32) return u32x4{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
+            if constexpr (PARTS != 1) return parts_of<PARTS>(y);
+            else if constexpr (F32) return u32x4{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
             else return u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
         };
         // a tile out of buffer `buf`, one step after the other
@@ -187,7 +217,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 }
             }
             float p[NX][4 * NK];
-            u32x4 pw[NX];
+            Operand pw[NX];
 #pragma unroll
             for (int x = 0; x < NX; ++x) {
                 float top = max3(y[x][0], y[x][1], fmaxf(y[x][2], y[x][3]));
@@ -210,6 +240,30 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 u32x4 bad = *reinterpret_cast<const u32x4*>(lost_in + buf * 8);
                 if constexpr (NW == 8) bad |= *reinterpret_cast<const u32x4*>(lost_in + buf * 8 + 4);
                 if (__builtin_amdgcn_readfirstlane(bad[0] | bad[1] | bad[2] | bad[3]) != 0) {   // (lost_part)
+                    if constexpr (BYTES) {        // (NaN, whatever the weight)
+                        u32x4 so[NX];
+#pragma unroll
+                        for (int x = 0; x < NX; ++x) {
+                            const Sight sight(query[x], a.rule, prefix, past);
+                            float some[4 * NK];
+#pragma unroll
+                            for (int i = 0; i < 4 * NK; ++i) some[i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? 0.0f : 1.0f;
+                            so[x] = parts_of<1>(some).of[0];
+                        }
+#pragma unroll
+                        for (int i = 0; i < CB; ++i) {
+                            const u32x4 v = v_frag(buf, i), rest_of = without_lost<E>(v), lost_of = lost_as_one<E, kAny>(v);
+#pragma unroll
+                            for (int x = 0; x < NX; ++x) {
+                                f32x4 lost = {0.0f, 0.0f, 0.0f, 0.0f};
+                                mma16(lost, lost_of, so[x]);
+                                multiply(oacc[i][x], rest_of, pw[x]);
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) oacc[i][x][r] = lost[r] > 0.0f ? __builtin_nanf("") : oacc[i][x][r];
+                            }
+                        }
+                        return;
+                    } else {
                     u32x4 so[NX], no[NX];
 #pragma unroll
                     for (int x = 0; x < NX; ++x) {
@@ -235,6 +289,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                         }
                     }
                     return;
+                    }
                 }
             }
 #pragma unroll
@@ -242,6 +297,54 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 const u32x4 v = v_frag(buf, i);
 #pragma unroll
                 for (int x = 0; x < NX; ++x) multiply(oacc[i][x], v, pw[x]);
+            }
+        };
+
+        // ---- a cache in 8 bits: two tiles of K or V on their way.  A wave brings pieces of 1 KiB, as many as its lanes, and makes bf16 of what it brought itself --------
+        // tiles tile, tile + 1 (of 32 keys from key 0 on; past `last` that one), slots from k0 on in `places`, past k1 the last
+        auto bring = [&](bool v, int tile, int last_tile, int k0, int k1) __attribute__((always_inline)) {
+            if constexpr (BYTES) {
+                const int lane_here = apart(lane), wave_here = apart_uniform(wave);
+                const char* const from = v ? a.cache.V : a.cache.K;
+#pragma unroll
+                for (int j = 0; j < C::XR; ++j) {
+                    const int y = wave_here + NW * j;
+                    if (2 * UB % NW != 0 && y >= 2 * UB) continue;
+                    const int x = (y >= UB ? y - UB : y) * 64 + lane_here, key = x / (2 * UB), at = (x - key * (2 * UB)) * 16;
+                    const int slot = min(min(tile + (y >= UB ? 1 : 0), last_tile) * KT + key, k1 - 1) - k0;
+                    dma16_untracked(from + place_offset(places[slot >> grain]) + (slot & ((1 << grain) - 1)) * (rb / 2) + (SHORT == 0 || at < rb / 2 ? at : at - rb / 2),
+                                    (uint32_t)uniform((int)(k_at - C::RAW + y * 1024)));
+                }
+            }
+        };
+        // the same two, which have arrived, into the ring; of V also whether something is no number
+        auto settle = [&](bool v, int tile, int last_tile, int k0, int k1, int ring0) __attribute__((always_inline)) {
+            if constexpr (BYTES) {
+                const int lane_here = apart(lane), wave_here = apart_uniform(wave);
+                uint32_t bad[2] = {0, 0};
+#pragma unroll
+                for (int j = 0; j < C::XR; ++j) {
+                    const int y = wave_here + NW * j;
+                    if (2 * UB % NW != 0 && y >= 2 * UB) continue;
+                    const int second = y >= UB ? 1 : 0, x = (y - second * UB) * 64 + lane_here, key = x / (2 * UB), c = (x - key * (2 * UB)) * 2;
+                    const int slot = min(min(tile + second, last_tile) * KT + key, k1 - 1) - k0;
+                    const uint32_t high = reinterpret_cast<const uint32_t*>(places)[2 * (slot >> grain) + 1];
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + y * 1024 + lane_here * 16);
+                    const float scale = v ? value_scale(high) : key_scale(high);
+                    const u32x4 lo = bf16_of(w[0], w[1], scale), hi = bf16_of(w[2], w[3], scale);
+                    char* const row = (v ? v_lds : k_lds) + ((ring0 + second) & (RING - 1)) * TILE + key * DB;
+                    *reinterpret_cast<u32x4*>(row + (v ? v_chunk(key, c) : c ^ L::k_chunk(key)) * 16) = lo;
+                    *reinterpret_cast<u32x4*>(row + (v ? v_chunk(key, c + 1) : (c + 1) ^ L::k_chunk(key)) * 16) = hi;
+                    if (v) bad[second] |= any_lost<E>(lo) | any_lost<E>(hi);
+                }
+                if (v) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t some = __builtin_amdgcn_ballot_w64(bad[k] != 0) != 0 ? 1u : 0u;
+                        if (lane_here == 0) lost_in[((ring0 + k) & (RING - 1)) * 8 + wave_here] = some;
+                    }
+                }
+                wait_lds();                       // (what has been read may be brought over)
             }
         };
 
@@ -301,16 +404,45 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 wait_vmem();
                 __syncthreads();                  // (and the wave's fragments have left the buffers)
             };
+            // (bytes: K of tiles t + 4 and t + 5 come while tile t is made, t even, V of t + 1 and t + 2 while t + 1 is)
+            auto bring_pair = [&](bool v, int t) __attribute__((always_inline)) { bring(v, wa + t, wb - 1, k0, wb * 32); };
+            auto settle_pair = [&](bool v, int t) __attribute__((always_inline)) {
+                arrived<0>();
+                settle(v, wa + t, wb - 1, k0, wb * 32, t & (RING - 1));
+            };
             __syncthreads();                      // (what the ring held has been read)
+            if constexpr (BYTES) {
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {     // K of tiles 0 to 3, V of 0 and 1
+                    bring_pair(i == 2, i == 1 ? 2 : 0);
+                    settle_pair(i == 2, i == 1 ? 2 : 0);
+                }
+            } else {
             look_up(0);
             request(-4, 0);                       // K of tiles 0, 1
             request(-4, 1);
             request(-2, 0);                       // 2, 3
             request(-2, 1);
             request(-1, 2);                       // V of tile 0
+            }
             end_of_pair();
             if (!active) {                        // (a wave without rows only moves tiles)
                 __syncthreads();
+                if constexpr (BYTES) {
+                    for (int t = 0; t < n_tiles - 1; ++t) {
+                        if (t % 2 == 0) {
+                            bring_pair(false, t + 4);
+                            settle_pair(false, t + 4);
+                            bring_pair(true, t + 1);
+                        } else {
+                            settle_pair(true, t);
+                            end_of_pair();
+                        }
+                    }
+                    if (n_tiles % 2 == 0) settle_pair(true, n_tiles - 1);
+                    end_of_pair();
+                    return;
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) request(0, i);
                 for (int t = 1; t < n_tiles - 1; ++t) {
@@ -400,8 +532,12 @@ void paged_tiles_kernel(AttendArgs a, int grain)
             };
             Scores s = scores(0, 0), sn = scores(1, 1);
             __syncthreads();
+            if constexpr (BYTES) {
+                bring_pair(false, 4);
+            } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) request(0, i);
+            }
             {
                 const float top[2] = {fmaxf(largest(s, 0), largest(sn, 0)), fmaxf(largest(s, 1), largest(sn, 1))};
                 follow(top, 0.0f, false);
@@ -415,6 +551,10 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 }
             }
             s = sn;
+            if constexpr (BYTES) {
+                settle_pair(false, 4);
+                bring_pair(true, 1);
+            }
             u32x4 kf[KF], vf[RV];
 #pragma unroll
             for (int f = 0; f < KF; ++f) kf[f] = k_frag(2, f);
@@ -425,6 +565,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 constexpr int STEPS = 2 * (KF + CB), OPS = 8 + 32 + 16 + (MODE != kPlain ? 0 : 8);
                 Weights pw;
                 float pn[2][8], sum[2], top[2];
+                if constexpr (BYTES && BUF % 2 == 0) bring_pair(false, t + 4);
                 auto vector_op = [&](auto oc) __attribute__((always_inline)) {
                     constexpr int I = decltype(oc)::value;
                     if constexpr (I < 8) {
@@ -468,7 +609,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                         vector_op(IC<I * OPS / STEPS + decltype(jc)::value>{});
                     });
                     // (transfers between the steps: a wave that issues them in a row waits 50 cycles for each)
-                    if constexpr (BUF % 2 == 0 && I % 2 == 0 && I / 2 < 4 * XW) transfer(t, I / 2 % XW, I / 2 / XW);
+                    if constexpr (!BYTES && BUF % 2 == 0 && I % 2 == 0 && I / 2 < 4 * XW) transfer(t, I / 2 % XW, I / 2 / XW);
                     __builtin_amdgcn_sched_barrier(0);
                 });
                 static_assert(2 * CB >= KF && 8 * XW <= STEPS);
@@ -483,6 +624,14 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 #pragma unroll
                     for (int r = 0; r < 8; ++r) p[x][r] = pn[x][r];
                 follow(top, kLazy, true);
+                if constexpr (BYTES) {
+                    if constexpr (BUF % 2 == 0) {
+                        settle_pair(false, t + 4);
+                        bring_pair(true, t + 1);
+                    } else {
+                        settle_pair(true, t);
+                    }
+                }
                 if constexpr (BUF % 2 == 1) end_of_pair();
             };
             for (int t = 1;;) {
@@ -496,6 +645,8 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 if (t % 16 == 0) look_up(t);
                 tile(t++, IC<0>{});
             }
+            if constexpr (BYTES)
+                if (n_tiles % 2 == 0) settle_pair(true, n_tiles - 1);
             end_of_pair();
             // ---- the last two tiles ---------------------------------------------------------------------------------------------------------
             output((n_tiles - 2) & 3, pack());
@@ -512,12 +663,13 @@ void paged_tiles_kernel(AttendArgs a, int grain)
 
         // keys from .. to - 1, which begin a place
         auto sweep = [&](int from, int to, bool near) __attribute__((always_inline)) {
-            const int most = kPlaces << grain;    // (a whole number of places of the plan)
+            const int most = C::PLACES << grain;  // (a whole number of places of the plan)
             for (int k0 = from; k0 < to;) {
                 const int k1 = min(to, k0 + most);
                 __syncthreads();                  // (the places, and the tiles, of what was before have been read)
                 for (int i = threadIdx.x; i < (k1 - k0 + (1 << grain) - 1) >> grain; i += 64 * NW)
-                    places[i] = slot_offset(a.cache, pages_of, kv_head, k0 + (i << grain));
+                    if constexpr (BYTES) places[i] = slot_place(a.cache, a.scales, pages_of, kv_head, k0 + (i << grain));
+                    else places[i] = slot_offset(a.cache, pages_of, kv_head, k0 + (i << grain));
                 wait_vmem();
                 __syncthreads();
                 // a transfer of tile t, by lanes: any pages; slots past the end are read as the last
@@ -531,6 +683,37 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                 };
                 // tiles ta .. tb - 1 one after the other
                 auto run_alone = [&](int ta, int tb) __attribute__((always_inline)) {
+                    if constexpr (BYTES) {
+                        const int n = tb - ta;
+                        auto bring_pair = [&](bool v, int i) __attribute__((always_inline)) { bring(v, ta + i, tb - 1, k0, k1); };
+                        auto settle_pair = [&](bool v, int i) __attribute__((always_inline)) {
+                            arrived<0>();
+                            settle(v, ta + i, tb - 1, k0, k1, i & (RING - 1));
+                        };
+                        __syncthreads();
+#pragma unroll
+                        for (int v = 0; v < 2; ++v) {
+                            bring_pair(v, 0);
+                            settle_pair(v, 0);
+                        }
+#pragma clang loop unroll(disable)
+                        for (int i = 0; i < n; ++i) {
+                            const bool even = i % 2 == 0, more = even ? i + 2 < n : i + 1 < n;
+                            if (even) {
+                                __syncthreads();  // two tiles are there, and nobody reads the two before them any more
+                                if (more) bring_pair(false, i + 2);
+                            }
+                            if (active) tile_alone(i & (RING - 1), (ta + i) * KT, k1);
+                            if (!more) continue;
+                            if (even) {
+                                settle_pair(false, i + 2);
+                                bring_pair(true, i + 2);
+                            } else {
+                                settle_pair(true, i + 1);
+                            }
+                        }
+                        return;
+                    }
                     const int lane_here = apart(lane), wave_here = apart_uniform(wave), k_here = apart_uniform((int)k_at), v_here = k_here + RING * TILE;
                     auto issue = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
@@ -605,7 +788,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
                     const int row = row0 + r, token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
                     const int64_t o = (int64_t)(seq.first + token) * a.heads + head;
 #pragma unroll
-                    for (int i = 0; i < CB; ++i) store_output<T>(a.O, o, rb, 16 * i + 4 * quarter_of_lane, oacc[i][x], l);
+                    for (int i = 0; i < CB; ++i) store_output<T>(a.O, o, qb, 16 * i + 4 * quarter_of_lane, oacc[i][x], l);
                     if (quarter_of_lane == 0 && a.lse) a.lse[o] = log_sum(m_run[x], l);
                 } else {
 #pragma unroll
@@ -620,6 +803,7 @@ void paged_tiles_kernel(AttendArgs a, int grain)
     }
 }
 
+template <typename T, int UB> int byte_workgroups() { return (compute_units() * TilesCfg<T, UB, true>::PER_CU + 7) & ~7; }
 template <typename T, int UB> int workgroups() { return (compute_units() * TilesCfg<T, UB>::PER_CU + 7) & ~7; }
 
 template <typename T, int UB, int SHORT, int MODE> hipError_t launch(const PagedArgs& p, hipStream_t stream)
@@ -632,6 +816,20 @@ template <typename T, int UB, int SHORT, int MODE> hipError_t launch(const Paged
     else paged_tiles_kernel<T, UB, SHORT, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, grain);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : launch_join<T>(a, C::ROWS, C::COLS, stream);
+}
+
+// The same over a cache in 8 bits: rows of 2 d bytes on chip.
+template <typename T, int UB, int SHORT, int MODE> hipError_t launch_bytes(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
+{
+    using C = TilesCfg<T, UB, true>;
+    ByteAttendArgs a;
+    static_cast<AttendArgs&>(a) = attend_args(p, byte_workgroups<T, UB>(), C::ROWS, C::UNIT, sizeof(T));
+    a.scales = scales;
+    paged_tiles_kernel<T, UB, SHORT, MODE, false, true><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, key_grain(a.cache, scales));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.cache.row_bytes *= (int)sizeof(T);          // (of the output)
+    return launch_join<T>(a, C::ROWS, C::COLS, stream);
 }
 
 template <typename T, typename F> auto by_row(int row_bytes, F&& f)
@@ -658,6 +856,23 @@ template <typename T, int MODE> hipError_t launch_tiles(const PagedArgs& p, hipS
         constexpr int UB = decltype(ubc)::value;
         if constexpr (sizeof(T) == 4 || UB > 5) return launch<T, UB, -1, MODE>(p, stream);
         else return p.cache.row_bytes == UB * 64 ? launch<T, UB, 0, MODE>(p, stream) : launch<T, UB, 32, MODE>(p, stream);
+    });
+}
+
+template <typename T, int MODE> hipError_t launch_byte_tiles(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
+{
+    return by_row<uint16_t>(2 * p.cache.row_bytes, [&](auto ubc) {
+        constexpr int UB = decltype(ubc)::value;
+        if constexpr (sizeof(T) == 4 || UB > 5) return launch_bytes<T, UB, -1, MODE>(p, scales, stream);
+        else return 2 * p.cache.row_bytes == UB * 64 ? launch_bytes<T, UB, 0, MODE>(p, scales, stream) : launch_bytes<T, UB, 32, MODE>(p, scales, stream);
+    });
+}
+
+template <typename T> int64_t byte_tiles_workspace(const PagedArgs& p)
+{
+    return by_row<uint16_t>(2 * p.cache.row_bytes, [&](auto ubc) {
+        constexpr int UB = decltype(ubc)::value;
+        return partial_bytes(byte_workgroups<T, UB>(), TilesCfg<T, UB, true>::ROWS, TilesCfg<T, UB, true>::COLS);
     });
 }
 

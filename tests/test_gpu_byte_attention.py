@@ -6,7 +6,7 @@ import torch
 
 import paper_2407_13885_amd as attnw
 from byte_util import Problem8
-from gpu_util import require_gpu
+from gpu_util import kernels, require_gpu
 from paged_util import within
 from test_gpu_paged import RULES
 
@@ -44,26 +44,41 @@ SHAPES = [
 ]
 
 
+@pytest.fixture(params=["rows", "tiles"])
+def kernel(request, monkeypatch):
+    """Every shape goes through both kernels, whichever it would take by itself."""
+    monkeypatch.setenv("ATTNW_PAGED_KERNEL", request.param)
+    return request.param
+
+
+def test_either_kernel_of_a_shape(kernel):
+    p = Problem8("bf16", [(1, 300), (9, 9)], 4, 2, 64, 16).on_gpu()
+    work = torch.empty(attnw.attnw_byte_paged_workspace(p.cache, p.T, 4), dtype=torch.uint8, device="cuda")
+    O, d = torch.empty((p.T, 4, 64), dtype=torch.bfloat16, device="cuda"), p.dev
+    ran = kernels(lambda s: attnw.attnw_byte_paged_attention(p.cache, p.rule, d["Q"], O, None, d["starts"], p.T, 4, p.q_stride, work, work.numel(), s))
+    assert ("byte_rows_kernel" if kernel == "rows" else "paged_tiles_kernel") in ran[0]
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("name,sequences,heads,kv_heads,d,page,block", SHAPES, ids=[s[0] for s in SHAPES])
-def test_attention(dtype, name, sequences, heads, kv_heads, d, page, block):
+def test_attention(kernel, dtype, name, sequences, heads, kv_heads, d, page, block):
     check(Problem8(dtype, sequences, heads, kv_heads, d, page, block, seed=len(name)))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", range(16, 257, 16))
-def test_head_sizes(dtype, d):
-    check(Problem8(dtype, [(1, 190), (18, 75)], 4, 2, d, 16, 16 if d % 32 else 8, seed=d))
+def test_head_sizes(kernel, dtype, d):
+    check(Problem8(dtype, [(1, 190), (50, 475)], 4, 2, d, 16, 16 if d % 32 else 8, seed=d))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("name,more", RULES, ids=[r[0] for r in RULES])
-def test_rules(dtype, name, more):
+def test_rules(kernel, dtype, name, more):
     check(Problem8(dtype, [(1, 410), (40, 333), (150, 420)], 8, 4, 64, 32, 16, seed=3, **more))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_rows_that_see_nothing(dtype):
+def test_rows_that_see_nothing(kernel, dtype):
     """A sequence of more tokens than slots: those before its first slot see the prefix or nothing."""
     p = Problem8(dtype, [(4, 60)], 4, 2, 64, 16, more_pages=1)
     p.lengths[0] = 2
@@ -79,7 +94,7 @@ def test_rows_that_see_nothing(dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 80, 192])
-def test_what_is_hidden_has_no_part(dtype, d):
+def test_what_is_hidden_has_no_part(kernel, dtype, d):
     """Keys, values and scales that a row does not see may hold anything: later tokens of its chunk, what lies in front of its window."""
     p = Problem8(dtype, [(30, 300)], 4, 2, d, 16, 8, seed=5, window=40)
     clean = p.on_gpu().run_attention()
@@ -111,7 +126,7 @@ def test_what_is_hidden_has_no_part(dtype, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_scales_at_their_ends(dtype):
+def test_scales_at_their_ends(kernel, dtype):
     """The least and greatest scales that appending makes, in blocks beside ordinary ones: values of either, keys of the least (a score of the others is then the only one)."""
     p = Problem8(dtype, [(5, 120), (33, 64)], 4, 2, 64, 16, 4, seed=11)
     p.V_scales[p.table[0, 2].long()] = 127 - 117
@@ -122,7 +137,7 @@ def test_scales_at_their_ends(dtype):
 
 
 @pytest.mark.parametrize("scale", [-0.125, 0.0, 3.0])
-def test_scales_of_either_sign(scale):
+def test_scales_of_either_sign(kernel, scale):
     for dtype in ("bf16", "f32"):
         p = Problem8(dtype, [(1, 90), (20, 333)], 4, 2, 64, 16, 16, seed=12)
         p.scale = scale
@@ -149,7 +164,7 @@ def test_padded_rows_and_rows_of_nobody():
     assert bool((P[:2] == 7).all()) and bool((P[14:] == 7).all()) and bool((lse2[:2] == 7).all()) and bool((lse2[14:] == 7).all())
 
 
-def test_counts_and_pages_in_no_order():
+def test_counts_and_pages_in_no_order(kernel):
     """Whatever lengths, starts and page ids hold, the call ends and what lies around its outputs stays."""
     for starts, lengths in (([41, 0, 2 ** 31 - 1, -2 ** 31], [-5, 2 ** 31 - 1, 7]), ([0, 41, 0, 41], [64, 64, 64]), ([-9, 100, -100, 50], [1, 1, 1])):
         p = Problem8("bf16", [(9, 40), (30, 50), (2, 20)], 4, 2, 64, 16, 4, seed=9)
@@ -164,7 +179,16 @@ def test_counts_and_pages_in_no_order():
         assert bool((O[p.T:] == 7).all()) and bool((lse[p.T:] == 7).all()) and bool((work[size:] == 91).all())
 
 
-def test_far_pages():
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,more", [(128, {}), (64, dict(cap=20.0)), (96, dict(slopes=True)), (16, dict(cap=9.0, slopes=True)), (160, dict(window=900)), (48, dict(prefix=[1100])),
+                                    (112, dict(cap=300.0)), (224, {})])
+def test_long_runs_of_tiles(kernel, dtype, d, more):
+    """Tiles that all rows see whole, one after the other, in numbers odd and even, and lists of places longer than what is on chip."""
+    for m, block in ((1290, 16), (1322, 2)):
+        check(Problem8(dtype, [(70, m)], 2, 1, d, 32, block, seed=m, **more))
+
+
+def test_far_pages(kernel):
     """Offsets past 2^32 bytes: keys and values in the last pages of a pool of five GiB."""
     p = Problem8("bf16", [(40, 150), (1, 64)], 8, 4, 64, 64, 32, seed=14, garbage=False)
     near = p.on_gpu().run_attention()
