@@ -413,7 +413,7 @@ int attnw_rotary_axes(const void *X, void *Y, const float *table, const int32_t 
 /*
  * A paged cache in 8 bits: K and V of `cache` hold a byte an element, an e4m3 number (4 bits of exponent, 3 of mantissa, up to
  * 448, no infinities), which stands for itself times 2^(s - 127), s the byte that `block` slots of a page share for a kv head: slot
- * row r of a page has K_scales[page][kv_head][r / block] (254 at most counts).  block divides page_size.
+ * row r of a page has K_scales[page][kv_head][r / block] (below 1 it counts as 1, above 246 as 246).  block divides page_size.
  * d: a multiple of 16.  `dtype` is the type of queries, new tokens and outputs.
  */
 typedef struct attnw_byte_cache {

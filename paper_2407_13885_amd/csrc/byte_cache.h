@@ -12,8 +12,11 @@ namespace {
 
 constexpr int kLeastScale = -117, kMostScale = 119;   // exponents: 2^-9 of the least scale and 448 of the greatest are normal fp32 numbers
 
-// A scale's byte as a number (255, which nothing here writes, as 254)
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(min(byte, 254u) << 23); }
+// A scale's byte as a number.  (Nothing here writes others than 10 to 246; from there on 448 times it would be no bf16 number.)
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(max(1u, min(byte, 127u + kMostScale)) << 23); }
+
+// Of four elements, whether one is NaN: flags in the signs' places.
+__device__ __forceinline__ uint32_t any_nan(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
 // The least e with |x| <= 448 2^e, x as the bits of a finite number without its sign.
 __device__ __forceinline__ int exponent_for(uint32_t x)

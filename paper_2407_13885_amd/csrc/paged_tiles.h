@@ -318,7 +318,8 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
             }
         };
         // the same two, which have arrived, into the ring; of V also whether something is no number
-        auto settle = [&](bool v, int tile, int last_tile, int k0, int k1, int ring0) __attribute__((always_inline)) {
+        auto settle = [&](bool v, int tile, int last_tile, int k0, int k1, int ring0, auto lookc) __attribute__((always_inline)) {
+            constexpr bool LOOK = decltype(lookc)::value != 0;
             if constexpr (BYTES) {
                 const int lane_here = apart(lane), wave_here = apart_uniform(wave);
                 uint32_t bad[2] = {0, 0};
@@ -335,9 +336,10 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
                     char* const row = (v ? v_lds : k_lds) + ((ring0 + second) & (RING - 1)) * TILE + key * DB;
                     *reinterpret_cast<u32x4*>(row + (v ? v_chunk(key, c) : c ^ L::k_chunk(key)) * 16) = lo;
                     *reinterpret_cast<u32x4*>(row + (v ? v_chunk(key, c + 1) : (c + 1) ^ L::k_chunk(key)) * 16) = hi;
-                    if (v) bad[second] |= any_lost<E>(lo) | any_lost<E>(hi);
+                    if constexpr (LOOK)
+                        if (v) bad[second] |= any_nan(w[0]) | any_nan(w[1]) | any_nan(w[2]) | any_nan(w[3]);
                 }
-                if (v) {
+                if (LOOK && v) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const uint32_t some = __builtin_amdgcn_ballot_w64(bad[k] != 0) != 0 ? 1u : 0u;
@@ -408,10 +410,49 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
             auto bring_pair = [&](bool v, int t) __attribute__((always_inline)) { bring(v, wa + t, wb - 1, k0, wb * 32); };
             auto settle_pair = [&](bool v, int t) __attribute__((always_inline)) {
                 arrived<0>();
-                settle(v, wa + t, wb - 1, k0, wb * 32, t & (RING - 1));
+                settle(v, wa + t, wb - 1, k0, wb * 32, t & (RING - 1), IC<0>{});   // (all rows see all of it: what is no number goes its way)
+            };
+            // UNIFORM: where a piece comes from and what its scale is are numbers of the wave, and a lane's places within it do not change
+            constexpr bool BY16 = UB == 2 || UB == 4;          // (a piece's keys are among 16; else they are any of a tile's)
+            constexpr int BYTE_OFFS = BYTES ? (UB == 4 ? 1 : C::XR) : 1;
+            int byte_off[BYTE_OFFS], k_to[BYTE_OFFS], v_to[BYTE_OFFS];
+            float byte_scale[C::XR];
+            u32x4 piece[C::XR];
+            if constexpr (BYTES && UNIFORM) {
+#pragma unroll
+                for (int j = 0; j < BYTE_OFFS; ++j) {
+                    const int y = wave_here + NW * j, x = (y >= UB ? y - UB : y) % UB * 64 + lane_here, key = x / (2 * UB), c = (x - key * (2 * UB)) * 2;
+                    byte_off[j] = (BY16 ? key & 15 : key) * (rb / 2) + (SHORT == 0 || c * 8 < rb / 2 ? c * 8 : c * 8 - rb / 2);
+                    k_to[j] = key * DB + (c ^ L::k_chunk(key)) * 16;
+                    v_to[j] = key * DB + v_chunk(key, c) * 16;
+                }
+            }
+            auto bring_piece = [&](bool v, int t, int j) __attribute__((always_inline)) {
+                const int y = wave_here + NW * j, second = y >= UB ? 1 : 0;
+                if (2 * UB % NW != 0 && y >= 2 * UB) return;
+                const int half = BY16 ? ((y - second * UB) * 64 / (2 * UB)) >> 4 : 0, from = 2 * min(t + second, n_tiles - 1) + half - place_base;
+                const uint32_t high = (uint32_t)__builtin_amdgcn_readlane((int)(place >> 32), from);
+                const int64_t off = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)place, from) | (int64_t)(high & 0xffffu) << 32;
+                byte_scale[j] = v ? value_scale(high) : key_scale(high);
+                dma16_untracked((v ? a.cache.V : a.cache.K) + off, (uint32_t)byte_off[j % BYTE_OFFS], (uint32_t)uniform((int)(k_here - C::RAW + y * 1024)));
+            };
+            auto read_piece = [&](int j) __attribute__((always_inline)) {
+                const int y = wave_here + NW * j;
+                if (2 * UB % NW != 0 && y >= 2 * UB) return;
+                piece[j] = *reinterpret_cast<const u32x4*>(lds + y * 1024 + lane_here * 16);
+            };
+            auto lay_piece = [&](bool v, int ring0, int j) __attribute__((always_inline)) {
+                const int y = wave_here + NW * j, second = y >= UB ? 1 : 0;
+                if (2 * UB % NW != 0 && y >= 2 * UB) return;
+                const u32x4 lo = bf16_of(piece[j][0], piece[j][1], byte_scale[j]), hi = bf16_of(piece[j][2], piece[j][3], byte_scale[j]);
+                char* const to = (v ? v_lds : k_lds) + ((ring0 + second) & (RING - 1)) * TILE;
+                const int at = v ? v_to[j % BYTE_OFFS] : k_to[j % BYTE_OFFS];
+                *reinterpret_cast<u32x4*>(to + at) = lo;
+                *reinterpret_cast<u32x4*>(to + (v ? at + 16 : at ^ 16)) = hi;   // (chunks of V trade places by twos)
             };
             __syncthreads();                      // (what the ring held has been read)
             if constexpr (BYTES) {
+                look_up(0);
 #pragma unroll
                 for (int i = 0; i < 3; ++i) {     // K of tiles 0 to 3, V of 0 and 1
                     bring_pair(i == 2, i == 1 ? 2 : 0);
@@ -433,13 +474,16 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
                         if (t % 2 == 0) {
                             bring_pair(false, t + 4);
                             settle_pair(false, t + 4);
-                            bring_pair(true, t + 1);
                         } else {
+                            bring_pair(true, t);
                             settle_pair(true, t);
                             end_of_pair();
                         }
                     }
-                    if (n_tiles % 2 == 0) settle_pair(true, n_tiles - 1);
+                    if (n_tiles % 2 == 0) {
+                        bring_pair(true, n_tiles - 1);
+                        settle_pair(true, n_tiles - 1);
+                    }
                     end_of_pair();
                     return;
                 }
@@ -553,7 +597,7 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
             s = sn;
             if constexpr (BYTES) {
                 settle_pair(false, 4);
-                bring_pair(true, 1);
+                if constexpr (!UNIFORM) bring_pair(true, 1);
             }
             u32x4 kf[KF], vf[RV];
 #pragma unroll
@@ -565,7 +609,7 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
                 constexpr int STEPS = 2 * (KF + CB), OPS = 8 + 32 + 16 + (MODE != kPlain ? 0 : 8);
                 Weights pw;
                 float pn[2][8], sum[2], top[2];
-                if constexpr (BYTES && BUF % 2 == 0) bring_pair(false, t + 4);
+                if constexpr (BYTES && !UNIFORM && BUF % 2 == 0) bring_pair(false, t + 4);
                 auto vector_op = [&](auto oc) __attribute__((always_inline)) {
                     constexpr int I = decltype(oc)::value;
                     if constexpr (I < 8) {
@@ -608,6 +652,18 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
                     static_for<(I + 1) * OPS / STEPS - I * OPS / STEPS>([&](auto jc) __attribute__((always_inline)) {
                         vector_op(IC<I * OPS / STEPS + decltype(jc)::value>{});
                     });
+                    if constexpr (BYTES && UNIFORM) {          // of K tiles t + 4 and t + 5, or, t odd, of V t and t + 1
+                        constexpr bool V = BUF % 2 == 1;
+                        constexpr int READ = STEPS * 5 / 8;
+                        static_assert(READ + 2 * C::XR < STEPS);
+                        if constexpr (I < C::XR) bring_piece(V, V ? t : t + 4, I);
+                        if constexpr (I == READ) {
+                            arrived<0>();
+#pragma unroll
+                            for (int j = 0; j < C::XR; ++j) read_piece(j);
+                        }
+                        if constexpr (I > READ + 1 && (I - READ) % 2 == 0 && I <= READ + 2 * C::XR) lay_piece(V, BUF, (I - READ) / 2 - 1);
+                    }
                     // (transfers between the steps: a wave that issues them in a row waits 50 cycles for each)
                     if constexpr (!BYTES && BUF % 2 == 0 && I % 2 == 0 && I / 2 < 4 * XW) transfer(t, I / 2 % XW, I / 2 / XW);
                     __builtin_amdgcn_sched_barrier(0);
@@ -624,7 +680,7 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
 #pragma unroll
                     for (int r = 0; r < 8; ++r) p[x][r] = pn[x][r];
                 follow(top, kLazy, true);
-                if constexpr (BYTES) {
+                if constexpr (BYTES && !UNIFORM) {
                     if constexpr (BUF % 2 == 0) {
                         settle_pair(false, t + 4);
                         bring_pair(true, t + 1);
@@ -646,7 +702,10 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
                 tile(t++, IC<0>{});
             }
             if constexpr (BYTES)
-                if (n_tiles % 2 == 0) settle_pair(true, n_tiles - 1);
+                if (n_tiles % 2 == 0) {
+                    if constexpr (UNIFORM) bring_pair(true, n_tiles - 1);
+                    settle_pair(true, n_tiles - 1);
+                }
             end_of_pair();
             // ---- the last two tiles ---------------------------------------------------------------------------------------------------------
             output((n_tiles - 2) & 3, pack());
@@ -688,7 +747,7 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
                         auto bring_pair = [&](bool v, int i) __attribute__((always_inline)) { bring(v, ta + i, tb - 1, k0, k1); };
                         auto settle_pair = [&](bool v, int i) __attribute__((always_inline)) {
                             arrived<0>();
-                            settle(v, ta + i, tb - 1, k0, k1, i & (RING - 1));
+                            settle(v, ta + i, tb - 1, k0, k1, i & (RING - 1), IC<1>{});
                         };
                         __syncthreads();
 #pragma unroll
@@ -825,7 +884,10 @@ template <typename T, int UB, int SHORT, int MODE> hipError_t launch_bytes(const
     ByteAttendArgs a;
     static_cast<AttendArgs&>(a) = attend_args(p, byte_workgroups<T, UB>(), C::ROWS, C::UNIT, sizeof(T));
     a.scales = scales;
-    paged_tiles_kernel<T, UB, SHORT, MODE, false, true><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, key_grain(a.cache, scales));
+    // (16 keys that share a page and scales, or a tile's)
+    constexpr bool CAN = C::PIPE;
+    if (CAN && scales.block.d % (UB == 2 || UB == 4 ? 16 : 32) == 0) paged_tiles_kernel<T, UB, SHORT, MODE, CAN, true><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, 4);
+    else paged_tiles_kernel<T, UB, SHORT, MODE, false, true><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, key_grain(a.cache, scales));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     a.cache.row_bytes *= (int)sizeof(T);          // (of the output)

@@ -38,7 +38,7 @@ def held(x, block):
 
 def values(b, scales, block):
     """What bytes and scales stand for, in fp32 (exact for scales from 2^-117 to 2^119)."""
-    s = torch.ldexp(torch.ones(()), scales.clamp(max=254).int() - 127).repeat_interleave(block, 2)
+    s = torch.ldexp(torch.ones(()), scales.clamp(1, 246).int() - 127).repeat_interleave(block, 2)
     return numbers(b) * s[..., None]
 
 
