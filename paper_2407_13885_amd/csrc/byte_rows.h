@@ -17,20 +17,19 @@
 namespace attnw {
 namespace {
 
-constexpr int kRows = 16;                         // of a block
-
-// UB: 64-byte groups of a row on chip.
-template <int UB> struct ByteRowsCfg {
+// UB: 64-byte groups of a row on chip.  NX: blocks of 16 rows that share the keys.
+template <int UB, int NX> struct ByteRowsCfg {
+    static constexpr int ROWS = 16 * NX;
     static constexpr int KT = 32;                 // keys of a tile
     static constexpr int DB = UB * 64, CPR = UB * 4, TILE = KT * DB, XFERS = TILE / 1024;
     static constexpr int COLS = DB, CB = COLS / 16;
-    static constexpr int NW = UB <= 2 ? 8 : 4;
+    static constexpr int NW = 4;
     static constexpr int UNIT = KT * NW;          // keys of a place
     static constexpr int PITCH = COLS + 4;        // floats of a row of partial results
-    static constexpr int STAGES = NW * 4 * TILE;
-    static constexpr int LDS = STAGES + kPlaces * 8 + NW * kRows * 8;
+    static constexpr int STAGES = NW * 4 * TILE, PLACES = kPlaces;
+    static constexpr int LDS = STAGES + PLACES * 8 + NW * ROWS * 8;
     static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;
-    static_assert(4 * TILE >= kRows * PITCH * 4, "partial results of a wave in its stages");
+    static_assert(4 * TILE >= 16 * PITCH * 4, "partial results of 16 rows of a wave in its stages");
     static_assert(STAGES <= kDirectLds);
 };
 
@@ -47,18 +46,18 @@ __device__ __forceinline__ u32x2 lds_read_tr8(const char* p)
     return u32x2{0u, 0u};
 #endif
 }
-template <typename T, int UB, int MODE, bool EXACT, int THREADS = 64 * ByteRowsCfg<UB>::NW>
-__global__ __launch_bounds__(THREADS, 2)
+template <typename T, int UB, int NX, int MODE, bool EXACT, int THREADS = 64 * ByteRowsCfg<UB, NX>::NW, int BLOCKS = ByteRowsCfg<UB, NX>::PER_CU>
+__global__ __launch_bounds__(THREADS, BLOCKS)
 void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
 {
-    using C = ByteRowsCfg<UB>;
+    using C = ByteRowsCfg<UB, NX>;
     using L = RowLayout<UB>;
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
     constexpr bool F32 = PARTS == 3;
     constexpr int NW = C::NW, KT = C::KT, DB = C::DB, CPR = C::CPR, TILE = C::TILE, XFERS = C::XFERS, CB = C::CB, NK = KT / 16, PITCH = C::PITCH;
     __shared__ __align__(1024) char lds[C::LDS];
     int64_t* const places = reinterpret_cast<int64_t*>(lds + C::STAGES);
-    float* const stats = reinterpret_cast<float*>(lds + C::STAGES + kPlaces * 8);   // [wave][row]{maximum, sum}
+    float* const stats = reinterpret_cast<float*>(lds + C::STAGES + C::PLACES * 8);   // [wave][row]{maximum, sum}
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
@@ -66,7 +65,7 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
     const uint32_t stage_at = lds_offset_of(stage);
     const int rb = EXACT ? DB : a.cache.row_bytes;
 
-    Walk<kRows> walk(a, lane);
+    Walk<C::ROWS> walk(a, lane);
     if (walk.at >= walk.end) return;
 
     const ScoreMap<(MODE & kCap) != 0, F32> map(a.rule);
@@ -81,13 +80,15 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
         // ---- the rows of the block ------------------------------------------------------------------------------------------------
         const int group = a.group.d, base = seq.length - seq.tokens;              // slot of the first new token
         const int first = base + (int)quotient(row0, a.group), last = base + (int)quotient(row0 + rows - 1, a.group);
-        const int row = row0 + min(l16, rows - 1);
-        const int token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
-        const int query = base + token;   // sees the slots query - window + 1 .. query
-        const float slope = MODE & kBias ? a.rule.slopes[head] * kLog2e : 0.0f;
-
-        Parts<PARTS> qf[2 * UB];                  // columns 64 g + 16 quarter .. + 7, and the 8 behind them (zeros behind the row's end)
-        {
+        int query[NX];                            // sees the slots query - window + 1 .. query
+        float slope[NX];
+        Parts<PARTS> qf[NX][2 * UB];              // columns 64 g + 16 quarter .. + 7, and the 8 behind them (zeros behind the row's end)
+#pragma unroll
+        for (int n = 0; n < NX; ++n) {
+            const int row = row0 + min(16 * n + l16, rows - 1);
+            const int token = (int)quotient(row, a.group), head = kv_head * group + row - token * group;
+            query[n] = base + token;
+            slope[n] = MODE & kBias ? a.rule.slopes[head] * kLog2e : 0.0f;
             const char* q = a.Q + (int64_t)(seq.first + token) * a.q_stride + (int64_t)head * rb * (int)sizeof(T);
 #pragma unroll
             for (int g = 0; g < UB; ++g) {
@@ -101,17 +102,21 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
                         float y[8];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) y[i] = inside ? lo[i] : 0.0f, y[4 + i] = inside ? hi[i] : 0.0f;
-                        qf[2 * g + half] = parts_of<PARTS>(y);
+                        qf[n][2 * g + half] = parts_of<PARTS>(y);
                     } else {
-                        qf[2 * g + half].of[0] = inside ? *reinterpret_cast<const u32x4*>(p) : u32x4{0, 0, 0, 0};
+                        qf[n][2 * g + half].of[0] = inside ? *reinterpret_cast<const u32x4*>(p) : u32x4{0, 0, 0, 0};
                     }
                 }
             }
         }
-        f32x4 oacc[CB];
+        f32x4 oacc[CB][NX];
 #pragma unroll
-        for (int c = 0; c < CB; ++c) oacc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        float m_run = -__builtin_inff(), l_run = 0.0f;
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int n = 0; n < NX; ++n) oacc[c][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        float m_run[NX], l_run[NX];
+#pragma unroll
+        for (int n = 0; n < NX; ++n) m_run[n] = -__builtin_inff(), l_run[n] = 0.0f;
 
         // ---- the keys of places v0 .. v1 - 1 -----------------------------------------------------------------------------------------
         const Span span = visible_span(a.unit_log, first, last, seq.length, prefix, a.rule.window);
@@ -121,7 +126,7 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
         const int32_t* const pages_of = a.cache.table + (int64_t)seg.b * a.cache.max_pages;
 
         auto sweep = [&](int from, int to) __attribute__((always_inline)) {   // keys
-            const int most = kPlaces << grain;    // (a whole number of units: the waves' tiles stay where they are)
+            const int most = C::PLACES << grain;    // (a whole number of units: the waves' tiles stay where they are)
             for (int k0 = from; k0 < to;) {
                 const int k1 = min(to, k0 + most);
                 __syncthreads();
@@ -155,61 +160,76 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
                     const char* const vt = kt + TILE;
                     if (more) arrived<3 * XFERS>();
                     else arrived<XFERS>();
-                    float x[NK * 4];
+                    float x[NX][NK * 4];
 #pragma unroll
                     for (int k = 0; k < NK; ++k) {
                         const float ks = key_scale(high_of(key0 + 16 * k + l16));
-                        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+                        f32x4 acc[NX];
+#pragma unroll
+                        for (int n = 0; n < NX; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                         for (int g = 0; g < UB; ++g) {
                             const u32x4 w = *reinterpret_cast<const u32x4*>(kt + (16 * k + l16) * DB + ((4 * g + quarter) ^ L::k_chunk(l16)) * 16);
-                            multiply_parts(acc, bf16_of(w[0], w[1], ks), qf[2 * g]);
-                            multiply_parts(acc, bf16_of(w[2], w[3], ks), qf[2 * g + 1]);
+                            const u32x4 lo = bf16_of(w[0], w[1], ks), hi = bf16_of(w[2], w[3], ks);
+#pragma unroll
+                            for (int n = 0; n < NX; ++n) {
+                                multiply_parts(acc[n], lo, qf[n][2 * g]);
+                                multiply_parts(acc[n], hi, qf[n][2 * g + 1]);
+                            }
                         }
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) x[4 * k + r] = acc[r];
+                        for (int n = 0; n < NX; ++n)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) x[n][4 * k + r] = acc[n][r];
                     }
-                    map(x);
                     const int key = key0 + 4 * quarter;        // + 16 k + r
-                    if constexpr ((MODE & kBias) != 0) {
-#pragma unroll
-                        for (int i = 0; i < NK * 4; ++i) x[i] -= slope * (float)abs(query - (key + 16 * (i / 4) + i % 4));
-                    }
                     const bool whole = key0 + KT <= k1 && ((key0 + KT - 1 <= first && key0 > last - a.rule.window) || key0 + KT <= prefix);
-                    if (!whole) {
-                        const Sight sight(query, a.rule, prefix, k1);
-#pragma unroll
-                        for (int i = 0; i < NK * 4; ++i) x[i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? -__builtin_inff() : x[i];
-                    }
-                    float top = x[0];
-#pragma unroll
-                    for (int i = 1; i < NK * 4; ++i) top = fmaxf(top, x[i]);
-                    top = quarter_wave_max(top);
-                    if (__builtin_amdgcn_ballot_w64(top > m_run) != 0) {
-                        const float m = fmaxf(m_run, top), alpha = m == -__builtin_inff() ? 1.0f : fast_exp2(m_run - m);
-                        l_run *= alpha;
-#pragma unroll
-                        for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
-                        m_run = m;
-                    }
-                    const float ref = m_run == -__builtin_inff() ? 0.0f : m_run;   // (nothing seen yet: all weights 0)
-                    float p[NK * 4];
-#pragma unroll
-                    for (int i = 0; i < NK * 4; ++i) {
-                        p[i] = fast_exp2(x[i] - ref);
-                        l_run += p[i];
-                    }
-                    // weights in units of the values' scales (powers of 2: no rounding)
+                    // the values' scales, which go into the weights (powers of 2: no rounding)
+                    float vs[NK * 4];
 #pragma unroll
                     for (int k = 0; k < NK; ++k) {
                         if (grain >= 2) {
-                            const float vs = value_scale(high_of(key + 16 * k));
+                            const float same = value_scale(high_of(key + 16 * k));
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) p[4 * k + r] *= vs;
+                            for (int r = 0; r < 4; ++r) vs[4 * k + r] = same;
                         } else {
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) p[4 * k + r] *= value_scale(high_of(key + 16 * k + r));
+                            for (int r = 0; r < 4; ++r) vs[4 * k + r] = value_scale(high_of(key + 16 * k + r));
                         }
+                    }
+                    Parts<PARTS> pw[NX];
+#pragma unroll
+                    for (int n = 0; n < NX; ++n) {
+                        float (&y)[NK * 4] = x[n];
+                        map(y);
+                        if constexpr ((MODE & kBias) != 0) {
+#pragma unroll
+                            for (int i = 0; i < NK * 4; ++i) y[i] -= slope[n] * (float)abs(query[n] - (key + 16 * (i / 4) + i % 4));
+                        }
+                        if (!whole) {
+                            const Sight sight(query[n], a.rule, prefix, k1);
+#pragma unroll
+                            for (int i = 0; i < NK * 4; ++i) y[i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? -__builtin_inff() : y[i];
+                        }
+                        float top = y[0];
+#pragma unroll
+                        for (int i = 1; i < NK * 4; ++i) top = fmaxf(top, y[i]);
+                        top = quarter_wave_max(top);
+                        if (__builtin_amdgcn_ballot_w64(top > m_run[n]) != 0) {
+                            const float m = fmaxf(m_run[n], top), alpha = m == -__builtin_inff() ? 1.0f : fast_exp2(m_run[n] - m);
+                            l_run[n] *= alpha;
+#pragma unroll
+                            for (int c = 0; c < CB; ++c) oacc[c][n] *= alpha;
+                            m_run[n] = m;
+                        }
+                        const float ref = m_run[n] == -__builtin_inff() ? 0.0f : m_run[n];   // (nothing seen yet: all weights 0)
+#pragma unroll
+                        for (int i = 0; i < NK * 4; ++i) {
+                            y[i] = fast_exp2(y[i] - ref);
+                            l_run[n] += y[i];
+                            y[i] *= vs[i];
+                        }
+                        pw[n] = parts_of<PARTS>(y);
                     }
                     if (more) arrived<2 * XFERS>();
                     else arrived<0>();
@@ -219,32 +239,42 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
                         const u32x2 w = lds_read_tr8(vt + vkey * DB + (c ^ v_chunk(vkey)) * 16 + (lane & 1) * 8);
                         return bf16_of(w[0], w[1], 1.0f);
                     };
-                    const Parts<PARTS> pw = parts_of<PARTS>(p);
                     if (!whole) {
                         uint32_t bad = 0;
 #pragma unroll
                         for (int c = 0; c < CB; ++c) bad |= any_lost<uint16_t>(v_frag(c));
                         if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
                             // NaN among the values, which must not reach rows that do not see them by way of a weight of 0: 0 in the product, and NaN for those that do
-                            const Sight sight(query, a.rule, prefix, k1);
-                            float some[NK * 4];
+                            u32x4 so[NX];
 #pragma unroll
-                            for (int i = 0; i < NK * 4; ++i) some[i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? 0.0f : 1.0f;
-                            const u32x4 so = parts_of<1>(some).of[0];
+                            for (int n = 0; n < NX; ++n) {
+                                const Sight sight(query[n], a.rule, prefix, k1);
+                                float some[NK * 4];
+#pragma unroll
+                                for (int i = 0; i < NK * 4; ++i) some[i] = sight.hidden(key + 16 * (i / 4) + i % 4) < 0 ? 0.0f : 1.0f;
+                                so[n] = parts_of<1>(some).of[0];
+                            }
 #pragma unroll
                             for (int c = 0; c < CB; ++c) {
                                 const u32x4 v = v_frag(c);
-                                f32x4 lost = {0.0f, 0.0f, 0.0f, 0.0f};
-                                mma16(lost, lost_as_one<uint16_t, kAny>(v), so);
-                                multiply_parts(oacc[c], without_lost<uint16_t>(v), pw);
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) oacc[c][r] = lost[r] > 0.0f ? __builtin_nanf("") : oacc[c][r];
+                                for (int n = 0; n < NX; ++n) {
+                                    f32x4 lost = {0.0f, 0.0f, 0.0f, 0.0f};
+                                    mma16(lost, lost_as_one<uint16_t, kAny>(v), so[n]);
+                                    multiply_parts(oacc[c][n], without_lost<uint16_t>(v), pw[n]);
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r) oacc[c][n][r] = lost[r] > 0.0f ? __builtin_nanf("") : oacc[c][n][r];
+                                }
                             }
                             return;
                         }
                     }
 #pragma unroll
-                    for (int c = 0; c < CB; ++c) multiply_parts(oacc[c], v_frag(c), pw);
+                    for (int c = 0; c < CB; ++c) {
+                        const u32x4 v = v_frag(c);
+#pragma unroll
+                        for (int n = 0; n < NX; ++n) multiply_parts(oacc[c][n], v, pw[n]);
+                    }
                 };
                 int key = k0 + wave * KT, s = 0;
                 if (key < k1) issue(key, 0);
@@ -262,66 +292,73 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
             const int f = part == 0 ? u0 : max(u0, span.head), t = part == 0 ? min(u1, span.head) : u1;
             if (f < t) sweep(span.unit(f) << a.unit_log, (int)min((int64_t)seen, (int64_t)(span.unit(t - 1) + 1) << a.unit_log));
         }
-        l_run = quarter_wave_sum(l_run);
-
-        // ---- the waves' results into one -----------------------------------------------------------------------------------------------
-        __syncthreads();
-        if (quarter == 0) {
-            stats[(wave * kRows + l16) * 2] = m_run;
-            stats[(wave * kRows + l16) * 2 + 1] = l_run;
-        }
-        float* const mine = reinterpret_cast<float*>(stage);
-#pragma unroll
-        for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4*>(mine + l16 * PITCH + 16 * c + 4 * quarter) = oacc[c];
-        __syncthreads();
+        // ---- the waves' results into one, 16 rows at a time -----------------------------------------------------------------------------
         const bool complete = seg.slot < 0;
-        float* const out = a.partial + max(seg.slot, 0) * (int64_t)(kRows * (C::COLS + 2));
+        float* const out = a.partial + max(seg.slot, 0) * (int64_t)(C::ROWS * (C::COLS + 2));
         constexpr int QUADS = C::COLS / 4;
-        for (int i = threadIdx.x; i < rows * QUADS; i += 64 * NW) {
-            const int r = i / QUADS, c = (i - r * QUADS) * 4;
-            float top = -__builtin_inff();
 #pragma unroll
-            for (int n = 0; n < NW; ++n) top = fmaxf(top, stats[(n * kRows + r) * 2]);
-            const float ref = top == -__builtin_inff() ? 0.0f : top;
-            f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-            float l = 0.0f;
-#pragma unroll
-            for (int n = 0; n < NW; ++n) {
-                const float f = fast_exp2(stats[(n * kRows + r) * 2] - ref);
-                l += f * stats[(n * kRows + r) * 2 + 1];
-                sum += *reinterpret_cast<const f32x4*>(lds + n * 4 * TILE + (r * PITCH + c) * 4) * f;
+        for (int n = 0; n < NX; ++n) {
+            const float l_all = quarter_wave_sum(l_run[n]);
+            __syncthreads();
+            if (quarter == 0) {
+                stats[(wave * 16 + l16) * 2] = m_run[n];
+                stats[(wave * 16 + l16) * 2 + 1] = l_all;
             }
-            if (complete) {
-                const int tk = (int)quotient(row0 + r, a.group), h = kv_head * group + row0 + r - tk * group;
-                const int64_t o = (int64_t)(seq.first + tk) * a.heads + h;
-                store_output<T>(a.O, o, rb * (int)sizeof(T), c, sum, l);
-                if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
-            } else {
-                *reinterpret_cast<f32x4*>(out + r * C::COLS + c) = sum;
-                if (c == 0) {
-                    out[kRows * C::COLS + 2 * r] = top;
-                    out[kRows * C::COLS + 2 * r + 1] = l;
+            float* const mine = reinterpret_cast<float*>(stage);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4*>(mine + l16 * PITCH + 16 * c + 4 * quarter) = oacc[c][n];
+            __syncthreads();
+            for (int i = threadIdx.x; i < min(16, rows - 16 * n) * QUADS; i += 64 * NW) {
+                const int r = i / QUADS, c = (i - r * QUADS) * 4;
+                float top = -__builtin_inff();
+#pragma unroll
+                for (int w = 0; w < NW; ++w) top = fmaxf(top, stats[(w * 16 + r) * 2]);
+                const float ref = top == -__builtin_inff() ? 0.0f : top;
+                f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+                float l = 0.0f;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {
+                    const float f = fast_exp2(stats[(w * 16 + r) * 2] - ref);
+                    l += f * stats[(w * 16 + r) * 2 + 1];
+                    sum += *reinterpret_cast<const f32x4*>(lds + w * 4 * TILE + (r * PITCH + c) * 4) * f;
+                }
+                const int row = 16 * n + r;
+                if (complete) {
+                    const int tk = (int)quotient(row0 + row, a.group), h = kv_head * group + row0 + row - tk * group;
+                    const int64_t o = (int64_t)(seq.first + tk) * a.heads + h;
+                    store_output<T>(a.O, o, rb * (int)sizeof(T), c, sum, l);
+                    if (c == 0 && a.lse) a.lse[o] = log_sum(top, l);
+                } else {
+                    *reinterpret_cast<f32x4*>(out + row * C::COLS + c) = sum;
+                    if (c == 0) {
+                        out[C::ROWS * C::COLS + 2 * row] = top;
+                        out[C::ROWS * C::COLS + 2 * row + 1] = l;
+                    }
                 }
             }
         }
     }
 }
 
-template <int UB> int byte_workgroups() { return (compute_units() * ByteRowsCfg<UB>::PER_CU + 7) & ~7; }
+// Blocks of 32 rows where a sequence has more than 16 (up to d = 128, fp32 64: beyond, the registers do not hold them).
+template <typename T, int UB> constexpr int kMostBlocks = UB == 1 || (UB == 2 && sizeof(T) == 2) ? 2 : 1;
+inline int blocks_of(const PagedArgs& p, int most) { return most > 1 && p.tokens * (p.heads / p.cache.kv_heads) > 16 * (int64_t)p.cache.batch ? 2 : 1; }
 
-template <typename T, int UB, int MODE> hipError_t launch(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
+template <int UB, int NX> int byte_workgroups() { return (compute_units() * ByteRowsCfg<UB, NX>::PER_CU + 7) & ~7; }
+
+template <typename T, int UB, int NX, int MODE> hipError_t launch(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
 {
-    using C = ByteRowsCfg<UB>;
-    AttendArgs a = attend_args(p, byte_workgroups<UB>(), kRows, C::UNIT, sizeof(T));
+    using C = ByteRowsCfg<UB, NX>;
+    AttendArgs a = attend_args(p, byte_workgroups<UB, NX>(), C::ROWS, C::UNIT, sizeof(T));
     const int grain = key_grain(a.cache, scales);
     // (rows that fill their place: kernels of their own for the usual sizes)
     constexpr bool OWN = UB != 3;
-    if (OWN && a.cache.row_bytes == C::DB) byte_rows_kernel<T, UB, MODE, OWN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
-    else byte_rows_kernel<T, UB, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
+    if (OWN && a.cache.row_bytes == C::DB) byte_rows_kernel<T, UB, NX, MODE, OWN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
+    else byte_rows_kernel<T, UB, NX, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     a.cache.row_bytes *= (int)sizeof(T);          // (of the output)
-    return launch_join<T>(a, kRows, C::COLS, stream);
+    return launch_join<T>(a, C::ROWS, C::COLS, stream);
 }
 
 template <typename F> auto by_row(int row_bytes, F&& f)
@@ -333,24 +370,32 @@ template <typename F> auto by_row(int row_bytes, F&& f)
     return f(IC<4>{});
 }
 
-inline int64_t rows_workspace(const PagedArgs& p)
+template <typename T> int64_t rows_workspace(const PagedArgs& p)
 {
-    return by_row(p.cache.row_bytes, [&](auto ub) {
-        constexpr int UB = decltype(ub)::value;
-        return partial_bytes(byte_workgroups<UB>(), kRows, ByteRowsCfg<UB>::COLS);
+    return by_row(p.cache.row_bytes, [&](auto ubc) {
+        constexpr int UB = decltype(ubc)::value, MOST = kMostBlocks<T, UB>;
+        const auto of = [](auto nx) {
+            using C = ByteRowsCfg<UB, decltype(nx)::value>;
+            return partial_bytes(byte_workgroups<UB, decltype(nx)::value>(), C::ROWS, C::COLS);
+        };
+        return blocks_of(p, MOST) == 2 ? of(IC<MOST>{}) : of(IC<1>{});
     });
 }
 
 template <typename T> hipError_t launch_rows(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
 {
     return by_row(p.cache.row_bytes, [&](auto ubc) {
-        constexpr int UB = decltype(ubc)::value;
-        switch (rule_mode(p.rule)) {
-        case kPlain: return launch<T, UB, kPlain>(p, scales, stream);
-        case kCap: return launch<T, UB, kCap>(p, scales, stream);
-        case kBias: return launch<T, UB, kBias>(p, scales, stream);
-        default: return launch<T, UB, kCap | kBias>(p, scales, stream);
-        }
+        constexpr int UB = decltype(ubc)::value, MOST = kMostBlocks<T, UB>;
+        const auto by_rule = [&](auto nx) {
+            constexpr int NX = decltype(nx)::value;
+            switch (rule_mode(p.rule)) {
+            case kPlain: return launch<T, UB, NX, kPlain>(p, scales, stream);
+            case kCap: return launch<T, UB, NX, kCap>(p, scales, stream);
+            case kBias: return launch<T, UB, NX, kBias>(p, scales, stream);
+            default: return launch<T, UB, NX, kCap | kBias>(p, scales, stream);
+            }
+        };
+        return blocks_of(p, MOST) == 2 ? by_rule(IC<MOST>{}) : by_rule(IC<1>{});
     });
 }
 

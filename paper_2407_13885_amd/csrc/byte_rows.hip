@@ -3,7 +3,7 @@
 
 namespace attnw {
 
-int64_t byte_workspace(const PagedArgs& p) { return prefers_byte_tiles(p) ? byte_tiles_workspace(p) : rows_workspace(p); }
+int64_t byte_workspace(const PagedArgs& p) { return prefers_byte_tiles(p) ? byte_tiles_workspace(p) : p.dt == DType::F32 ? byte_rows_workspace_f32(p) : rows_workspace<uint16_t>(p); }
 
 hipError_t launch_byte_attention(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
 {

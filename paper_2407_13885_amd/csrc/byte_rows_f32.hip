@@ -3,6 +3,8 @@
 
 namespace attnw {
 
+int64_t byte_rows_workspace_f32(const PagedArgs& p) { return rows_workspace<float>(p); }
+
 hipError_t launch_byte_rows_f32(const PagedArgs& p, const ScalesView& scales, hipStream_t stream) { return launch_rows<float>(p, scales, stream); }
 
 }  // namespace attnw

@@ -1,4 +1,4 @@
-// Attention over a paged cache in 8 bits by blocks of 128 rows (paged_tiles.h): scores as they are; and when.
+// Attention over a paged cache in 8 bits by blocks of 128 rows (paged_tiles.h): scores as they are; and when a call goes there.
 #include "paged_tiles.h"
 
 #include <cstdlib>
@@ -8,13 +8,22 @@ namespace attnw {
 
 bool prefers_byte_tiles(const PagedArgs& p)
 {
+    const int64_t group = p.heads / p.cache.kv_heads, rows = p.tokens * group, all = p.tokens * p.heads;
+    const bool f32 = p.dt == DType::F32, wide = p.cache.row_bytes > 128;
+    // fp32: blocks of 16 rows, whose waves share nothing, are the faster ones up to d = 128 however many there are (2048 tokens over 4096 slots, 32 heads on 8, d = 64 266 / 312 us,
+    // 128 497 / 526; 80, where rows do not fill their place, 496 / 459)
+    if (f32 && !wide) return false;
     // (ATTNW_PAGED_KERNEL=rows / =tiles: tests and measurements compare the two)
     const char* force = getenv("ATTNW_PAGED_KERNEL");
     if (force && strcmp(force, "rows") == 0) return false;
     if (force && strcmp(force, "tiles") == 0) return true;
-    const int64_t group = p.heads / p.cache.kv_heads, rows = p.tokens * group, all = p.tokens * p.heads, d = p.cache.row_bytes;
-    if (rows < 48 * (int64_t)p.cache.batch) return false;
-    return all * d >= 1 << 19;
+    // Small blocks read and convert K and V once for every 32 rows (beyond d = 128, and in fp32: 16), large ones leave partial results of 128 rows to a join.
+    // Small / large, us, one sequence of 4096 slots, of 16384, 32 heads on 8, bf16:  64 tokens: d = 64 20 / 24, 36 / 32, 128 27 / 32, 50 / 45;  128 tokens: d = 64
+    // 26 / 27, 58 / 41, 128 36 / 38, 81 / 60;  256 tokens: d = 64 37 / 32, 100 / 61, 128 50 / 45, 140 / 91;  d = 256, 16 tokens: 28 / 28, 56 / 51, 32 tokens: 38 / 33, 95 / 58.
+    // fp32, 8 heads, d = 256, 64 tokens: 31 / 40, 66 / 84, 128 tokens: 45 / 48, 112 / 96, 256 tokens: 65 / 65, 199 / 162.
+    // Sequences beside each other, 16 of 4096 slots, bf16: d = 64, 64 rows each 36 / 40, 128 rows 55 / 43; d = 128 53 / 65, 78 / 71; d = 256, 32 rows 90 / 145, 64 rows 172 / 148.
+    if (rows < (wide ? 48 : 96) * (int64_t)p.cache.batch) return false;
+    return !wide ? all > 2048 : all >= (f32 ? 1024 : 768);
 }
 
 int64_t byte_tiles_workspace(const PagedArgs& p) { return p.dt == DType::F32 ? byte_tiles_workspace_f32(p) : byte_tiles_workspace<uint16_t>(p); }

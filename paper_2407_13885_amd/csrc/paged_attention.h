@@ -183,18 +183,13 @@ template <typename T> __device__ __forceinline__ void store_output(char* O, int6
 // log of a sum l of weights 2^(x - top)
 __device__ __forceinline__ float log_sum(float top, float l) { return l == 0.0f ? -__builtin_inff() : (top + fast_log2(l)) * (1.0f / kLog2e); }
 
-// The partial results of the blocks that end in a workgroup's stretch and did not begin there, ROWS rows of a block a workgroup.  Two loads one after the other bound
-// it: its threads read the parts' exponents at once, then share the columns and the parts.
+// A slice of ROWS rows of one block's partial results, which end in workgroup w's stretch and did not begin there.  Two loads one after the other bound
+// it: the threads of a workgroup read the parts' exponents at once, then share the columns and the parts.
 template <typename T, int ROWS>
-__global__ __launch_bounds__(256)
-void paged_join_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
+__device__ __forceinline__ void join_rows(const AttendArgs& a, const Joint& j, int w, int first, int32_t block_rows, int32_t cols, float (&tops)[256], float (&sums)[256][5])
 {
-    __shared__ float tops[256];
-    __shared__ float sums[256][5];
-    const Joint j = a.joints[blockIdx.x];
-    const int first = blockIdx.y * ROWS, rows = min(ROWS, j.rows - first);   // of the block
-    if (j.first < 0 || rows <= 0) return;
-    const int w = blockIdx.x, parts = w - j.first + 1, tid = threadIdx.x;
+    const int rows = min(ROWS, j.rows - first), parts = w - j.first + 1, tid = threadIdx.x;
+    if (rows <= 0) return;
     const int64_t slot = (int64_t)block_rows * (cols + 2);
     const float* const p0 = a.partial + (2 * (int64_t)j.first + j.later) * slot;         // the first part; the others are 2 places apart
     const float* const p1 = a.partial + 2 * (int64_t)j.first * slot;
@@ -248,6 +243,56 @@ void paged_join_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
     }
 }
 
+// One workgroup for each note and slice that there might be.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256)
+void paged_join_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
+{
+    __shared__ float tops[256];
+    __shared__ float sums[256][5];
+    const Joint j = a.joints[blockIdx.x];
+    if (j.first < 0) return;
+    join_rows<T, ROWS>(a, j, blockIdx.x, blockIdx.y * ROWS, block_rows, cols, tops, sums);
+}
+
+// The same where that would be many more than there are (blocks of 128 rows, of which few are in pieces: 128 rows of 8 heads over 4096 slots 36 us of 54 for workgroups without
+// work): every workgroup lists the notes that say something, and takes what is its own of them.
+constexpr int kMostJoints = 1024;
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256)
+void paged_join_listed_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
+{
+    __shared__ float tops[256];
+    __shared__ float sums[256][5];
+    __shared__ uint16_t list[kMostJoints];
+    __shared__ int counts[kMostJoints / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint64_t some[kMostJoints / 256];
+#pragma unroll
+    for (int n = 0; n < kMostJoints / 256; ++n) {
+        const int w = 256 * n + tid;
+        some[n] = __builtin_amdgcn_ballot_w64(w < a.workgroups && a.joints[min(w, a.workgroups - 1)].first >= 0);
+        if (lane == 0) counts[4 * n + wave] = __builtin_popcountll(some[n]);
+    }
+    __syncthreads();
+    int count = 0;
+#pragma unroll
+    for (int n = 0; n < kMostJoints / 256; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k == wave && (some[n] >> lane & 1) != 0) list[count + __builtin_popcountll(some[n] & (((uint64_t)1 << lane) - 1))] = (uint16_t)(256 * n + tid);
+            count += counts[4 * n + k];
+        }
+    __syncthreads();
+    const int slices = block_rows / ROWS;
+    for (int item = blockIdx.x; item < count * slices; item += gridDim.x) {
+        const int w = list[item / slices];
+        const Joint j = a.joints[w];
+        __syncthreads();                          // (the sums of the piece before have been read)
+        join_rows<T, ROWS>(a, j, w, item % slices * ROWS, block_rows, cols, tops, sums);
+    }
+}
+
 inline AttendArgs attend_args(const PagedArgs& p, int workgroups, int rows, int unit, int64_t size)
 {
     AttendArgs a;
@@ -278,7 +323,16 @@ template <typename T> hipError_t launch_join(const AttendArgs& a, int rows, int 
     // Few blocks are in many parts each: then more workgroups to a block.  4 rows a workgroup / 16, us of attention and join: a token over 16384 slots, one
     // kv head of 128 18.6 / 21.3, 8 kv heads and 4097 slots 12.6 / 12.5; 512 tokens over 14336 slots, 8 kv heads 159 / 146.
     const int64_t blocks = ((int64_t)a.tokens * a.group.d / rows + a.cache.batch) * a.cache.kv_heads;
-    if (blocks * 8 <= a.workgroups) paged_join_kernel<T, 4><<<dim3(a.workgroups, rows / 4), 256, 0, stream>>>(a, rows, cols);
+    const int few = blocks * 8 <= a.workgroups ? 4 : 16;
+    if (rows > 16 && a.workgroups <= kMostJoints) {
+        // so many pieces there are at most, where starts are in order
+        const int64_t pieces = (blocks < a.workgroups ? blocks : a.workgroups) * (rows / few);
+        const uint32_t grid = (uint32_t)(pieces < 2048 ? pieces : 2048);
+        if (few == 4) paged_join_listed_kernel<T, 4><<<grid, 256, 0, stream>>>(a, rows, cols);
+        else paged_join_listed_kernel<T, 16><<<grid, 256, 0, stream>>>(a, rows, cols);
+        return hipGetLastError();
+    }
+    if (few == 4) paged_join_kernel<T, 4><<<dim3(a.workgroups, rows / 4), 256, 0, stream>>>(a, rows, cols);
     else paged_join_kernel<T, 16><<<dim3(a.workgroups, rows / 16), 256, 0, stream>>>(a, rows, cols);
     return hipGetLastError();
 }

@@ -337,6 +337,7 @@ hipError_t launch_paged_tiles_both(const PagedArgs& a, hipStream_t stream);
 // The same over a cache that holds a byte an element (a.cache in bytes, a.dt the type of Q and O).
 int64_t byte_workspace(const PagedArgs& a);
 hipError_t launch_byte_attention(const PagedArgs& a, const ScalesView& scales, hipStream_t stream);
+int64_t byte_rows_workspace_f32(const PagedArgs& a);
 hipError_t launch_byte_rows_f32(const PagedArgs& a, const ScalesView& scales, hipStream_t stream);
 bool prefers_byte_tiles(const PagedArgs& a);
 int64_t byte_tiles_workspace(const PagedArgs& a);

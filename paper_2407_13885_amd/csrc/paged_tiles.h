@@ -921,9 +921,20 @@ template <typename T, int MODE> hipError_t launch_tiles(const PagedArgs& p, hipS
     });
 }
 
+// (fp32: beyond d = 128 only, prefers_byte_tiles says why)
+template <typename T, typename F> auto by_byte_row(int row_bytes, F&& f)
+{
+    if constexpr (sizeof(T) == 4) {
+        const int ub = (2 * row_bytes + 63) / 64;
+        return ub <= 5 ? f(IC<5>{}) : ub <= 6 ? f(IC<6>{}) : f(IC<8>{});
+    } else {
+        return by_row<T>(2 * row_bytes, f);
+    }
+}
+
 template <typename T, int MODE> hipError_t launch_byte_tiles(const PagedArgs& p, const ScalesView& scales, hipStream_t stream)
 {
-    return by_row<uint16_t>(2 * p.cache.row_bytes, [&](auto ubc) {
+    return by_byte_row<T>(p.cache.row_bytes, [&](auto ubc) {
         constexpr int UB = decltype(ubc)::value;
         if constexpr (sizeof(T) == 4 || UB > 5) return launch_bytes<T, UB, -1, MODE>(p, scales, stream);
         else return 2 * p.cache.row_bytes == UB * 64 ? launch_bytes<T, UB, 0, MODE>(p, scales, stream) : launch_bytes<T, UB, 32, MODE>(p, scales, stream);
@@ -932,7 +943,7 @@ template <typename T, int MODE> hipError_t launch_byte_tiles(const PagedArgs& p,
 
 template <typename T> int64_t byte_tiles_workspace(const PagedArgs& p)
 {
-    return by_row<uint16_t>(2 * p.cache.row_bytes, [&](auto ubc) {
+    return by_byte_row<T>(p.cache.row_bytes, [&](auto ubc) {
         constexpr int UB = decltype(ubc)::value;
         return partial_bytes(byte_workgroups<T, UB>(), TilesCfg<T, UB, true>::ROWS, TilesCfg<T, UB, true>::COLS);
     });
