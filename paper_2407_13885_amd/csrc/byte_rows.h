@@ -46,7 +46,8 @@ __device__ __forceinline__ u32x2 lds_read_tr8(const char* p)
     return u32x2{0u, 0u};
 #endif
 }
-template <typename T, int UB, int NX, int MODE, bool EXACT, int THREADS = 64 * ByteRowsCfg<UB, NX>::NW, int BLOCKS = ByteRowsCfg<UB, NX>::PER_CU>
+// EXACT: rows fill their place on chip.  UNIFORM: 16 keys lie in one page and share their scales, so that where they are and what they count are numbers of the wave.
+template <typename T, int UB, int NX, int MODE, bool EXACT, bool UNIFORM, int THREADS = 64 * ByteRowsCfg<UB, NX>::NW, int BLOCKS = ByteRowsCfg<UB, NX>::PER_CU>
 __global__ __launch_bounds__(THREADS, BLOCKS)
 void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
 {
@@ -73,6 +74,16 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
     const auto v_chunk = [](int key) __attribute__((always_inline)) {
         return UB % 2 == 0 ? (key & 3) | (key >> 2 & 4) : (key >> 1 & 1) | (key >> 3 & 2);
     };
+    int k_from[UB], v_from[XFERS];                // UNIFORM: where a lane's 16 bytes lie in the 16 keys
+    if constexpr (UNIFORM) {
+#pragma unroll
+        for (int j = 0; j < XFERS; ++j) {
+            const int x = j * 64 + lane, key = x / CPR, c = x - key * CPR;
+            const auto at = [&](int ch) __attribute__((always_inline)) { return (key & 15) * rb + (EXACT ? ch * 16 : chunk_in_row(ch * 16, rb)); };
+            if (j < UB) k_from[j] = at(c ^ L::k_chunk(key));
+            v_from[j] = at(c ^ v_chunk(key));
+        }
+    }
     Segment seg;
     while (walk.next(seg)) {
         const Sequence& seq = seg.seq;
@@ -135,27 +146,34 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
                 wait_vmem();
                 __syncthreads();
 
-                auto issue = [&](int key0, int s) __attribute__((always_inline)) {
-                    int64_t row[XFERS];
+                // K (v = 0) or V of a tile into stage s.  Past the end: the last slot, or, of 16 keys some of which are there, those behind them, which nobody sees.
+                // (Behind a row's end on chip: its first chunks, which meet zeros of Q and make columns of V that nobody stores.)
+                auto issue = [&](int v, int key0, int s) __attribute__((always_inline)) {
+                    const char* const from = v ? a.cache.V : a.cache.K;
+                    if constexpr (UNIFORM) {
+                        const char* half[2];
 #pragma unroll
-                    for (int j = 0; j < XFERS; ++j) {          // (past the end the last slot)
-                        const int slot = min(key0 + (j * 64 + lane) / CPR, k1 - 1) - k0;
-                        row[j] = place_offset(places[slot >> grain]) + (slot & ((1 << grain) - 1)) * rb;
-                    }
+                        for (int k = 0; k < 2; ++k) {
+                            const int64_t place = places[(min(key0 + 16 * k, k1 - 1) - k0) >> 4];
+                            half[k] = from + ((int64_t)(uint32_t)uniform((int)place) | (int64_t)(uniform((int)(place >> 32)) & 0xffff) << 32);
+                        }
 #pragma unroll
-                    for (int v = 0; v < 2; ++v)
+                        for (int j = 0; j < XFERS; ++j)
+                            dma16_untracked(half[j / UB], (uint32_t)(v ? v_from[j] : k_from[j % UB]), stage_at + (2 * s + v) * TILE + j * 1024);
+                    } else {
 #pragma unroll
                         for (int j = 0; j < XFERS; ++j) {
-                            const int x = j * 64 + lane, key = x / CPR, c = x - key * CPR;
+                            const int x = j * 64 + lane, key = x / CPR, c = x - key * CPR, slot = min(key0 + key, k1 - 1) - k0;
                             const int ch = v == 0 ? c ^ L::k_chunk(key) : c ^ v_chunk(key);
-                            // (behind a row's end on chip: its first chunks, which meet zeros of Q and make columns of V that nobody stores)
-                            dma16_untracked((v ? a.cache.V : a.cache.K) + row[j] + (EXACT ? ch * 16 : chunk_in_row(ch * 16, rb)), stage_at + (2 * s + v) * TILE + j * 1024);
+                            dma16_untracked(from + place_offset(places[slot >> grain]) + (slot & ((1 << grain) - 1)) * rb + (EXACT ? ch * 16 : chunk_in_row(ch * 16, rb)),
+                                            stage_at + (2 * s + v) * TILE + j * 1024);
                         }
+                    }
                 };
                 const auto high_of = [&](int key) __attribute__((always_inline)) {   // of a key's place the half with the scales
-                    return reinterpret_cast<const uint32_t*>(places)[2 * ((min(key, k1 - 1) - k0) >> grain) + 1];
+                    return reinterpret_cast<const uint32_t*>(places)[2 * ((min(key, k1 - 1) - k0) >> (UNIFORM ? 4 : grain)) + 1];
                 };
-                auto compute = [&](int key0, int s, bool more) __attribute__((always_inline)) {
+                auto compute = [&](int key0, int s, bool more, bool yet_more) __attribute__((always_inline)) {
                     const char* const kt = stage + 2 * s * TILE;
                     const char* const vt = kt + TILE;
                     if (more) arrived<3 * XFERS>();
@@ -163,7 +181,7 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
                     float x[NX][NK * 4];
 #pragma unroll
                     for (int k = 0; k < NK; ++k) {
-                        const float ks = key_scale(high_of(key0 + 16 * k + l16));
+                        const float ks = key_scale(high_of(key0 + 16 * k + (UNIFORM ? 0 : l16)));
                         f32x4 acc[NX];
 #pragma unroll
                         for (int n = 0; n < NX; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -182,14 +200,18 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) x[n][4 * k + r] = acc[n][r];
                     }
+                    if (yet_more) {                            // (K has been read: its place is the tile's after the next)
+                        wait_lds();
+                        issue(0, key0 + 2 * C::UNIT, s);
+                    }
                     const int key = key0 + 4 * quarter;        // + 16 k + r
                     const bool whole = key0 + KT <= k1 && ((key0 + KT - 1 <= first && key0 > last - a.rule.window) || key0 + KT <= prefix);
                     // the values' scales, which go into the weights (powers of 2: no rounding)
                     float vs[NK * 4];
 #pragma unroll
                     for (int k = 0; k < NK; ++k) {
-                        if (grain >= 2) {
-                            const float same = value_scale(high_of(key + 16 * k));
+                        if (UNIFORM || grain >= 2) {
+                            const float same = value_scale(high_of((UNIFORM ? key0 : key) + 16 * k));
 #pragma unroll
                             for (int r = 0; r < 4; ++r) vs[4 * k + r] = same;
                         } else {
@@ -231,7 +253,8 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
                         }
                         pw[n] = parts_of<PARTS>(y);
                     }
-                    if (more) arrived<2 * XFERS>();
+                    if (yet_more) arrived<3 * XFERS>();
+                    else if (more) arrived<2 * XFERS>();
                     else arrived<0>();
                     // fragments of V: 16 columns x the keys of this lane's weights
                     const int vkey = 4 * quarter + (l16 >> 1 & 3) + (l16 >> 3) * 16;
@@ -277,12 +300,18 @@ void byte_rows_kernel(AttendArgs a, ScalesView scales, int grain)
                     }
                 };
                 int key = k0 + wave * KT, s = 0;
-                if (key < k1) issue(key, 0);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int v = 0; v < 2; ++v)
+                        if (key + n * C::UNIT < k1) issue(v, key + n * C::UNIT, n);
                 for (; key < k1; key += C::UNIT, s ^= 1) {
-                    const bool more = key + C::UNIT < k1;
-                    if (more) issue(key + C::UNIT, s ^ 1);
-                    compute(key, s, more);
-                    wait_lds();                   // (the fragments have left the stage that is filled next)
+                    const bool more = key + C::UNIT < k1, yet_more = key + 2 * C::UNIT < k1;
+                    compute(key, s, more, yet_more);
+                    if (yet_more) {
+                        wait_lds();               // (the fragments have left the place that is filled next)
+                        issue(1, key + 2 * C::UNIT, s);
+                    }
                 }
                 k0 = k1;
             }
@@ -353,8 +382,9 @@ template <typename T, int UB, int NX, int MODE> hipError_t launch(const PagedArg
     const int grain = key_grain(a.cache, scales);
     // (rows that fill their place: kernels of their own for the usual sizes)
     constexpr bool OWN = UB != 3;
-    if (OWN && a.cache.row_bytes == C::DB) byte_rows_kernel<T, UB, NX, MODE, OWN><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
-    else byte_rows_kernel<T, UB, NX, MODE, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
+    if (grain < 4) byte_rows_kernel<T, UB, NX, MODE, false, false><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
+    else if (OWN && a.cache.row_bytes == C::DB) byte_rows_kernel<T, UB, NX, MODE, OWN, true><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
+    else byte_rows_kernel<T, UB, NX, MODE, false, true><<<a.workgroups, 64 * C::NW, 0, stream>>>(a, scales, grain);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     a.cache.row_bytes *= (int)sizeof(T);          // (of the output)
