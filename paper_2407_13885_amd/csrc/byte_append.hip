@@ -22,6 +22,8 @@ struct AppendArgs {
     ScalesView scales;
     TurnUnits queries, keys;
     FastDiv value_units;                          // units of a row of values
+    FastDiv per_block;                            // groups of heads, of keys and of values
+    int32_t blocks;                               // that the launch takes at a time
     int64_t rows, q_stride, kv_stride;
     int32_t tokens, heads, d, rot, most_blocks;   // most_blocks: of all sequences, at most
     uint32_t kv_workgroups, q_blocks, q_parts;
@@ -38,6 +40,7 @@ __device__ __forceinline__ void turn_apart(float& x, float& y, float c, float s)
 
 // LANES: so many share a block of a head; HOLD: units of it that a lane keeps (the others are read again).
 template <typename T, int V> constexpr int kHold = V == 8 ? 4 : 8;
+constexpr int kQueriesAtOnce = 4;                 // (the kernel has the registers of few waves: each has more on its way)
 
 template <typename T, int V, bool INTERLEAVED, int LANES>
 __global__ __launch_bounds__(256)
@@ -47,7 +50,7 @@ void byte_append_kernel(AppendArgs a)
     constexpr bool TWO = !INTERLEAVED || V == 1;
     constexpr int P = TWO ? V : V / 2, HOLD = kHold<T, V>, HEADS = LANES < 64 ? 64 / LANES : 1;   // HEADS: that a wave works on at once
     __shared__ uint32_t of[8];
-    __shared__ uint32_t tops[4];
+    __shared__ float tops[4];
     if (threadIdx.x < 8) of[threadIdx.x] = a.axes.of[threadIdx.x];
     __syncthreads();
     const CacheView& cache = a.cache;
@@ -68,46 +71,61 @@ void byte_append_kernel(AppendArgs a)
             return t >= s.first ? slot : (int64_t)-1;
         };
         const uint32_t w = blockIdx.x - a.kv_workgroups, block = w % a.q_blocks;
-        turn_rows<T, V, INTERLEAVED>(static_cast<const T*>(a.Q), static_cast<T*>(a.R), a.angles, a.axes.count, of, position, a.tokens, a.d, a.rot, a.rows, a.q_stride,
+        turn_rows<T, V, INTERLEAVED, kQueriesAtOnce>(static_cast<const T*>(a.Q), static_cast<T*>(a.R), a.angles, a.axes.count, of, position, a.tokens, a.d, a.rot, a.rows, a.q_stride,
                                      (int64_t)a.heads * a.d, 1.0f, a.queries, block, a.q_blocks, w / a.q_blocks, a.q_parts);
         return;
     }
 
     // ---- keys and values -------------------------------------------------------------------------------------------------------------------
     const int32_t size = (int32_t)a.scales.block.d;
-    const auto blocks_of = [&](int b) __attribute__((always_inline)) {   // that new tokens of sequence b lie in
-        const Sequence s = sequence_at(cache, a.starts, a.tokens, b);
+    const auto blocks_in = [&](const Sequence& s) __attribute__((always_inline)) {   // that its new tokens lie in
         if (s.tokens == 0 || s.length == 0) return 0;
         return (int32_t)(quotient(s.length - 1, a.scales.block) - quotient(max(0, s.length - s.tokens), a.scales.block)) + 1;
     };
-    const int32_t total = plan_total(cache.batch, lane, blocks_of);
-    const int32_t groups = (cache.kv_heads + HEADS - 1) / HEADS, per_block = 2 * groups;
+    const auto blocks_of = [&](int b) __attribute__((always_inline)) { return blocks_in(sequence_at(cache, a.starts, a.tokens, b)); };
+    // (of up to 64 sequences each lane holds one, read once)
+    const bool one_look = cache.batch <= 64;
+    Sequence own{0, 0, 0};
+    int32_t upto = 0, total;
+    if (one_look) {
+        if (lane < cache.batch) own = sequence_at(cache, a.starts, a.tokens, lane);
+        upto = wave_inclusive_sum(lane < cache.batch ? blocks_in(own) : 0, lane, cache.batch);
+        total = __builtin_amdgcn_readlane(upto, cache.batch - 1);
+    } else {
+        total = plan_total(cache.batch, lane, blocks_of);
+    }
     constexpr int AT_ONCE = LANES == 256 ? 1 : 4;              // items of a workgroup
     const int l = LANES == 256 ? (int)threadIdx.x : lane % LANES;
-    for (int64_t item = (int64_t)blockIdx.x * AT_ONCE + (AT_ONCE > 1 ? wave : 0); item < (int64_t)total * per_block; item += (int64_t)a.kv_workgroups * AT_ONCE) {
-        const int32_t block = (int32_t)(item / per_block), of_block = (int32_t)(item - (int64_t)block * per_block);
-        const bool value = of_block >= groups;
-        const int32_t head = (value ? of_block - groups : of_block) * HEADS + (HEADS > 1 ? lane / LANES : 0);
+    const uint32_t item = blockIdx.x * AT_ONCE + (AT_ONCE > 1 ? wave : 0), begin = quotient(item, a.per_block);
+    const int32_t of_block = (int32_t)(item - begin * a.per_block.d), groups = (int32_t)(a.per_block.d / 2);
+    const bool value = of_block >= groups;
+    const int32_t head = (value ? of_block - groups : of_block) * HEADS + (HEADS > 1 ? lane / LANES : 0);
+    if ((int32_t)begin >= a.blocks) return;
+    for (int32_t block = (int32_t)begin; block < total; block = plus(block, a.blocks)) {
         int32_t b, before;
-        plan_find(cache.batch, lane, block, blocks_of, b, before);
-        if (b >= cache.batch) break;              // (starts in no order)
-        const Sequence s = sequence_at(cache, a.starts, a.tokens, b);
+        Sequence s;
+        if (one_look) {
+            const uint64_t past = __builtin_amdgcn_ballot_w64(lane < cache.batch && upto > block);
+            if (past == 0) break;                 // (starts in no order)
+            b = __builtin_ctzll(past);
+            before = b > 0 ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
+            s = Sequence{__builtin_amdgcn_readlane(own.length, b), __builtin_amdgcn_readlane(own.tokens, b), __builtin_amdgcn_readlane(own.first, b)};
+        } else {
+            plan_find(cache.batch, lane, block, blocks_of, b, before);
+            if (b >= cache.batch) break;
+            s = sequence_at(cache, a.starts, a.tokens, b);
+        }
         const int32_t base = max(0, s.length - s.tokens);
         const int32_t slot0 = (int32_t)(quotient(base, a.scales.block) + (block - before)) * size;   // the block's first
         const int32_t first = max(slot0, base), count = min(slot0 + size, s.length) - first;          // its new ones
         const uint32_t page = quotient(slot0, cache.page);
         const int32_t id = cache.table[(int64_t)b * cache.max_pages + page];
-        if ((uint32_t)id >= (uint32_t)cache.pages) continue;  // no such page: nothing is cached
         const int32_t row0 = slot0 - (int32_t)(page * cache.page.d);
         const bool active = head < cache.kv_heads;
-        const int64_t place = (int64_t)id * cache.kv_heads + (active ? head : 0);
-        uint8_t* const at = (value ? a.Vc : a.Kc) + (place * cache.page.d + row0) * a.d;              // of slot0
-        uint8_t* const scale = (value ? a.scales.V : a.scales.K) + place * a.scales.per_page + quotient(row0, a.scales.block);
         const T* const src = static_cast<const T*>(value ? a.V : a.K) + (int64_t)(active ? head : 0) * a.d;
         const int64_t t0 = (int64_t)s.first + s.tokens - (s.length - first);                           // the token of slot `first`
         const FastDiv by_row = value ? a.value_units : a.keys.by_head;
         const int32_t units = active ? count * (int32_t)by_row.d : 0;
-        const int32_t held = first > slot0 ? (int32_t)*scale : 0;   // (the block had rows before)
 
         struct Unit { C a, b; };
         float x[HOLD][TWO ? 2 : 1][V];
@@ -143,18 +161,22 @@ void byte_append_kernel(AppendArgs a)
 #pragma unroll
             for (int e = 0; e < P; ++e) turn_apart(TWO ? y[0][e] : y[0][2 * e % V], TWO ? y[TWO ? 1 : 0][e] : y[0][(2 * e + 1) % V], co.x[e], si.x[e]);
         };
-        const auto largest = [](const float (&y)[TWO ? 2 : 1][V]) __attribute__((always_inline)) {
-            uint32_t top = 0;
+        // (fmaxf leaves NaN aside)
+        const auto largest = [](float top, const float (&y)[TWO ? 2 : 1][V]) __attribute__((always_inline)) {
 #pragma unroll
             for (int n = 0; n < (TWO ? 2 : 1); ++n)
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const uint32_t bits = __float_as_uint(y[n][e]) & 0x7fffffffu;
-                    top = max(top, bits < 0x7f800000u ? bits : 0u);   // (infinities and NaN come to be NaN and leave the others their scale)
-                }
+                for (int e = 0; e < V; e += 2) top = V == 1 ? fmaxf(top, fabsf(y[n][0])) : max3(top, fabsf(y[n][e]), fabsf(y[n][(e + 1) % V]));
             return top;
         };
-        const auto store = [&](int32_t u, const float (&y)[TWO ? 2 : 1][V], float up) __attribute__((always_inline)) {
+        const auto largest_finite = [](float top, const float (&y)[TWO ? 2 : 1][V]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < (TWO ? 2 : 1); ++n)
+#pragma unroll
+                for (int e = 0; e < V; ++e) top = fabsf(y[n][e]) < __builtin_inff() ? fmaxf(top, fabsf(y[n][e])) : top;
+            return top;
+        };
+        const auto store = [&](uint8_t* at, int32_t u, const float (&y)[TWO ? 2 : 1][V], float scale_up) __attribute__((always_inline)) {
             const int32_t row = (int32_t)quotient(u, by_row);
             const UnitColumns c = columns(row, u);
             uint8_t* const to = at + (int64_t)(first - slot0 + row) * a.d;
@@ -163,75 +185,114 @@ void byte_append_kernel(AppendArgs a)
                 if (n == 1 && c.b < 0) break;
                 uint8_t* const p = to + (n == 0 ? c.a : c.b);
                 if constexpr (V == 1) {
-                    *p = (uint8_t)pack_e4m3<false>(y[n][0] * up, 0.0f, 0);
+                    *p = (uint8_t)pack_e4m3<false>(y[n][0], 0.0f, 0, scale_up);
                 } else {
                     uint32_t w[V / 4 > 0 ? V / 4 : 1];
 #pragma unroll
-                    for (int q = 0; q < V / 4; ++q) w[q] = pack_e4m3(y[n][4 * q] * up, y[n][(4 * q + 1) % V] * up, y[n][(4 * q + 2) % V] * up, y[n][(4 * q + 3) % V] * up);
+                    for (int q = 0; q < V / 4; ++q) w[q] = pack_e4m3(y[n][4 * q], y[n][(4 * q + 1) % V], y[n][(4 * q + 2) % V], y[n][(4 * q + 3) % V], scale_up);
                     if constexpr (V == 8) *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[V / 4 > 1 ? 1 : 0]};
                     else *reinterpret_cast<uint32_t*>(p) = w[0];
                 }
             }
         };
 
-        uint32_t top = 0;
-        {
-            Unit raw[HOLD];
+        float top = 0.0f;
+        Unit raw[HOLD];                           // (on their way before it is known where they go)
 #pragma unroll
-            for (int n = 0; n < HOLD; ++n)
-                if (l + n * LANES < units) raw[n] = load(l + n * LANES);
+        for (int n = 0; n < HOLD; ++n)
+            if (l + n * LANES < units) raw[n] = load(l + n * LANES);
+        if ((uint32_t)id >= (uint32_t)cache.pages) continue;  // no such page: nothing is cached
+        const int64_t place = (int64_t)id * cache.kv_heads + (active ? head : 0);
+        uint8_t* const at = (value ? a.Vc : a.Kc) + (place * cache.page.d + row0) * a.d;              // of slot0
+        uint8_t* const scale = (value ? a.scales.V : a.scales.K) + place * a.scales.per_page + quotient(row0, a.scales.block);
+        const int32_t held = first > slot0 ? (int32_t)*scale : 0;   // (the block had rows before)
+        {
 #pragma unroll
             for (int n = 0; n < HOLD; ++n)
                 if (l + n * LANES < units) {
                     turn(l + n * LANES, raw[n], x[n]);
-                    top = max(top, largest(x[n]));
+                    top = largest(top, x[n]);
                 }
         }
         for (int32_t u = l + HOLD * LANES; u < units; u += LANES) {
             float y[TWO ? 2 : 1][V];
             turn(u, load(u), y);
-            top = max(top, largest(y));
+            top = largest(top, y);
         }
+        const auto of_all = [&](float x) __attribute__((always_inline)) {   // the lanes of the block
 #pragma unroll
-        for (int off = (LANES < 64 ? LANES : 64) / 2; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
-        if constexpr (LANES == 256) {
-            if (lane == 0) tops[wave] = top;
-            __syncthreads();
-            top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-            __syncthreads();
+            for (int off = (LANES < 64 ? LANES : 64) / 2; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
+            if constexpr (LANES == 256) {
+                if (lane == 0) tops[wave] = x;
+                __syncthreads();
+                x = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
+                __syncthreads();
+            }
+            return x;
+        };
+        top = of_all(top);
+        // (infinities and NaN come to be NaN and leave the others their scale: where there is one they are looked through once more)
+        if (__builtin_amdgcn_ballot_w64(top == __builtin_inff()) != 0) {
+            float rest = 0.0f;
+            for (int32_t u = l; u < units; u += LANES) {
+                float y[TWO ? 2 : 1][V];
+                turn(u, load(u), y);
+                rest = largest_finite(rest, y);
+            }
+            rest = of_all(rest);
+            top = top == __builtin_inff() ? rest : top;
         }
         if (!active) continue;
-        int e = exponent_for(top);
+        int e = exponent_for(__float_as_uint(top));
         if (first > slot0) {
             const int old = max(kLeastScale, min(held - 127, kMostScale));
-            if (e > old) {                        // older rows in units of the new scale
-                const float down = __uint_as_float((uint32_t)max(0, 127 + old - e) << 23);
-                uint32_t* const words = reinterpret_cast<uint32_t*>(at);
-                for (int32_t i = l; i < (first - slot0) * (a.d / 4); i += LANES) {
-                    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(words[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(words[i], true);
-                    words[i] = pack_e4m3(lo[0] * down, lo[1] * down, hi[0] * down, hi[1] * down);
-                }
+            if (e > old) {                        // in units of the new scale
+                const float down = scale_of(127 + e - old);
+                const auto again = [&](u32x4 w) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
+                        w[i] = pack_e4m3(lo[0], lo[1], hi[0], hi[1], down);
+                    }
+                    return w;
+                };
+                u32x4* const older = reinterpret_cast<u32x4*>(at);
+#pragma unroll 2
+                for (int32_t i = l; i < (first - slot0) * (a.d / 16); i += LANES) older[i] = again(older[i]);
             } else {
                 e = old;
             }
         }
         if (l == 0) *scale = (uint8_t)(e + 127);
-        const float up = __uint_as_float((uint32_t)(127 - e) << 23);
+        const float up = scale_of(e + 127);       // what the elements are in units of
+        // (beyond 448 of the greatest scale)
+        const auto clamp = [&](float (&y)[TWO ? 2 : 1][V]) __attribute__((always_inline)) {
+            if (e < kMostScale) return;
+            const float most = 448.0f * up;
+#pragma unroll
+            for (int n = 0; n < (TWO ? 2 : 1); ++n)
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[n][i] = fabsf(y[n][i]) < __builtin_inff() ? __builtin_amdgcn_fmed3f(y[n][i], -most, most) : y[n][i];
+        };
 #pragma unroll
         for (int n = 0; n < HOLD; ++n)
-            if (l + n * LANES < units) store(l + n * LANES, x[n], up);
+            if (l + n * LANES < units) {
+                clamp(x[n]);
+                store(at, l + n * LANES, x[n], up);
+            }
         for (int32_t u = l + HOLD * LANES; u < units; u += LANES) {
             float y[TWO ? 2 : 1][V];
             turn(u, load(u), y);
-            store(u, y, up);
+            clamp(y);
+            store(at, u, y, up);
         }
     }
 }
 
 template <typename T, int V, bool INTERLEAVED> hipError_t launch(AppendArgs a, hipStream_t stream)
 {
-    a.queries = turn_units<V, INTERLEAVED>(a.heads > 0 ? a.heads : 1, a.d, a.rot);
-    a.keys = turn_units<V, INTERLEAVED>(1, a.d, a.rot);
+    a.queries = turn_units<V, INTERLEAVED>(a.heads > 0 ? a.heads : 1, a.d, a.rot, kQueriesAtOnce);
+    a.keys = turn_units<V, INTERLEAVED>(1, a.d, a.rot, 1);
     a.value_units = fast_div((uint32_t)(a.d / V));
     const dim3 q = turn_grid(a.queries, a.tokens);
     a.q_blocks = q.x;
@@ -239,8 +300,11 @@ template <typename T, int V, bool INTERLEAVED> hipError_t launch(AppendArgs a, h
     const int64_t units = (int64_t)a.scales.block.d * (a.d / V);   // of a block, at most
     auto go = [&](auto kernel, int lanes) {
         const int64_t groups = lanes < 64 ? (a.cache.kv_heads + 64 / lanes - 1) / (64 / lanes) : a.cache.kv_heads;
-        const int64_t items = a.most_blocks * 2 * groups, all = lanes == 256 ? items : (items + 3) / 4;
-        a.kv_workgroups = (uint32_t)(all < 1 << 20 ? all : 1 << 20);
+        const int64_t at_once = ((int64_t)1 << 20) / (2 * groups);
+        a.per_block = fast_div((uint32_t)(2 * groups));
+        a.blocks = (int32_t)(a.most_blocks < at_once ? a.most_blocks : at_once);
+        const uint32_t items = (uint32_t)(a.blocks * 2 * groups);
+        a.kv_workgroups = lanes == 256 ? items : (items + 3) / 4;
         kernel<<<a.kv_workgroups + (a.heads > 0 ? a.q_blocks * a.q_parts : 0), 256, 0, stream>>>(a);
         return hipGetLastError();
     };

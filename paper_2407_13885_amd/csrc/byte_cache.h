@@ -24,16 +24,20 @@ __device__ __forceinline__ int exponent_for(uint32_t x)
     return max(kLeastScale, min((int)(x >> 23) - 127 - 8 + ((x & 0x7fffffu) > 0x600000u ? 1 : 0), kMostScale));
 }
 
-// To nearest even; numbers beyond 448 (where the scale is the greatest there is) as 448, infinities as NaN.
-__device__ __forceinline__ float in_reach(float x)
+// Numbers in units of a power of 2, to nearest even; what is infinite or beyond 464 of them as NaN.
+template <bool HIGH> __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi, uint32_t old, float scale)
 {
-    return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u ? __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f) : __builtin_nanf("");
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(__builtin_bit_cast(s16x2, old), lo, hi, scale, HIGH));
+#else
+    (void)lo;
+    (void)hi;
+    (void)scale;
+    return old;
+#endif
 }
-template <bool HIGH> __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi, uint32_t old)
-{
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(in_reach(lo), in_reach(hi), (int)old, HIGH);
-}
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) { return pack_e4m3<true>(c, d, pack_e4m3<false>(a, b, 0)); }
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d, float scale) { return pack_e4m3<true>(c, d, pack_e4m3<false>(a, b, 0, scale), scale); }
 
 // Four elements as bf16, times a power of 2; eight of them, the operand of a matrix instruction.
 __device__ __forceinline__ u32x2 bf16_of(uint32_t w, float scale)

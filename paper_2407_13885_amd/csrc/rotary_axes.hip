@@ -19,13 +19,13 @@ void rotary_axes_kernel(const T* X, T* Y, const float* __restrict__ angles, Axes
     __shared__ uint32_t of[8];
     if (threadIdx.x < 8) of[threadIdx.x] = axes.of[threadIdx.x];
     __syncthreads();
-    turn_rows<T, V, INTERLEAVED>(X, Y, angles, axes.count, of, [&](int64_t t, int axis) __attribute__((always_inline)) { return (int64_t)axes.positions[axis * axes.tokens + t]; },
+    turn_rows<T, V, INTERLEAVED, 1>(X, Y, angles, axes.count, of, [&](int64_t t, int axis) __attribute__((always_inline)) { return (int64_t)axes.positions[axis * axes.tokens + t]; },
                                  tokens, d, rot, rows, x_stride, y_stride, sign, u, blockIdx.x, gridDim.x, blockIdx.y, gridDim.y);
 }
 
 template <typename T, int V, bool INTERLEAVED> hipError_t launch(const RotaryArgs& a, const AxesView& axes, hipStream_t stream)
 {
-    const TurnUnits u = turn_units<V, INTERLEAVED>(a.heads, a.d, a.rot);
+    const TurnUnits u = turn_units<V, INTERLEAVED>(a.heads, a.d, a.rot, 1);
     rotary_axes_kernel<T, V, INTERLEAVED><<<turn_grid(u, a.tokens), 256, 0, stream>>>(static_cast<const T*>(a.Q), static_cast<T*>(a.R), a.angles, axes, (int32_t)a.tokens, (int32_t)a.d,
                                                                                 (int32_t)a.rot, a.rows, a.q_stride, a.r_stride, a.inverse ? -1.0f : 1.0f, u);
     return hipGetLastError();

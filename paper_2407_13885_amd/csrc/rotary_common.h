@@ -80,13 +80,14 @@ struct TurnUnits {
     int32_t per_token, block_tokens;
     FastDiv by_token, by_head;
 };
-template <int V, bool INTERLEAVED> inline TurnUnits turn_units(int64_t heads, int64_t d, int64_t rot)
+// (a block of threads takes `at_once` units a thread at a time)
+template <int V, bool INTERLEAVED> inline TurnUnits turn_units(int64_t heads, int64_t d, int64_t rot, int at_once)
 {
     TurnUnits u;
     u.pairs = (int32_t)(INTERLEAVED && V > 1 ? rot / V : rot / 2 / V);
     u.per_head = u.pairs + (int32_t)((d - rot) / V);
     u.per_token = (int32_t)heads * u.per_head;
-    u.block_tokens = u.per_token >= 256 ? 1 : 256 / u.per_token;
+    u.block_tokens = u.per_token >= 256 * at_once ? 1 : 256 * at_once / u.per_token;
     u.by_token = fast_div(u.per_token);
     u.by_head = fast_div(u.per_head);
     return u;
@@ -116,8 +117,8 @@ template <int V, bool INTERLEAVED> __device__ __forceinline__ UnitColumns unit_c
     return {a, !TWO ? a : INTERLEAVED ? 2 * x + 1 : x * V + rot / 2};
 }
 
-// Tokens from block `block` of `blocks` on: rows of X turned (sign -1: back) into rows of Y.  position(t, axis).
-template <typename T, int V, bool INTERLEAVED, typename Position>
+// Tokens from block `block` of `blocks` on: rows of X turned (sign -1: back) into rows of Y.  position(t, axis).  AT_ONCE: units that a thread loads before it stores any.
+template <typename T, int V, bool INTERLEAVED, int AT_ONCE, typename Position>
 __device__ __forceinline__ void turn_rows(const T* X, T* Y, const float* __restrict__ angles, int32_t axes, const uint32_t* of, Position&& position, int32_t tokens, int32_t d,
                                           int32_t rot, int64_t rows, int64_t x_stride, int64_t y_stride, float sign, const TurnUnits& u, uint32_t block, uint32_t blocks,
                                           uint32_t part, uint32_t parts)
@@ -127,29 +128,43 @@ __device__ __forceinline__ void turn_rows(const T* X, T* Y, const float* __restr
     constexpr int P = TWO ? V : V / 2;                         // pairs of a unit
     for (int64_t t0 = (int64_t)block * u.block_tokens; t0 < tokens; t0 += (int64_t)blocks * u.block_tokens) {
         const int32_t mine = (int32_t)min((int64_t)u.block_tokens, tokens - t0) * u.per_token;
-        for (int32_t i = threadIdx.x + part * 256; i < mine; i += 256 * parts) {
-            const int32_t in_block = u.block_tokens == 1 ? 0 : (int32_t)quotient(i, u.by_token), unit = i - in_block * u.per_token;
-            const int32_t head = (int32_t)quotient(unit, u.by_head), x = unit - head * u.per_head;
-            const int64_t t = t0 + in_block;
-            const T* const src = X + t * x_stride + (int64_t)head * d;
-            T* const dst = Y + t * y_stride + (int64_t)head * d;
-            const UnitColumns at = unit_columns<V, INTERLEAVED>(u, x, rot);
-            C va = *reinterpret_cast<const C*>(src + at.a), vb = va;
-            if (at.b >= 0) {
-                if constexpr (TWO) vb = *reinterpret_cast<const C*>(src + at.b);
-                Chunk<float, P> co, si;
-                load_angles<P>(angles, rot, rows, x * P, axes, of, [&](int axis) __attribute__((always_inline)) { return position(t, axis); }, co, si);
+        for (int32_t i0 = threadIdx.x + part * 256; i0 < mine; i0 += 256 * parts * AT_ONCE) {
+            C va[AT_ONCE], vb[AT_ONCE];
+            Chunk<float, P> co[AT_ONCE], si[AT_ONCE];
+            UnitColumns at[AT_ONCE];
+            T* dst[AT_ONCE];
 #pragma unroll
-                for (int e = 0; e < P; ++e) {
-                    T& p = TWO ? va.x[e] : va.x[2 * e % V];
-                    T& q = TWO ? vb.x[e] : va.x[(2 * e + 1) % V];
-                    const float a = wide(p), b = wide(q), c = co.x[e], s = sign * si.x[e];
-                    p = narrow<T>(a * c - b * s);
-                    q = narrow<T>(b * c + a * s);
+            for (int n = 0; n < AT_ONCE; ++n) {
+                const int32_t i = i0 + n * 256 * parts;
+                if (AT_ONCE > 1 && i >= mine) break;
+                const int32_t in_block = u.block_tokens == 1 ? 0 : (int32_t)quotient(i, u.by_token), unit = i - in_block * u.per_token;
+                const int32_t head = (int32_t)quotient(unit, u.by_head), x = unit - head * u.per_head;
+                const int64_t t = t0 + in_block;
+                const T* const src = X + t * x_stride + (int64_t)head * d;
+                dst[n] = Y + t * y_stride + (int64_t)head * d;
+                at[n] = unit_columns<V, INTERLEAVED>(u, x, rot);
+                va[n] = *reinterpret_cast<const C*>(src + at[n].a);
+                if (at[n].b >= 0) {
+                    if constexpr (TWO) vb[n] = *reinterpret_cast<const C*>(src + at[n].b);
+                    load_angles<P>(angles, rot, rows, x * P, axes, of, [&](int axis) __attribute__((always_inline)) { return position(t, axis); }, co[n], si[n]);
                 }
-                if constexpr (TWO) *reinterpret_cast<C*>(dst + at.b) = vb;
             }
-            *reinterpret_cast<C*>(dst + at.a) = va;
+#pragma unroll
+            for (int n = 0; n < AT_ONCE; ++n) {
+                if (AT_ONCE > 1 && i0 + n * 256 * (int32_t)parts >= mine) break;
+                if (at[n].b >= 0) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) {
+                        T& p = TWO ? va[n].x[e] : va[n].x[2 * e % V];
+                        T& q = TWO ? vb[n].x[e] : va[n].x[(2 * e + 1) % V];
+                        const float a = wide(p), b = wide(q), c = co[n].x[e], s = sign * si[n].x[e];
+                        p = narrow<T>(a * c - b * s);
+                        q = narrow<T>(b * c + a * s);
+                    }
+                    if constexpr (TWO) *reinterpret_cast<C*>(dst[n] + at[n].b) = vb[n];
+                }
+                *reinterpret_cast<C*>(dst[n] + at[n].a) = va[n];
+            }
         }
     }
 }
