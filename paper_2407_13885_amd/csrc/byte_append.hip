@@ -20,8 +20,8 @@ struct AppendArgs {
     AxesView axes;
     CacheView cache;
     ScalesView scales;
-    TurnUnits queries, keys;
-    FastDiv value_units;                          // units of a row of values
+    TurnUnits queries;
+    FastDiv key_units, value_units;               // units of a row of keys, of values
     FastDiv per_block;                            // groups of heads, of keys and of values
     int32_t blocks;                               // that the launch takes at a time
     int64_t rows, q_stride, kv_stride;
@@ -38,19 +38,24 @@ __device__ __forceinline__ void turn_apart(float& x, float& y, float c, float s)
     y = b;
 }
 
-// LANES: so many share a block of a head; HOLD: units of it that a lane keeps (the others are read again).
-template <typename T, int V> constexpr int kHold = V == 8 ? 4 : 8;
+// Of a row of keys or values a unit is V neighbouring columns (pairs, V > 1: INTERLEAVED) or twice V: those that turn together, or neighbours; in single columns (V = 1) a
+// pair of columns, or one that does not turn.
+// LANES: so many share a block of a head; HOLD: units of it that a lane keeps (32 elements, 16 of single columns; the others are read again).
+template <int V, bool INTERLEAVED> constexpr int kHold = V == 1 ? 8 : (INTERLEAVED ? 32 : 16) / V;
+constexpr int kStaged = 4096;                     // angles in LDS, of the tokens whose queries a workgroup turns
 constexpr int kQueriesAtOnce = 4;                 // (the kernel has the registers of few waves: each has more on its way)
 
-template <typename T, int V, bool INTERLEAVED, int LANES>
-__global__ __launch_bounds__(256)
+// (Neighbouring columns: held to the registers of four waves of a SIMD, 9045 tokens of 48 heads of 128 58.8 -> 54.6 us; halves, which hold more at once, 48 us, so held 59.)
+template <typename T, int V, bool INTERLEAVED, int LANES, int WAVES = (INTERLEAVED && V > 1 ? 4 : 1)>
+__global__ __launch_bounds__(256, WAVES)
 void byte_append_kernel(AppendArgs a)
 {
     typedef Chunk<T, V> C;
     constexpr bool TWO = !INTERLEAVED || V == 1;
-    constexpr int P = TWO ? V : V / 2, HOLD = kHold<T, V>, HEADS = LANES < 64 ? 64 / LANES : 1;   // HEADS: that a wave works on at once
+    constexpr int P = TWO ? V : V / 2, HOLD = kHold<V, INTERLEAVED>, HEADS = LANES < 64 ? 64 / LANES : 1;   // HEADS: that a wave works on at once
     __shared__ uint32_t of[8];
     __shared__ float tops[4];
+    __shared__ __align__(32) float staged[kStaged];
     if (threadIdx.x < 8) of[threadIdx.x] = a.axes.of[threadIdx.x];
     __syncthreads();
     const CacheView& cache = a.cache;
@@ -71,7 +76,7 @@ void byte_append_kernel(AppendArgs a)
             return t >= s.first ? slot : (int64_t)-1;
         };
         const uint32_t w = blockIdx.x - a.kv_workgroups, block = w % a.q_blocks;
-        turn_rows<T, V, INTERLEAVED, kQueriesAtOnce>(static_cast<const T*>(a.Q), static_cast<T*>(a.R), a.angles, a.axes.count, of, position, a.tokens, a.d, a.rot, a.rows, a.q_stride,
+        turn_rows_staged<T, V, INTERLEAVED, kQueriesAtOnce>(static_cast<const T*>(a.Q), static_cast<T*>(a.R), a.angles, a.axes.count, of, staged, position, a.tokens, a.d, a.rot, a.rows, a.q_stride,
                                      (int64_t)a.heads * a.d, 1.0f, a.queries, block, a.q_blocks, w / a.q_blocks, a.q_parts);
         return;
     }
@@ -124,18 +129,27 @@ void byte_append_kernel(AppendArgs a)
         const bool active = head < cache.kv_heads;
         const T* const src = static_cast<const T*>(value ? a.V : a.K) + (int64_t)(active ? head : 0) * a.d;
         const int64_t t0 = (int64_t)s.first + s.tokens - (s.length - first);                           // the token of slot `first`
-        const FastDiv by_row = value ? a.value_units : a.keys.by_head;
+        const FastDiv by_row = value ? a.value_units : a.key_units;
         const int32_t units = active ? count * (int32_t)by_row.d : 0;
 
+        const auto position = [&](int64_t t, int axis) __attribute__((always_inline)) {
+            return a.axes.positions ? (int64_t)a.axes.positions[axis * a.axes.tokens + t] : first + (t - t0);
+        };
         struct Unit { C a, b; };
         float x[HOLD][TWO ? 2 : 1][V];
+        const int32_t turning = value ? 0 : (TWO ? a.rot / 2 : a.rot) / V;   // units of a row
+        struct Columns { int32_t a, b; bool turned; };         // b < 0: none
         const auto columns = [&](int32_t row, int32_t u) __attribute__((always_inline)) {
-            const int32_t k = u - row * (int32_t)by_row.d;
-            return value ? UnitColumns{k * V, -1} : unit_columns<V, INTERLEAVED>(a.keys, k, a.rot);
+            const int32_t k = u - row * (int32_t)by_row.d, rest = (value ? 0 : a.rot) + (k - turning) * (TWO && V > 1 ? 2 * V : V);
+            Columns c;
+            c.turned = k < turning;
+            c.a = !c.turned ? rest : INTERLEAVED && V == 1 ? 2 * k : k * V;
+            c.b = !TWO ? -1 : c.turned ? (INTERLEAVED ? c.a + 1 : c.a + a.rot / 2) : V > 1 ? rest + V : -1;
+            return c;
         };
         const auto load = [&](int32_t u) __attribute__((always_inline)) {
             const int32_t row = (int32_t)quotient(u, by_row);
-            const UnitColumns c = columns(row, u);
+            const Columns c = columns(row, u);
             const T* const p = src + (t0 + row) * a.kv_stride;
             Unit r;
             r.a = *reinterpret_cast<const C*>(p + c.a);
@@ -146,18 +160,16 @@ void byte_append_kernel(AppendArgs a)
         };
         const auto turn = [&](int32_t u, const Unit& r, float (&y)[TWO ? 2 : 1][V]) __attribute__((always_inline)) {
             const int32_t row = (int32_t)quotient(u, by_row);
-            const UnitColumns c = columns(row, u);
+            const Columns c = columns(row, u);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 y[0][e] = wide(r.a.x[e]);
                 if constexpr (TWO) y[TWO ? 1 : 0][e] = c.b < 0 ? 0.0f : wide(r.b.x[e]);
             }
-            if (c.b < 0) return;
+            if (!c.turned) return;
+            const int32_t pair = (u - row * (int32_t)by_row.d) * P;
             Chunk<float, P> co, si;
-            load_angles<P>(a.angles, a.rot, a.rows, (u - row * (int32_t)by_row.d) * P, a.axes.count, of,
-                           [&](int axis) __attribute__((always_inline)) {
-                               return a.axes.positions ? (int64_t)a.axes.positions[axis * a.axes.tokens + t0 + row] : (int64_t)first + row;
-                           }, co, si);
+            load_angles<P>(a.angles, a.rot, a.rows, pair, a.axes.count, of, [&](int axis) __attribute__((always_inline)) { return position(t0 + row, axis); }, co, si);
 #pragma unroll
             for (int e = 0; e < P; ++e) turn_apart(TWO ? y[0][e] : y[0][2 * e % V], TWO ? y[TWO ? 1 : 0][e] : y[0][(2 * e + 1) % V], co.x[e], si.x[e]);
         };
@@ -178,7 +190,7 @@ void byte_append_kernel(AppendArgs a)
         };
         const auto store = [&](uint8_t* at, int32_t u, const float (&y)[TWO ? 2 : 1][V], float scale_up) __attribute__((always_inline)) {
             const int32_t row = (int32_t)quotient(u, by_row);
-            const UnitColumns c = columns(row, u);
+            const Columns c = columns(row, u);
             uint8_t* const to = at + (int64_t)(first - slot0 + row) * a.d;
 #pragma unroll
             for (int n = 0; n < (TWO ? 2 : 1); ++n) {
@@ -291,13 +303,14 @@ void byte_append_kernel(AppendArgs a)
 
 template <typename T, int V, bool INTERLEAVED> hipError_t launch(AppendArgs a, hipStream_t stream)
 {
-    a.queries = turn_units<V, INTERLEAVED>(a.heads > 0 ? a.heads : 1, a.d, a.rot, kQueriesAtOnce);
-    a.keys = turn_units<V, INTERLEAVED>(1, a.d, a.rot, 1);
-    a.value_units = fast_div((uint32_t)(a.d / V));
+    a.queries = turn_units<V, INTERLEAVED>(a.heads > 0 ? a.heads : 1, a.d, a.rot, kQueriesAtOnce, kStaged);
+    const int64_t of_values = a.d / (INTERLEAVED || V == 1 ? V : 2 * V), of_keys = V > 1 ? of_values : a.rot / 2 + (a.d - a.rot);
+    a.key_units = fast_div((uint32_t)of_keys);
+    a.value_units = fast_div((uint32_t)of_values);
     const dim3 q = turn_grid(a.queries, a.tokens);
     a.q_blocks = q.x;
     a.q_parts = q.y;
-    const int64_t units = (int64_t)a.scales.block.d * (a.d / V);   // of a block, at most
+    const int64_t units = (int64_t)a.scales.block.d * of_values;   // of a block, at most
     auto go = [&](auto kernel, int lanes) {
         const int64_t groups = lanes < 64 ? (a.cache.kv_heads + 64 / lanes - 1) / (64 / lanes) : a.cache.kv_heads;
         const int64_t at_once = ((int64_t)1 << 20) / (2 * groups);
@@ -308,8 +321,8 @@ template <typename T, int V, bool INTERLEAVED> hipError_t launch(AppendArgs a, h
         kernel<<<a.kv_workgroups + (a.heads > 0 ? a.q_blocks * a.q_parts : 0), 256, 0, stream>>>(a);
         return hipGetLastError();
     };
-    if (units <= 16 * kHold<T, V>) return go(byte_append_kernel<T, V, INTERLEAVED, 16>, 16);
-    if (units <= 64 * kHold<T, V>) return go(byte_append_kernel<T, V, INTERLEAVED, 64>, 64);
+    if (units <= 16 * kHold<V, INTERLEAVED>) return go(byte_append_kernel<T, V, INTERLEAVED, 16>, 16);
+    if (units <= 64 * kHold<V, INTERLEAVED>) return go(byte_append_kernel<T, V, INTERLEAVED, 64>, 64);
     return go(byte_append_kernel<T, V, INTERLEAVED, 256>, 256);
 }
 

@@ -74,20 +74,48 @@ __device__ __forceinline__ void load_angles(const float* __restrict__ angles, in
     }
 }
 
+// cos and sin of pair j of a token that stands at position(axis).
+template <typename Position>
+__device__ __forceinline__ f32x2 angle_of(const float* __restrict__ angles, int32_t rot, int64_t rows, int32_t axes, const uint32_t* of, int32_t j, Position&& position)
+{
+    const int64_t p = position(axes == 1 ? 0 : (int)(of[j >> 4] >> 2 * (j & 15) & 3));
+    const bool known = p >= 0 && p < rows;
+    const float* const row = angles + (known ? p : 0) * (int64_t)rot + j;
+    const float c = row[0], s = row[rot / 2];
+    return known ? f32x2{c, s} : f32x2{__builtin_nanf(""), __builtin_nanf("")};
+}
+
+// The angles of whole tokens, side by side in LDS: cos and sin of the pairs as their axes have them.  (All heads of a token use them; where axes take pairs in turns,
+// every unit would read a row for each.)
+template <typename Position>
+__device__ __forceinline__ void stage_angles(float* staged, const float* __restrict__ angles, int32_t rot, const FastDiv& by_half, int64_t rows, int32_t axes, const uint32_t* of,
+                                             int32_t tokens, int64_t t0, Position&& position, int32_t thread, int32_t threads)
+{
+    const int32_t half = rot / 2;
+    for (int32_t i = thread; i < tokens * half; i += threads) {
+        const int32_t t = (int32_t)quotient(i, by_half), j = i - t * half;
+        const f32x2 cs = angle_of(angles, rot, rows, axes, of, j, [&](int axis) __attribute__((always_inline)) { return position(t0 + t, axis); });
+        staged[t * rot + j] = cs[0];
+        staged[t * rot + half + j] = cs[1];
+    }
+}
+
 // How the rows of a token fall into units: V columns and their V partners (halves), V neighbouring columns (pairs), or V columns behind the turned ones.
 struct TurnUnits {
     int32_t per_head, pairs;                      // units of a head; those of them that turn
     int32_t per_token, block_tokens;
-    FastDiv by_token, by_head;
+    FastDiv by_token, by_head, by_half;           // by_half: pairs of a token's angles
 };
-// (a block of threads takes `at_once` units a thread at a time)
-template <int V, bool INTERLEAVED> inline TurnUnits turn_units(int64_t heads, int64_t d, int64_t rot, int at_once)
+// (a block of threads takes `at_once` units a thread at a time, of tokens with at most so many angles)
+template <int V, bool INTERLEAVED> inline TurnUnits turn_units(int64_t heads, int64_t d, int64_t rot, int at_once, int angles)
 {
     TurnUnits u;
     u.pairs = (int32_t)(INTERLEAVED && V > 1 ? rot / V : rot / 2 / V);
     u.per_head = u.pairs + (int32_t)((d - rot) / V);
     u.per_token = (int32_t)heads * u.per_head;
     u.block_tokens = u.per_token >= 256 * at_once ? 1 : 256 * at_once / u.per_token;
+    if (u.block_tokens * rot > angles) u.block_tokens = (int32_t)(angles / rot);
+    u.by_half = fast_div((uint32_t)(rot > 0 ? rot / 2 : 1));
     u.by_token = fast_div(u.per_token);
     u.by_head = fast_div(u.per_head);
     return u;
@@ -117,8 +145,22 @@ template <int V, bool INTERLEAVED> __device__ __forceinline__ UnitColumns unit_c
     return {a, !TWO ? a : INTERLEAVED ? 2 * x + 1 : x * V + rot / 2};
 }
 
-// Tokens from block `block` of `blocks` on: rows of X turned (sign -1: back) into rows of Y.  position(t, axis).  AT_ONCE: units that a thread loads before it stores any.
-template <typename T, int V, bool INTERLEAVED, int AT_ONCE, typename Position>
+// A unit turned.
+template <bool TWO, typename T, int V, int P>
+__device__ __forceinline__ void turn_unit(Chunk<T, V>& va, Chunk<T, V>& vb, const Chunk<float, P>& co, const Chunk<float, P>& si, float sign)
+{
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+        T& p = TWO ? va.x[e] : va.x[2 * e % V];
+        T& q = TWO ? vb.x[e] : va.x[(2 * e + 1) % V];
+        const float a = wide(p), b = wide(q), c = co.x[e], s = sign * si.x[e];
+        p = narrow<T>(a * c - b * s);
+        q = narrow<T>(b * c + a * s);
+    }
+}
+
+// Tokens from block `block` of `blocks` on: rows of X turned (sign -1: back) into rows of Y.  position(t, axis).
+template <typename T, int V, bool INTERLEAVED, typename Position>
 __device__ __forceinline__ void turn_rows(const T* X, T* Y, const float* __restrict__ angles, int32_t axes, const uint32_t* of, Position&& position, int32_t tokens, int32_t d,
                                           int32_t rot, int64_t rows, int64_t x_stride, int64_t y_stride, float sign, const TurnUnits& u, uint32_t block, uint32_t blocks,
                                           uint32_t part, uint32_t parts)
@@ -128,44 +170,75 @@ __device__ __forceinline__ void turn_rows(const T* X, T* Y, const float* __restr
     constexpr int P = TWO ? V : V / 2;                         // pairs of a unit
     for (int64_t t0 = (int64_t)block * u.block_tokens; t0 < tokens; t0 += (int64_t)blocks * u.block_tokens) {
         const int32_t mine = (int32_t)min((int64_t)u.block_tokens, tokens - t0) * u.per_token;
-        for (int32_t i0 = threadIdx.x + part * 256; i0 < mine; i0 += 256 * parts * AT_ONCE) {
-            C va[AT_ONCE], vb[AT_ONCE];
-            Chunk<float, P> co[AT_ONCE], si[AT_ONCE];
-            UnitColumns at[AT_ONCE];
-            T* dst[AT_ONCE];
+        for (int32_t i = threadIdx.x + part * 256; i < mine; i += 256 * parts) {
+            const int32_t in_block = u.block_tokens == 1 ? 0 : (int32_t)quotient(i, u.by_token), unit = i - in_block * u.per_token;
+            const int32_t head = (int32_t)quotient(unit, u.by_head), x = unit - head * u.per_head;
+            const int64_t t = t0 + in_block;
+            const T* const src = X + t * x_stride + (int64_t)head * d;
+            T* const dst = Y + t * y_stride + (int64_t)head * d;
+            const UnitColumns at = unit_columns<V, INTERLEAVED>(u, x, rot);
+            C va = *reinterpret_cast<const C*>(src + at.a), vb = va;
+            if (at.b >= 0) {
+                if constexpr (TWO) vb = *reinterpret_cast<const C*>(src + at.b);
+                Chunk<float, P> co, si;
+                load_angles<P>(angles, rot, rows, x * P, axes, of, [&](int axis) __attribute__((always_inline)) { return position(t, axis); }, co, si);
+                turn_unit<TWO>(va, vb, co, si, sign);
+                if constexpr (TWO) *reinterpret_cast<C*>(dst + at.b) = vb;
+            }
+            *reinterpret_cast<C*>(dst + at.a) = va;
+        }
+    }
+}
+
+// The same with the angles of the tokens in LDS (u made for so many).  AT_ONCE: units that a thread loads before it stores any.
+template <typename T, int V, bool INTERLEAVED, int AT_ONCE, typename Position>
+__device__ __forceinline__ void turn_rows_staged(const T* X, T* Y, const float* __restrict__ angles, int32_t axes, const uint32_t* of, float* staged, Position&& position,
+                                          int32_t tokens, int32_t d, int32_t rot, int64_t rows, int64_t x_stride, int64_t y_stride, float sign, const TurnUnits& u,
+                                          uint32_t block, uint32_t blocks, uint32_t part, uint32_t parts)
+{
+    typedef Chunk<T, V> C;
+    constexpr bool TWO = !INTERLEAVED || V == 1;
+    constexpr int P = TWO ? V : V / 2;                         // pairs of a unit
+    for (int64_t t0 = (int64_t)block * u.block_tokens; t0 < tokens; t0 += (int64_t)blocks * u.block_tokens) {
+        const int32_t here = (int32_t)min((int64_t)u.block_tokens, tokens - t0), mine = here * u.per_token;
+        C va[AT_ONCE], vb[AT_ONCE];
+        UnitColumns at[AT_ONCE];
+        T* dst[AT_ONCE];
+        const float* turns[AT_ONCE];
+        const auto load = [&](int32_t i0) __attribute__((always_inline)) {
 #pragma unroll
             for (int n = 0; n < AT_ONCE; ++n) {
-                const int32_t i = i0 + n * 256 * parts;
-                if (AT_ONCE > 1 && i >= mine) break;
+                const int32_t i = i0 + n * 256 * (int32_t)parts;
+                if (i >= mine) break;
                 const int32_t in_block = u.block_tokens == 1 ? 0 : (int32_t)quotient(i, u.by_token), unit = i - in_block * u.per_token;
                 const int32_t head = (int32_t)quotient(unit, u.by_head), x = unit - head * u.per_head;
                 const int64_t t = t0 + in_block;
                 const T* const src = X + t * x_stride + (int64_t)head * d;
                 dst[n] = Y + t * y_stride + (int64_t)head * d;
                 at[n] = unit_columns<V, INTERLEAVED>(u, x, rot);
+                turns[n] = staged + in_block * rot + x * P;
                 va[n] = *reinterpret_cast<const C*>(src + at[n].a);
-                if (at[n].b >= 0) {
-                    if constexpr (TWO) vb[n] = *reinterpret_cast<const C*>(src + at[n].b);
-                    load_angles<P>(angles, rot, rows, x * P, axes, of, [&](int axis) __attribute__((always_inline)) { return position(t, axis); }, co[n], si[n]);
-                }
+                if constexpr (TWO)
+                    if (at[n].b >= 0) vb[n] = *reinterpret_cast<const C*>(src + at[n].b);
             }
+        };
+        const int32_t first = threadIdx.x + part * 256;
+        load(first);
+        stage_angles(staged, angles, rot, u.by_half, rows, axes, of, here, t0, position, threadIdx.x, 256);
+        __syncthreads();
+        for (int32_t i0 = first; i0 < mine; i0 += 256 * parts * AT_ONCE) {
+            if (i0 != first) load(i0);
 #pragma unroll
             for (int n = 0; n < AT_ONCE; ++n) {
-                if (AT_ONCE > 1 && i0 + n * 256 * (int32_t)parts >= mine) break;
+                if (i0 + n * 256 * (int32_t)parts >= mine) break;
                 if (at[n].b >= 0) {
-#pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        T& p = TWO ? va[n].x[e] : va[n].x[2 * e % V];
-                        T& q = TWO ? vb[n].x[e] : va[n].x[(2 * e + 1) % V];
-                        const float a = wide(p), b = wide(q), c = co[n].x[e], s = sign * si[n].x[e];
-                        p = narrow<T>(a * c - b * s);
-                        q = narrow<T>(b * c + a * s);
-                    }
+                    turn_unit<TWO>(va[n], vb[n], *reinterpret_cast<const Chunk<float, P>*>(turns[n]), *reinterpret_cast<const Chunk<float, P>*>(turns[n] + rot / 2), sign);
                     if constexpr (TWO) *reinterpret_cast<C*>(dst[n] + at[n].b) = vb[n];
                 }
                 *reinterpret_cast<C*>(dst[n] + at[n].a) = va[n];
             }
         }
+        __syncthreads();      // (the angles have been read)
     }
 }
 
