@@ -256,7 +256,7 @@ void paged_join_kernel(AttendArgs a, int32_t block_rows, int32_t cols)
 }
 
 // The same where that would be many more than there are (blocks of 128 rows, of which few are in pieces: 128 rows of 8 heads over 4096 slots 36 us of 54 for workgroups without
-// work): every workgroup lists the notes that say something, and takes what is its own of them.
+// work, listed 8): every workgroup lists the notes that say something, and takes what is its own of them.  (Up to 2048 workgroups 5 us, listed 7.)
 constexpr int kMostJoints = 1024;
 template <typename T, int ROWS>
 __global__ __launch_bounds__(256)
@@ -324,7 +324,7 @@ template <typename T> hipError_t launch_join(const AttendArgs& a, int rows, int 
     // kv head of 128 18.6 / 21.3, 8 kv heads and 4097 slots 12.6 / 12.5; 512 tokens over 14336 slots, 8 kv heads 159 / 146.
     const int64_t blocks = ((int64_t)a.tokens * a.group.d / rows + a.cache.batch) * a.cache.kv_heads;
     const int few = blocks * 8 <= a.workgroups ? 4 : 16;
-    if (rows > 16 && a.workgroups <= kMostJoints) {
+    if (rows > 16 && a.workgroups * (rows / few) > 2048 && a.workgroups <= kMostJoints) {
         // so many pieces there are at most, where starts are in order
         const int64_t pieces = (blocks < a.workgroups ? blocks : a.workgroups) * (rows / few);
         const uint32_t grid = (uint32_t)(pieces < 2048 ? pieces : 2048);

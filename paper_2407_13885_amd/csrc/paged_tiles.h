@@ -654,7 +654,7 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
                     });
                     if constexpr (BYTES && UNIFORM) {          // of K tiles t + 4 and t + 5, or, t odd, of V t and t + 1
                         constexpr bool V = BUF % 2 == 1;
-                        constexpr int READ = STEPS * 5 / 8;
+                        constexpr int READ = STEPS * 11 / 16;
                         static_assert(READ + 2 * C::XR < STEPS);
                         if constexpr (I < C::XR) bring_piece(V, V ? t : t + 4, I);
                         if constexpr (I == READ) {
