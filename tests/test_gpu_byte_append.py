@@ -147,6 +147,29 @@ def test_a_block_that_fills_token_by_token(dtype):
         p.dev["lengths"] += 1
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [HALVES, PAIRS])
+@pytest.mark.parametrize("pad", [1, 4, 8])
+def test_strides(dtype, layout, pad):
+    """Rows that start at any element, beside each other in rows of any length: in chunks or element by element."""
+    p = Problem8(dtype, [(5, 40), (33, 70), (1, 17)], 3, 2, 32, 16, 8, seed=pad).on_gpu()
+    x, table = new_rows(p, pad), table_of(400, 24)
+    q, k, v = x.split([96, 64, 64], 1)
+    q_dev, kv_dev = (torch.full((p.T, n + pad), 7.0, dtype=x.dtype, device="cuda") for n in (96, 64))
+    q_dev[:, :96] = q.cuda()
+    kv_dev[:, :64] = k.cuda()
+    v_dev = kv_dev.clone()
+    v_dev[:, :64] = v.cuda()
+    R = torch.full((p.T, 3, 32), 7.0, dtype=x.dtype, device="cuda")
+    attnw.attnw_byte_cache_append(p.cache, q_dev, kv_dev, v_dev, R, table.cuda(), None, None, p.dev["starts"], p.T, 3, 24, 400, 96 + pad, 64 + pad, layout)
+    torch.cuda.synchronize()
+    at = torch.cat([torch.arange(m - n, m) for n, m in p.sequences])[None]
+    q = q.reshape(p.T, 3, 32)
+    within(R, turned32(q, table.cpu(), at, [0] * 12, 24, layout).double(), 2 * bound_of(q, dtype), "R")
+    rows = {"K": turned32(k.reshape(p.T, 2, 32), table.cpu(), at, [0] * 12, 24, layout), "V": v.reshape(p.T, 2, 32).float()}
+    check(p, {n: appended(getattr(p, n + "8"), getattr(p, n + "_scales"), 8, p.table, p.lengths, p.starts, 16, rows[n]) for n in "KV"})
+
+
 def test_what_is_not_cached():
     """Tokens before a sequence's first slot, pages that are none, rows that no sequence owns, no queries; K and V elsewhere stay as they were."""
     p = Problem8("bf16", [(6, 40), (30, 50), (2, 20)], 4, 2, 64, 16, 16, seed=8)
