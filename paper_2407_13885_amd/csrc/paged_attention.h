@@ -321,7 +321,7 @@ inline int64_t partial_bytes(int workgroups, int rows, int cols) { return (int64
 template <typename T> hipError_t launch_join(const AttendArgs& a, int rows, int cols, hipStream_t stream)
 {
     // Few blocks are in many parts each: then more workgroups to a block.  4 rows a workgroup / 16, us of attention and join: a token over 16384 slots, one
-    // kv head of 128 18.6 / 21.3, 8 kv heads and 4097 slots 12.6 / 12.5; 512 tokens over 14336 slots, 8 kv heads 159 / 146.
+    // kv head of 128 18.6 / 21.3, 8 kv heads and 4097 slots 12.6 / 12.5; 512 tokens over 14336 slots, 8 kv heads (blocks of 128 rows, before their pieces were listed) 159 / 146.
     const int64_t blocks = ((int64_t)a.tokens * a.group.d / rows + a.cache.batch) * a.cache.kv_heads;
     const int few = blocks * 8 <= a.workgroups ? 4 : 16;
     if (rows > 16 && a.workgroups * (rows / few) > 2048 && a.workgroups <= kMostJoints) {

@@ -10,7 +10,10 @@
 // heads on 8 of 128, causal, 482 to 514 us (1.07 to 1.0 PFLOP/s); fp32 ragged chunks of d = 80 with bias, window and prefix 48 us.
 //
 // BYTES: a cache in 8 bits (byte_cache.h).  Two tiles of keys, then two of values, come as they lie in memory; the wave that brought 16 bytes a lane makes bf16 of them, scales
-// included, where the other kernels have the rows themselves.  From there on everything is the same; fp32 queries and weights are three bf16 parts each.
+// included, where the other kernels have the rows themselves.  From there on everything is the same; fp32 queries and weights are three bf16 parts each.  The read is
+// half, the work of every workgroup a quarter of the vector unit more: the chunk above 505 to 540 us by the card and its clock, beside 486 to 510 over a cache in bf16.  In the
+// loop of tiles that all rows see whole the pieces are asked for, read and laid among the steps of the products (in a row: 691 us); places, where keys
+// lie, are half as many as elsewhere, for room on chip.
 #pragma once
 
 #include "paged_attention.h"
@@ -654,7 +657,7 @@ void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
                     });
                     if constexpr (BYTES && UNIFORM) {          // of K tiles t + 4 and t + 5, or, t odd, of V t and t + 1
                         constexpr bool V = BUF % 2 == 1;
-                        constexpr int READ = STEPS * 11 / 16;
+                        constexpr int READ = STEPS * 11 / 16;  // (when they have arrived; at 1/2 530 us, 5/8 525, 11/16 515, later 522 to 526)
                         static_assert(READ + 2 * C::XR < STEPS);
                         if constexpr (I < C::XR) bring_piece(V, V ? t : t + 4, I);
                         if constexpr (I == READ) {
