@@ -1,4 +1,4 @@
-// Attention over a paged cache in 8 bits by blocks of 64 or 128 rows (paged_tiles.h), fp32, d above 128.
+// Attention over a paged cache in 8 bits by blocks of 128 rows (paged_tiles.h), fp32, d = 80, 96 and above 128.
 #include "paged_tiles.h"
 
 namespace attnw {

@@ -26,7 +26,7 @@ template <typename T, int UB, bool BYTES = false> struct TilesCfg {
     static constexpr bool F32 = sizeof(T) == 4 && !BYTES;      // on chip
     static constexpr int PARTS = sizeof(T) == 4 && BYTES ? 3 : 1;
     static constexpr int NX = !F32 && PARTS == 1 && UB <= 5 ? 2 : 1;         // blocks of 16 rows of a wave
-    static constexpr int NW = F32 || UB <= 5 ? 4 : 8;          // waves
+    static constexpr int NW = F32 || (UB <= 5 && PARTS == 1) ? 4 : 8;        // waves (PARTS = 3, with four: 512 tokens over 3584 slots, d = 160 316 instead of 158 us)
     static constexpr int ROWS = 16 * NX * NW, UNIT = F32 ? 64 : 128, KT = F32 ? 16 : 32;   // keys of a tile
     static constexpr int DB = UB * 64, CPR = UB * 4, TILE = KT * DB, XFERS = TILE / 1024, XW = (XFERS + NW - 1) / NW;
     static constexpr int COLS = DB / (F32 ? 4 : 2), CB = COLS / 16;
@@ -47,7 +47,7 @@ template <> struct TilesArgs<true> { using type = ByteAttendArgs; };
 
 // SHORT: by how many bytes a row in memory (of bytes: as bf16) is shorter than on chip (up to d = 160: 0 or 32; beyond, -1: known at run time).
 template <typename T, int UB, int SHORT, int MODE, bool UNIFORM, bool BYTES = false, int THREADS = 64 * TilesCfg<T, UB, BYTES>::NW,
-          int BLOCKS = (UB > (TilesCfg<T, UB, BYTES>::F32 ? 8 : 5)) ? 1 : 2>
+          int BLOCKS = TilesCfg<T, UB, BYTES>::NW == 8 || (UB > (TilesCfg<T, UB, BYTES>::F32 ? 8 : 5)) ? 1 : 2>
 __global__ __launch_bounds__(THREADS, BLOCKS)
 void paged_tiles_kernel(typename TilesArgs<BYTES>::type a, int grain)
 {
@@ -924,12 +924,12 @@ template <typename T, int MODE> hipError_t launch_tiles(const PagedArgs& p, hipS
     });
 }
 
-// (fp32: beyond d = 128 only, prefers_byte_tiles says why)
+// (fp32: d = 80 and 96, and beyond 128, prefers_byte_tiles says why)
 template <typename T, typename F> auto by_byte_row(int row_bytes, F&& f)
 {
     if constexpr (sizeof(T) == 4) {
         const int ub = (2 * row_bytes + 63) / 64;
-        return ub <= 5 ? f(IC<5>{}) : ub <= 6 ? f(IC<6>{}) : f(IC<8>{});
+        return ub <= 3 ? f(IC<3>{}) : ub <= 5 ? f(IC<5>{}) : ub <= 6 ? f(IC<6>{}) : f(IC<8>{});
     } else {
         return by_row<T>(2 * row_bytes, f);
     }
