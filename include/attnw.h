@@ -441,7 +441,8 @@ int64_t attnw_byte_paged_workspace(const attnw_byte_cache *cache, int64_t tokens
 
 /*
  * attnw_paged_attention over a cache in 8 bits, by the same rule, with the values that its elements stand for (bf16 holds them exactly: nothing of the cache is rounded
- * again).  bf16: as there.  fp32: queries and weights in three bf16 parts, which hold 24 bits (of numbers from 2^-110 to 2^127), fp32 sums.
+ * again).  bf16: as there.  fp32: queries and weights in three bf16 parts, which hold 24 bits (of numbers from 2^-110 to 2^127; an infinite query
+ * makes its row NaN), fp32 sums.
  */
 int attnw_byte_paged_attention(const attnw_byte_cache *cache, const attnw_rule *rule, const void *Q,
                            void *O, float *lse, const int32_t *starts, int64_t tokens,

@@ -208,6 +208,16 @@ def test_counts_in_no_order():
             assert bool((whole[:4096] == 91).all()) and bool((whole[-4096:] == 91).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sequences,block", [([(4500, 4600)], 32), ([(1, i % 97 + 1) for i in range(1500)], 8)], ids=["a long prompt", "1500 sequences"])
+def test_sizes_that_are_large(dtype, sequences, block):
+    p = Problem8(dtype, sequences, 2, 1, 32, 64, block, seed=23).on_gpu()
+    x = new_rows(p, 5)
+    R, q, want_R, want = run(p, x, 32, rows=4700)
+    within(R, want_R.double(), 2 * bound_of(q, dtype), "R")
+    check(p, want)
+
+
 def test_far_pages():
     """Offsets past 2^32 bytes: the last pages of a pool of five GiB."""
     pages, page, d, heads = 327680, 64, 64, 4

@@ -188,6 +188,30 @@ def test_long_runs_of_tiles(kernel, dtype, d, more):
         check(Problem8(dtype, [(70, m)], 2, 1, d, 32, block, seed=m, **more))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 96, 160])
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+def test_queries_that_are_no_numbers(kernel, dtype, d, what):
+    """They make their own rows NaN, and change no bit of the others."""
+    p = Problem8(dtype, [(70, 900), (1, 333)], 4, 2, d, 32, 16, seed=21)
+    p.on_gpu()
+    O, lse = (x.clone() for x in p.run_attention())
+    bad = torch.zeros((p.T, 4), dtype=torch.bool)
+    for t, h in ((0, 0), (7, 3), (33, 1), (69, 2), (70, 0)):
+        bad[t, h] = True
+        p.dev["Q"][t, h * d + 5] = what
+    got, got_lse = p.run_attention()
+    bad = bad.cuda()
+    assert torch.equal(got[~bad], O[~bad]) and torch.equal(got_lse[~bad], lse[~bad])
+    assert bool(got[bad].isnan().all()) and bool(got_lse[bad].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sequences,d", [([(1, 200001), (3, 70007)], 16), ([(4500, 4500)], 32), ([(1, i % 97 + 1) for i in range(1500)], 16)], ids=["long rows", "a long prompt", "1500 sequences"])
+def test_sizes_that_are_large(dtype, sequences, d):
+    check(Problem8(dtype, sequences, 2, 1, d, 64, 32, seed=22))
+
+
 def test_far_pages(kernel):
     """Offsets past 2^32 bytes: keys and values in the last pages of a pool of five GiB."""
     p = Problem8("bf16", [(40, 150), (1, 64)], 8, 4, 64, 64, 32, seed=14, garbage=False)
