@@ -48,11 +48,13 @@ template <typename T, int V, bool INTERLEAVED> hipError_t launch(const RotaryArg
     return hipGetLastError();
 }
 
+// The widest units that rows, halves and the rest are whole ones of.  (8974 tokens of 16 heads of 72, bf16, 18 columns by pairs: two
+// at a time 16.1 us, one 26.2; 36 columns by halves, two 17.2, one 24.1.)
 template <typename T, int V> hipError_t launch_typed(const RotaryArgs& a, const AxesView& axes, hipStream_t stream)
 {
-    const bool chunks = turns_by_chunks(V, a.d, a.rot, a.q_stride, a.r_stride, a.interleaved);
-    if (a.interleaved) return chunks ? launch<T, V, true>(a, axes, stream) : launch<T, 1, true>(a, axes, stream);
-    return chunks ? launch<T, V, false>(a, axes, stream) : launch<T, 1, false>(a, axes, stream);
+    if constexpr (V > 1)
+        if (!turns_by_chunks(V, a.d, a.rot, a.q_stride, a.r_stride, a.interleaved)) return launch_typed<T, V / 2>(a, axes, stream);
+    return a.interleaved ? launch<T, V, true>(a, axes, stream) : launch<T, V, false>(a, axes, stream);
 }
 
 // step[j]: the exponent of 2 that column j's frequency is the inverse of

@@ -68,7 +68,8 @@ def turned(x, table, positions, pairs, order, layout, inverse=False):
 
 # tokens, heads, d, pairs: sections that vectors do and do not fall into, whole heads and parts, one axis to four
 SHAPES = [(1, 1, 64, [32]), (37, 3, 128, [16, 24, 24]), (300, 2, 128, [64]), (33, 5, 80, [14, 13, 13]), (70, 4, 64, [5, 3, 7, 1]), (9, 4, 256, [32, 96]),
-          (1000, 1, 64, [1, 1, 1]), (3, 2, 72, [12, 12, 12]), (129, 20, 48, [2, 6]), (5, 3, 50, [7, 4]), (2, 1, 16, [4, 4])]
+          (1000, 1, 64, [1, 1, 1]), (3, 2, 72, [12, 12, 12]), (129, 20, 48, [2, 6]), (5, 3, 50, [7, 4]), (2, 1, 16, [4, 4]),
+          (33, 3, 36, [4, 5]), (21, 2, 36, [6, 4]), (11, 5, 26, [5, 4, 4]), (301, 16, 72, [1, 3, 2, 3]), (71, 7, 44, [10, 2])]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
