@@ -201,6 +201,8 @@ void byte_append_kernel(AppendArgs a)
                 uint8_t* const p = to + (n == 0 ? c.a : c.b);
                 if constexpr (V == 1) {
                     *p = (uint8_t)pack_e4m3<false>(y[n][0], 0.0f, 0, scale_up);
+                } else if constexpr (V == 2) {
+                    *reinterpret_cast<uint16_t*>(p) = (uint16_t)pack_e4m3<false>(y[n][0], y[n][1], 0, scale_up);
                 } else {
                     uint32_t w[V / 4 > 0 ? V / 4 : 1];
 #pragma unroll
@@ -329,11 +331,13 @@ template <typename T, int V, bool INTERLEAVED> hipError_t launch(AppendArgs a, h
     return go(byte_append_kernel<T, V, INTERLEAVED, 256>, 256);
 }
 
+// The widest units that rows, halves and the rest are whole ones of.  (9000 tokens, 32 heads on 8 of 128, bf16, us: pairs, 100 columns turned, four at a time 65, one 158; 98, two at
+// a time 88, one 159; halves, 120 columns, four 77, one 143; 98 by one 158.)
 template <typename T, int V> hipError_t launch_typed(const RotaryArgs& r, const AppendArgs& a, hipStream_t stream)
 {
-    const bool chunks = turns_by_chunks(V, a.d, a.rot, a.heads > 0 ? a.q_stride : V, a.kv_stride, r.interleaved);
-    if (r.interleaved) return chunks ? launch<T, V, true>(a, stream) : launch<T, 1, true>(a, stream);
-    return chunks ? launch<T, V, false>(a, stream) : launch<T, 1, false>(a, stream);
+    if constexpr (V > 1)
+        if (!turns_by_chunks(V, a.d, a.rot, a.heads > 0 ? a.q_stride : V, a.kv_stride, r.interleaved)) return launch_typed<T, V / 2>(r, a, stream);
+    return r.interleaved ? launch<T, V, true>(a, stream) : launch<T, V, false>(a, stream);
 }
 
 }  // namespace
