@@ -428,6 +428,7 @@ typedef struct attnw_byte_cache {
  * number that the cache holds.  A block's scale is the least 2^e, e from -117 to 119, with |x| <= 448 2^e for all its new rows, and not less than the one it
  * had where it had rows before the new ones; where that grows, those are rounded again in place (times a power of 2: what stays above 2^-6 of the scale keeps
  * its value).  NaN and infinities become NaN and do not count for the scale; beyond 448 2^119 numbers become that.
+ * block d: 2^30 at most.
  */
 int attnw_byte_cache_append(const attnw_byte_cache *cache, const void *Q, const void *K,
                         const void *V, void *R, const float *table,

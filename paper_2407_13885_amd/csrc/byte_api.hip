@@ -54,6 +54,7 @@ int check_block(const attnw_byte_cache* c)   // (of a cache whose sizes are supp
     if (c->block < 1 || c->block > c->cache.page_size || c->cache.page_size % c->block != 0) return ATTNW_ERR_UNSUPPORTED;
     return cache_bytes(&c->cache, 1) < (int64_t)1 << 47 ? ATTNW_OK : ATTNW_ERR_UNSUPPORTED;   // (kernels keep scales beside 48 bits of a place)
 }
+constexpr int64_t kMostBlock = (int64_t)1 << 30;    // elements of a block and head: appending counts its units, a column each at the least, in 32 bits
 int64_t scale_bytes(const attnw_byte_cache* c) { return c->cache.pages * c->cache.kv_heads * (c->cache.page_size / c->block); }
 ScalesView scales(const attnw_byte_cache* c)
 {
@@ -163,6 +164,7 @@ int attnw_byte_cache_append(const attnw_byte_cache* cache, const void* Q, const 
         mul_overflows(n, size, &n) || mul_overflows(tokens, wide, &n) || mul_overflows(n, size, &n) || mul_overflows(rows, rot, &n) || mul_overflows(n, 4, &n))
         return ATTNW_ERR_SHAPE;
     if ((e = check_support(&c, 1)) != ATTNW_OK || (e = check_block(cache)) != ATTNW_OK) return e;
+    if (cache->block * c.d > kMostBlock) return ATTNW_ERR_UNSUPPORTED;
     const int64_t kv_wide = c.kv_heads * c.d;
     if (rot % 2 != 0 || rot > c.d || (rot > 0 && rows < 1) || (layout != ATTNW_HALVES && layout != ATTNW_PAIRS) || tokens > ((int64_t)1 << 30) ||
         heads > (1 << 16) || q_stride < wide || kv_stride < kv_wide)
