@@ -262,7 +262,7 @@ void byte_append_kernel(AppendArgs a)
         if (!active) continue;
         int e = exponent_for(__float_as_uint(top));
         if (first > slot0) {
-            const int old = max(kLeastScale, min(held - 127, kMostScale));
+            const int old = max(1, min(held, 127 + kMostScale)) - 127;   // (below kLeastScale where something else wrote it: scale_of)
             if (e > old) {                        // in units of the new scale
                 const float down = scale_of(127 + e - old);
                 const auto again = [&](u32x4 w) __attribute__((always_inline)) {
