@@ -169,7 +169,13 @@ void byte_append_kernel(AppendArgs a)
                 y[0][e] = wide(r.a.x[e]);
                 if constexpr (TWO) y[TWO ? 1 : 0][e] = c.b < 0 ? 0.0f : wide(r.b.x[e]);
             }
-            if (!c.turned) return;
+            if (!c.turned) {                      // (quiet, as products are: the largest of a signalling NaN and a number is NaN, and of that and the next the next)
+#pragma unroll
+                for (int n = 0; n < (TWO ? 2 : 1); ++n)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) y[n][e] = __builtin_canonicalizef(y[n][e]);
+                return;
+            }
             const int32_t pair = (u - row * (int32_t)by_row.d) * P;
             Chunk<float, P> co, si;
             load_angles<P>(a.angles, a.rot, a.rows, pair, a.axes.count, of, [&](int axis) __attribute__((always_inline)) { return position(t0 + row, axis); }, co, si);
