@@ -335,6 +335,8 @@ int64_t attnw_paged_workspace(const attnw_cache *cache, int64_t tokens, int64_t 
  *   lse[t][h] = log sum_j exp(x_j)   (lse may be NULL).
  * A row that sees nothing gives 0 and -infinity (and so may one all of whose x lie below -10^29).  Rows of
  * tokens that no sequence owns are not written.
+ * Weights of up to 2^6 are summed with V in fp32 and divided by their sum at the end: finite values give finite rows
+ * while the slots that a row sees times the largest |V| among them stay below 2^122.
  *
  * Q : rows of heads * d, q_stride apart (a multiple of 16 bytes).   O : [tokens][heads][d], dense.
  * workspace: at least attnw_paged_workspace bytes, 16-byte aligned, of any content; calls that
@@ -441,8 +443,9 @@ int attnw_byte_cache_append(const attnw_byte_cache *cache, const void *Q, const 
 int64_t attnw_byte_paged_workspace(const attnw_byte_cache *cache, int64_t tokens, int64_t heads);
 
 /*
- * attnw_paged_attention over a cache in 8 bits, by the same rule, with the values that its elements stand for (bf16 holds them exactly: nothing of the cache is rounded
- * again).  bf16: as there.  fp32: queries and weights in three bf16 parts, which hold 24 bits (of numbers from 2^-110 to 2^127; an infinite query
+ * attnw_paged_attention over a cache in 8 bits, by the same rule, with the values that its elements stand for (bf16 holds those of scales from 2^-117 on
+ * exactly: nothing that appending caches is rounded again; its greatest scale is 2^119, and the limit of 2^122 on slots times values holds here too).
+ * bf16: as there.  fp32: queries and weights in three bf16 parts, which hold 24 bits (of numbers from 2^-110 to 2^127; an infinite query
  * makes its row NaN), fp32 sums.
  */
 int attnw_byte_paged_attention(const attnw_byte_cache *cache, const attnw_rule *rule, const void *Q,
