@@ -417,6 +417,8 @@ int attnw_rotary_axes(const void *X, void *Y, const float *table, const int32_t 
  * 448, no infinities), which stands for itself times 2^(s - 127), s the byte that `block` slots of a page share for a kv head: slot
  * row r of a page has K_scales[page][kv_head][r / block] (below 1 it counts as 1, above 246 as 246).  block divides page_size.
  * d: a multiple of 16.  `dtype` is the type of queries, new tokens and outputs.
+ * Only the calls that take an attnw_byte_cache know its elements: `cache` by itself must not be given to the others (attnw_paged_sums and attnw_cache_evict
+ * among them), which would take its bytes for numbers of `dtype`.
  */
 typedef struct attnw_byte_cache {
     attnw_cache cache;          /* K, V: [pages][kv_heads][page_size][d] of bytes */

@@ -7,6 +7,8 @@
 // What bounds it: memory.  Rows of queries are turned as without a cache (rotary_common.h), by other workgroups of the same launch.  Measured: 9045 tokens, 32 heads on 8 of
 // 128, bf16, pairs of 64 columns by three axes, 206 MB 55 us = 3.75 TB/s (waves wait 73 % of their life, the vector unit works 42 % of the cycles; halves of all columns 48), fp32
 // by halves 62 to 88; eight tokens 6.2 us, a chain of the plan, the page, the rows and the largest.  Keys and values alone take 26, queries alone 38.6.
+// A block is the work of one group however long it is: the same tokens on 32 heads, halves, blocks of 16 slots 44.5 us, 128 47.6, 512 60, 1024 98, 4096 350.  A block of
+// 128 whose scale grows, a token each of 64 sequences, 9.4 instead of 7.1.
 // Workgroups of both in turns took 72, keys' angles by way of LDS 68, a block's older rows on their way early 77 (registers).
 #include "rotary_common.h"
 #include "byte_cache.h"

@@ -11,7 +11,8 @@ bool prefers_byte_tiles(const PagedArgs& p)
     const int64_t group = p.heads / p.cache.kv_heads, rows = p.tokens * group, all = p.tokens * p.heads;
     const bool f32 = p.dt == DType::F32, wide = p.cache.row_bytes > 128;
     // fp32: blocks of 16 rows, whose waves share nothing, are the faster ones up to d = 128 however many there are (512 tokens over 3584 slots, 32 heads on 8: d = 64 76 / 85 us,
-    // 128 133 / 133), but for d = 80 and 96, which do not fill their place there (132 / 106)
+    // 128 133 / 133), but for d = 80 and 96, which do not fill their place there (132 / 106).
+    // (d = 112 takes there what 128 does, 116 / 116 on another day; large blocks are not built for it.)
     if (f32 && !wide && (p.cache.row_bytes <= 64 || p.cache.row_bytes > 96)) return false;
     // (ATTNW_PAGED_KERNEL=rows / =tiles: tests and measurements compare the two)
     const char* force = getenv("ATTNW_PAGED_KERNEL");

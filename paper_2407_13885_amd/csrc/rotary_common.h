@@ -129,7 +129,7 @@ inline dim3 turn_grid(const TurnUnits& u, int64_t tokens)
     while (blocks * across < 512 && across * 256 < (uint32_t)u.per_token) ++across;
     return dim3(blocks, across);
 }
-// 16 bytes at a time where rows, halves and the rest are whole chunks of them (V elements), else element by element.
+// Whether units of V elements will do: rows, strides, halves and the rest are whole ones of them.  (Callers begin at 16 bytes and halve V until they are.)
 inline bool turns_by_chunks(int V, int64_t d, int64_t rot, int64_t x_stride, int64_t y_stride, bool interleaved)
 {
     return d % V == 0 && x_stride % V == 0 && y_stride % V == 0 && (interleaved ? rot % V == 0 : rot % (2 * V) == 0);
